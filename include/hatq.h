@@ -439,6 +439,138 @@ int32_t hatq_layer_forward(const hatq_weights *W, int32_t form, const float *x, 
                            float *act_scale, int32_t next_hblock, float *next_absmax,
                            void *ws, size_t ws_bytes, void *stream);
 
+/* ---- Linear layers over tokens -------------------------------------------------
+ *
+ * The fully connected layer Y = X W^T + b of rows of tokens, in the DH form
+ * (Eq. double_hadamard_quantization) with a scale for each token instead of one
+ * for each sample, one layer or several experts.  For token t, channel c, block
+ * b = hblock:
+ *   S[t]   = B_cin x[t]                      fp32 butterflies, ascending stages
+ *   s[t]   = fl32(max|S[t]| / 127)           1 where that is 0
+ *   q[t,d] = clamp(rne(fl32(S[t,d] / s[t])), -127, 127)
+ *   z[t,c] = fma(float(sum_d q[t,d] wq[c,d]), fl(s[t] w_scale[c]) (1/b), bias[c])
+ *   y[t,c] = z[t,c], or for a gated layer, which holds 2 cout channels, gates
+ *            first: g u / (1 + exp(-g)) with g = z[t,c], u = z[t,cout+c].
+ * The sums are exact in INT32.  y is rounded once, to y_type.  A token that
+ * holds a NaN or an infinity, or whose transform overflows fp32, has the scale
+ * NaN and codes 0: its outputs are NaN, every other token's are unaffected.
+ *
+ * Here rows have strides, in elements; the elements of a row are adjacent.  A
+ * call with no rows is HATQ_OK and launches nothing, one of more than 2^24 rows
+ * HATQ_EUNSUPPORTED.  x and y may have any
+ * alignment of their type (rows at multiples of 16 bytes are read and written
+ * faster); codes and prepared weights are 16-byte aligned.  No kernel's result
+ * depends on the order in which blocks run. */
+typedef enum { HATQ_F32 = 0, HATQ_BF16 = 1, HATQ_F16 = 2 } hatq_dtype;
+
+/* Prepared linear weights: a plain view into the caller's device buffer.
+ * experts >= 1 layers of the same shape.  k_stride = cin rounded up to 64 is the
+ * row stride of the layer's input codes; cout_pad the channels held, a gated
+ * layer's gates and values taken 32 by 32 in turn, rounded up to 32 each.
+ * wpack holds the codes in the kernels' order (library-internal): per expert,
+ * per 16 channels, per 64-deep contraction step, 1 KB as [4][16 channels][16].
+ * w_scale and bias are fp32 [experts][cout_pad] in wpack's channel order, 0 in
+ * the padding. */
+typedef struct {
+    int32_t experts, cin, cout;
+    int32_t gated;          /* 1: holds 2 cout channels, gives cout */
+    int32_t hblock;         /* transform block on cin, a power of two in [1, 128] */
+    int32_t k_stride, cout_pad;
+    int8_t *wpack;
+    float *w_scale;
+    float *bias;
+} hatq_linear_weights;
+
+/* Bytes of device memory for such weights; 0 for sizes that are not supported
+ * (cin % hblock != 0, cin or held channels over 65536, experts over 1024). */
+size_t hatq_linear_weights_bytes(int32_t experts, int32_t cin, int32_t cout, int32_t gated, int32_t hblock);
+
+/* Weights from floats: w device [experts][held][cin] of w_type (held = cout, or
+ * 2 cout for a gated layer: gates, then values), bias device fp32
+ * [experts][held] or NULL.  As hatq_prepare_weights: the transform in fp64,
+ * rounded once to fp32, w_scale = fl32(max|W'| / 127) (1 for a zero row), codes
+ * clamp(rne(fl32(W' / w_scale)), -127, 127).
+ *   dst: device buffer of at least hatq_linear_weights_bytes, 256-byte aligned;
+ *   *out receives the view into it.  Runs on `stream`. */
+int32_t hatq_prepare_linear(int32_t experts, int32_t cin, int32_t cout, int32_t gated, int32_t hblock, const void *w,
+                            int32_t w_type, const float *bias, void *dst, size_t dst_bytes,
+                            hatq_linear_weights *out, void *stream);
+
+/* The same from codes quantized elsewhere (a deployment checkpoint): codes
+ * device int8 [experts][held][cin] of the transformed weights, w_scale device
+ * fp32 [experts][held], bias fp32 [experts][held] or NULL. */
+int32_t hatq_pack_linear(int32_t experts, int32_t cin, int32_t cout, int32_t gated, int32_t hblock,
+                         const int8_t *codes, const float *w_scale, const float *bias, void *dst, size_t dst_bytes,
+                         hatq_linear_weights *out, void *stream);
+
+/* Codes and scales of tokens.
+ *   x:  device [rows][cin] of x_type, row stride x_stride >= cin elements.
+ *   xq: device int8 [rows][k_stride], k_stride = cin rounded up to 64, the bytes
+ *       past cin written 0; act_scale: device fp32 [rows].
+ * cin % hblock == 0, cin <= 65536, hblock a power of two in [1, 128]
+ * (HATQ_EUNSUPPORTED for the orders 192 and 320). */
+int32_t hatq_token_quant(const void *x, int32_t x_type, int32_t rows, int32_t cin, int64_t x_stride, int32_t hblock,
+                         int8_t *xq, float *act_scale, void *stream);
+
+/* The product of token codes with one layer's weights (W->experts == 1) and its
+ * epilogue.
+ *   xq, act_scale: as hatq_token_quant writes them (any bytes past cin).
+ *   y: device [rows][cout] of y_type, row stride y_stride >= cout elements. */
+int32_t hatq_linear_int8(const hatq_linear_weights *W, const int8_t *xq, const float *act_scale, int32_t rows,
+                         void *y, int32_t y_type, int64_t y_stride, void *stream);
+
+/* The whole layer, floats in: hatq_token_quant into the workspace, then
+ * hatq_linear_int8.  ws: device memory, 256-byte aligned, of at least
+ * hatq_linear_ws_bytes(W, rows) bytes. */
+size_t hatq_linear_ws_bytes(const hatq_linear_weights *W, int32_t rows);
+int32_t hatq_linear_forward(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t rows,
+                            int64_t x_stride, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,
+                            void *stream);
+
+/* Products grouped by expert: output row i belongs to the first expert e with
+ * i < ends[e] and takes the codes of token src[i].
+ *   ends: device int32 [experts], the experts' row ends, ascending; values are
+ *         taken into [the end before, rows], so no contents make a call unsafe.
+ *         Rows past the last end are written 0.
+ *   src:  device int32 [rows], or NULL (then x_rows >= rows, token i).  A value
+ *         outside [0, x_rows) stands for an empty token: y is the layer's output
+ *         for x = 0, its bias (gated: of its biases).
+ *   x_rows: tokens in xq and act_scale (at least 1 where rows is). */
+int32_t hatq_experts_int8(const hatq_linear_weights *W, const int8_t *xq, const float *act_scale, int32_t x_rows,
+                          const int32_t *ends, const int32_t *src, int32_t rows, void *y, int32_t y_type,
+                          int64_t y_stride, void *stream);
+
+/* The same, floats in: the x_rows tokens are quantized once each.  ws: at least
+ * hatq_linear_ws_bytes(W, x_rows) bytes, 256-byte aligned. */
+int32_t hatq_experts_forward(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t x_rows,
+                             int64_t x_stride, const int32_t *ends, const int32_t *src, int32_t rows, void *y,
+                             int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* The rows of hatq_experts_* from each token's chosen experts: a stable counting
+ * sort of the pairs p = t topk + j by ids[p].
+ *   ids:  device int32 [tokens][topk]; a pair whose id is outside [0, experts)
+ *         is masked: it has no row.
+ *   ends: device int32 [experts], written.
+ *   src:  device int32 [tokens topk], written: the token of each row, -1 past the
+ *         last end.
+ *   pos:  device int32 [tokens topk], written: the row of each pair, -1 for a
+ *         masked one.
+ *   ws:   device memory, 256-byte aligned, of at least hatq_expert_order_ws_bytes
+ *         bytes (0 for sizes that are not supported: tokens topk over 2^24,
+ *         experts over 1024). */
+size_t hatq_expert_order_ws_bytes(int32_t tokens, int32_t topk, int32_t experts);
+int32_t hatq_expert_order(const int32_t *ids, int32_t tokens, int32_t topk, int32_t experts, int32_t *ends,
+                          int32_t *src, int32_t *pos, void *ws, size_t ws_bytes, void *stream);
+
+/* The weighted sum of each token's rows, y[t] = sum_j weights[t,j] h[pos[t,j]],
+ * fp32 fma in ascending j, rounded once to y_type.
+ *   h: device fp32 [h_rows][cols], row stride h_stride elements.
+ *   pos: device int32 [tokens][topk]; a value outside [0, h_rows) adds nothing
+ *   (a token with none gives 0).  weights: device fp32 [tokens][topk]. */
+int32_t hatq_expert_combine(const float *h, int32_t h_rows, int32_t cols, int64_t h_stride, const int32_t *pos,
+                            const float *weights, int32_t tokens, int32_t topk, void *y, int32_t y_type,
+                            int64_t y_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,387 @@
+// INT8 products of token codes with linear weights, one layer or grouped by expert,
+// and their epilogue: z = fma(float(acc), fl(s w_scale) / b, bias), the gated unit,
+// one rounding to the output type.
+//
+// Operand roles: the weights are the MFMA's first operand, the tokens its second, so
+// an accumulator lane holds one token and runs of four adjacent channels, which it
+// stores as one piece.  The contraction index inside a 64-byte step is the same
+// permutation on both sides, which an integer sum does not see.
+#include "hatq_device.h"
+#include "linear.h"
+#include "linear_device.h"
+
+namespace hatq {
+namespace {
+
+typedef int v16i __attribute__((ext_vector_type(16)));
+
+#define HATQ_LDS(p) ((__attribute__((address_space(3))) void *)(p))
+#define HATQ_GLOBAL(p) ((__attribute__((address_space(1))) const void *)(p))
+
+// At most N of this wave's memory operations under way, none of its LDS reads.
+template <int N>
+__device__ __forceinline__ void wait_vmcnt_lds() {
+    static_assert(N >= 0 && N < 64, "vmcnt");
+    // s_waitcnt simm16 (gfx9): vmcnt[3:0], expcnt[6:4]=7, lgkmcnt[11:8]=0, vmcnt_hi[15:14]
+    __builtin_amdgcn_s_waitcnt((N & 15) | 0x70 | ((N >> 4) << 14));
+}
+
+// ---- which rows a tile has --------------------------------------------------------
+struct RowTile {
+    int expert;     // -1: rows past the last end, written 0
+    int row0, end;  // rows [row0, min(row0 + BM, end))
+};
+
+// Row tiles of BM rows, each expert's rows starting a tile of their own: tile t of
+// them, or false past the last.  Every lane of the wave takes part; the ends are
+// clamped here, so any contents give rows in [0, rows).
+template <int BM>
+__device__ bool row_tile(const LinearArgs &a, int t, RowTile &r) {
+    if (!a.ends) {
+        r = {0, t * BM, a.rows};
+        return r.row0 < a.rows;
+    }
+    const int lane = threadIdx.x & 63;
+    int last = 0, tiles = 0;
+    for (int base = 0; base < a.experts; base += 64) {
+        const int i = base + lane;
+        int end = i < a.experts ? a.ends[i] : 0;
+        end = max(min(end, a.rows), last);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(end, o, 64);
+            if (lane >= o) end = max(end, u);
+        }
+        int begin = __shfl_up(end, 1, 64);
+        if (lane == 0) begin = last;
+        const int n = (end - begin + BM - 1) / BM;
+        int c = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(c, o, 64);
+            if (lane >= o) c += u;
+        }
+        const int first = tiles + c - n;
+        const uint64_t hit = __ballot(t >= first && t < first + n);
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            r.expert = base + l;
+            r.row0 = __builtin_amdgcn_readlane(begin, l) + (t - __builtin_amdgcn_readlane(first, l)) * BM;
+            r.end = __builtin_amdgcn_readlane(end, l);
+            return true;
+        }
+        last = __builtin_amdgcn_readlane(end, 63);
+        tiles += __builtin_amdgcn_readlane(c, 63);
+    }
+    r = {-1, last + (t - tiles) * BM, a.rows};
+    return r.row0 < a.rows;
+}
+
+// Upper bound of the row tiles over any ends (host).
+int64_t row_tiles(const LinearArgs &a, int bm) {
+    const int64_t full = (a.rows + bm - 1) / bm;
+    if (!a.ends) return full;
+    // each group adds at most one part tile, and there are at most `rows` groups
+    const int64_t groups = a.experts + 1 < a.rows ? a.experts + 1 : a.rows;
+    return a.rows / bm + groups;
+}
+
+// Token of an output row; -1 for an empty one.
+__device__ __forceinline__ int token_of(const LinearArgs &a, int row) {
+    if (!a.src) return row;
+    const int t = a.src[row];
+    return (unsigned)t < (unsigned)a.x_rows ? t : -1;
+}
+
+// ---- epilogue -----------------------------------------------------------------------
+// g / (1 + exp(-g)) u by the hardware's exp2 and reciprocal (1 ulp each; the product
+// -g log2 e rounds to |g| 2^-24 of the result, 1e-6 where it is still 1e-6 of g).
+__device__ __forceinline__ float gated_unit(float g, float u) {
+    const float e = __builtin_amdgcn_exp2f(g * -1.44269504f);
+    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+}
+
+// z of four adjacent packed columns, at column p of the expert's factors.
+__device__ __forceinline__ void dequant4(const LinearArgs &a, const float *w_scale, const float *bias, int p,
+                                         const int *acc, float s, float *z) {
+    const float4 w = *reinterpret_cast<const float4 *>(w_scale + p), b = *reinterpret_cast<const float4 *>(bias + p);
+    z[0] = __builtin_fmaf((float)acc[0], s * w.x * a.inv_b, b.x);
+    z[1] = __builtin_fmaf((float)acc[1], s * w.y * a.inv_b, b.y);
+    z[2] = __builtin_fmaf((float)acc[2], s * w.z * a.inv_b, b.z);
+    z[3] = __builtin_fmaf((float)acc[3], s * w.w * a.inv_b, b.w);
+}
+
+template <typename T>
+__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z, bool vec) {
+    T *y = static_cast<T *>(a.y) + row * a.y_stride + c;
+    if (vec && c + 4 <= a.cout) {
+        store4(y, z);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (c + j < a.cout) y[j] = from_float<T>(z[j]);
+    }
+}
+__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z, bool vec) {
+    if (a.y_type == kBf16) put4<bf16_t>(a, row, c, z, vec);
+    else if (a.y_type == kF16) put4<_Float16>(a, row, c, z, vec);
+    else put4<float>(a, row, c, z, vec);
+}
+
+__device__ __forceinline__ bool vector_rows(const LinearArgs &a) {
+    const int size = a.y_type == kF32 ? 4 : 2;
+    return (reinterpret_cast<uintptr_t>(a.y) & (4 * size - 1)) == 0 && (a.y_stride & 3) == 0;
+}
+
+// Rows of a tile past the last end: BN outputs each of zeros.
+__device__ void zero_tile(const LinearArgs &a, int row0, int rows, int c0, int cols) {
+    const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const bool vec = vector_rows(a);
+    const int groups = cols / 4;
+    for (int u = threadIdx.x; u < rows * groups; u += blockDim.x) {
+        const int r = u / groups, c = c0 + (u - r * groups) * 4;
+        if (c < a.cout) put4(a, row0 + r, c, z, vec);
+    }
+}
+
+// ---- few rows -------------------------------------------------------------------------
+// A block takes 16 output channels (gated: of their gates and their values) and 16 MT
+// rows; its waves share the contraction, 64 bytes in turn, and add up in LDS.  The
+// weights go from memory to registers in runs of 1 KB, U of them in flight a wave:
+// the kernel is bound by their bytes.
+template <int MT, int G, int U>
+__global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) {
+    constexpr int WAVES = 8;
+    __shared__ v4i part[WAVES][MT][G][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int groups = (a.cout + 15) / 16;
+    const int bid = blockIdx.y * gridDim.x + blockIdx.x;
+    const int t = bid / groups, c16 = bid - t * groups;
+    RowTile r;
+    if (!row_tile<16 * MT>(a, t, r)) return;
+    const int rows = min(r.end - r.row0, 16 * MT);
+    if (r.expert < 0) return zero_tile(a, r.row0, rows, c16 * 16, 16);
+
+    const int nks = a.k_stride >> 6;
+    const int block0 = G == 1 ? c16 : (c16 >> 1) * 4 + (c16 & 1);   // of 16 packed columns
+    const int8_t *w = a.wp + ((int64_t)r.expert * a.cout_pad + block0 * 16) * a.k_stride + lane * 16;
+    const int64_t value = (int64_t)32 * a.k_stride;   // from the gates' columns to the values'
+    const int8_t *x[MT];
+    float s[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int tok = token_of(a, r.row0 + min(16 * m + (lane & 15), rows - 1));
+        x[m] = a.xq + (int64_t)max(tok, 0) * a.k_stride + (lane >> 4) * 16;
+        s[m] = tok < 0 ? 0.0f : a.sx[tok];
+    }
+    v4i acc[MT][G];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int g = 0; g < G; ++g) acc[m][g] = v4i{0, 0, 0, 0};
+    for (int k0 = wave; k0 < nks; k0 += WAVES * U) {
+        v4i fw[U][G], fx[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = min(k0 + WAVES * u, nks - 1);
+#pragma unroll
+            for (int g = 0; g < G; ++g) fw[u][g] = *reinterpret_cast<const v4i *>(w + g * value + (int64_t)k * 1024);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) fx[u][m] = *reinterpret_cast<const v4i *>(x[m] + k * 64);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k0 + WAVES * u >= nks) break;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    acc[m][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][g], fx[u][m], acc[m][g], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int g = 0; g < G; ++g) part[wave][m][g][lane] = acc[m][g];
+    __syncthreads();
+    const bool vec = vector_rows(a);
+    const float *w_scale = a.w_scale + (int64_t)r.expert * a.cout_pad, *bias = a.bias + (int64_t)r.expert * a.cout_pad;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        if (m % WAVES != wave) continue;
+        float z[2][4];
+        const int p = block0 * 16 + (lane >> 4) * 4;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            v4i sum = part[0][m][g][lane];
+#pragma unroll
+            for (int k = 1; k < WAVES; ++k) sum += part[k][m][g][lane];
+            const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
+            dequant4(a, w_scale, bias, p + 32 * g, q, s[m], z[g]);
+        }
+        if (G == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
+        }
+        const int row = 16 * m + (lane & 15), c = c16 * 16 + (lane >> 4) * 4;
+        if (row < rows && c < a.cout) put4(a, r.row0 + row, c, z[0], vec);
+    }
+}
+
+// ---- many rows --------------------------------------------------------------------------
+// Tiles of BM rows x BN packed columns by WM x WN waves of FM x FN MFMAs of 32 x 32,
+// the contraction in steps of 64 bytes through a ring of STAGES LDS buffers that are
+// filled by direct-to-LDS loads.  A row's four 16-byte pieces of a step are permuted
+// by the row (piece c of row m at place c ^ (m >> 1 & 3)), so the reads of 32 rows'
+// fragments do not meet in a bank; the weights lie in memory as they are read.
+template <int WM, int WN, int FM, int FN, int STAGES, int G>
+__global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearArgs a) {
+    constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
+    constexpr int A_INSTR = BM / 16 / NW, B_INSTR = BN / 16 / NW, PER_STAGE = A_INSTR + B_INSTR;
+    constexpr int STAGE_BYTES = (BM + BN) * 64;
+    static_assert(A_INSTR * NW * 16 == BM && B_INSTR * NW * 16 == BN && FN % G == 0, "tile");
+    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE_BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    const int tiles_n = (a.cout_pad + BN - 1) / BN;
+    const int bid = blockIdx.y * gridDim.x + blockIdx.x;
+    const int t = bid / tiles_n, tn = bid - t * tiles_n;
+    RowTile r;
+    if (!row_tile<BM>(a, t, r)) return;
+    const int rows = min(r.end - r.row0, BM);
+    if (r.expert < 0) return zero_tile(a, r.row0, rows, tn * BN / G, BN / G);
+
+    const int nks = a.k_stride >> 6;
+    const int8_t *pa[A_INSTR], *pb[B_INSTR];
+#pragma unroll
+    for (int j = 0; j < A_INSTR; ++j) {
+        const int m = 16 * (wave + NW * j) + (lane >> 2);
+        const int tok = token_of(a, r.row0 + min(m, rows - 1));
+        pa[j] = a.xq + (int64_t)max(tok, 0) * a.k_stride + 16 * ((lane & 3) ^ ((m >> 1) & 3));
+    }
+#pragma unroll
+    for (int j = 0; j < B_INSTR; ++j) {
+        const int block = min(tn * (BN / 16) + wave + NW * j, a.cout_pad / 16 - 1);
+        pb[j] = a.wp + ((int64_t)r.expert * a.cout_pad + block * 16) * a.k_stride + lane * 16;
+    }
+    auto issue = [&](int ks) {
+        int8_t *to = lds + (ks % STAGES) * STAGE_BYTES;
+#pragma unroll
+        for (int j = 0; j < A_INSTR; ++j)
+            __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(pa[j] + ks * 64), HATQ_LDS(to + 1024 * (wave + NW * j)), 16, 0, 0);
+#pragma unroll
+        for (int j = 0; j < B_INSTR; ++j)
+            __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(pb[j] + (int64_t)ks * 1024),
+                                             HATQ_LDS(to + BM * 64 + 1024 * (wave + NW * j)), 16, 0, 0);
+    };
+    int fa[FM][2], fb[FN][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int c = 2 * h + (lane >> 5);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int m = (wm * FM + i) * 32 + (lane & 31);
+            fa[i][h] = m * 64 + 16 * (c ^ ((m >> 1) & 3));
+        }
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+            fb[j][h] = BM * 64 + ((wn * FN + j) * 2 + ((lane >> 4) & 1)) * 1024 + c * 256 + (lane & 15) * 16;
+    }
+    v16i acc[FN][FM];
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[j][i][e] = 0;
+
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+        if (k < nks) issue(k);
+    for (int ks = 0; ks < nks; ++ks) {
+        // this step's loads have landed (those of up to STAGES - 2 later steps may be under way)
+        if (ks + STAGES - 2 < nks) wait_vmcnt_lds<(STAGES - 2) * PER_STAGE>();
+        else wait_vmcnt_lds<0>();
+        __builtin_amdgcn_s_barrier();   // for every wave; and every wave has left the buffer filled next
+        if (ks + STAGES - 1 < nks) issue(ks + STAGES - 1);
+        const int8_t *from = lds + (ks % STAGES) * STAGE_BYTES;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v4i xa[FM], wb[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) xa[i] = *reinterpret_cast<const v4i *>(from + fa[i][h]);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) wb[j] = *reinterpret_cast<const v4i *>(from + fb[j][h]);
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+                    acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wb[j], xa[i], acc[j][i], 0, 0, 0);
+        }
+    }
+
+    const bool vec = vector_rows(a);
+    const float *w_scale = a.w_scale + (int64_t)r.expert * a.cout_pad, *bias = a.bias + (int64_t)r.expert * a.cout_pad;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int row = (wm * FM + i) * 32 + (lane & 31);
+        if (row >= rows) continue;
+        const int tok = token_of(a, r.row0 + row);
+        const float s = tok < 0 ? 0.0f : a.sx[tok];
+#pragma unroll
+        for (int j = 0; j < FN; j += G)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                // packed column of element 0: rows 8 q + 4 (lane / 32) of the 32 x 32 tile
+                const int in = 8 * q + 4 * (lane >> 5), p = tn * BN + (wn * FN + j) * 32 + in;
+                if (p >= a.cout_pad) continue;
+                float z[2][4];
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const int v[4] = {acc[j + g][i][4 * q], acc[j + g][i][4 * q + 1], acc[j + g][i][4 * q + 2],
+                                      acc[j + g][i][4 * q + 3]};
+                    dequant4(a, w_scale, bias, p + 32 * g, v, s, z[g]);
+                }
+                if (G == 2) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[0][e] = gated_unit(z[0][e], z[1][e]);
+                }
+                const int c = G == 1 ? p : (tn * BN + (wn * FN + j) * 32) / 2 + in;
+                if (c < a.cout) put4(a, r.row0 + row, c, z[0], vec);
+            }
+    }
+}
+
+template <int MT, int U>
+void stream(const LinearArgs &a, hipStream_t st) {
+    const dim3 grid = grid_of(row_tiles(a, 16 * MT) * ((a.cout + 15) / 16));
+    if (a.gated) linear_stream_kernel<MT, 2, U><<<grid, 512, 0, st>>>(a);
+    else linear_stream_kernel<MT, 1, U><<<grid, 512, 0, st>>>(a);
+}
+
+template <int WM, int WN, int FM, int FN, int STAGES>
+void tile(const LinearArgs &a, hipStream_t st) {
+    constexpr int BM = WM * FM * 32, BN = WN * FN * 32;
+    const dim3 grid = grid_of(row_tiles(a, BM) * ((a.cout_pad + BN - 1) / BN));
+    if (a.gated) linear_tile_kernel<WM, WN, FM, FN, STAGES, 2><<<grid, 64 * WM * WN, 0, st>>>(a);
+    else linear_tile_kernel<WM, WN, FM, FN, STAGES, 1><<<grid, 64 * WM * WN, 0, st>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_linear(const LinearArgs &a, hipStream_t st) {
+    // rows a group has on average
+    const int64_t per = a.ends ? (a.rows + a.experts - 1) / a.experts : a.rows;
+    if (per <= 16) stream<1, 8>(a, st);
+    else if (per <= 32) stream<2, 4>(a, st);
+    else if (per <= 64) stream<4, 4>(a, st);
+    else {
+        const int64_t big = row_tiles(a, 256) * ((a.cout_pad + 255) / 256);
+        if (big >= 256) tile<2, 4, 4, 2, 4>(a, st);
+        else tile<2, 2, 2, 2, 4>(a, st);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace hatq

@@ -1,0 +1,415 @@
+// Linear layers over tokens: token codes, weight preparation, and the order and
+// the weighted sum of expert rows.  The products are in linear.hip.
+#include "hatq_device.h"
+#include "linear.h"
+#include "linear_device.h"
+
+namespace hatq {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---- token codes ----------------------------------------------------------------
+// S = B x per token, s = fl32(max|S| / 127), q = clamp(rne(fl32(S / s))).
+//
+// A token's row stays in registers between its maximum and its codes, so x is read
+// once.  A lane holds chunks of 8 adjacent elements, chunk i of row thread t being
+// number i * 64 * WAVES + t: index bits 0-2 are registers, bits 3-6 lanes of one
+// 16-lane row, so the butterflies of a block of up to 128 never leave a DPP row.
+//
+// The maximum is taken over the bits of |S| as integers, which puts infinities
+// and NaN above every number: such a token gets the scale NaN and codes 0.
+template <int WAVES, int CH, typename T>
+__global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quant_kernel(const TokenArgs a, int vec) {
+    constexpr int RT = 64 * WAVES;   // threads of a row
+    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int block = blockIdx.y * gridDim.x + blockIdx.x;
+    const int row = WAVES == 1 ? block * (kThreads / 64) + (threadIdx.x >> 6) : block;
+    if (row >= a.rows) return;   // whole waves; all of a block where a row has several
+    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+    const int chunks = a.k_stride >> 3;
+
+    float v[CH * 8];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int e = (i * RT + t) * 8;
+        if (vec && e + 8 <= a.cin) {
+            load8(x + e, &v[8 * i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < a.cin ? to_float(x[e + j]) : 0.0f;
+        }
+    }
+    float sigma = 1.0f;
+    const int lb = a.log_b;
+    if (lb >= 1) reg_stage<1>(v);
+    if (lb >= 2) reg_stage<2>(v);
+    if (lb >= 3) reg_stage<4>(v);
+    if (lb >= 4) {
+        const float c = (t & 1) ? -1.0f : 1.0f;
+        cross_stage<1>(v, c);
+        sigma *= c;
+    }
+    if (lb >= 5) {
+        const float c = (t & 2) ? -1.0f : 1.0f;
+        cross_stage<2>(v, c);
+        sigma *= c;
+    }
+    if (lb >= 6) {
+        const float c = (t & 4) ? -1.0f : 1.0f;
+        cross_stage<4>(v, c);
+        sigma *= c;
+    }
+    if (lb >= 7) {
+        const float c = (t & 8) ? -1.0f : 1.0f;
+        cross_stage<8>(v, c);
+        sigma *= c;
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int r = 0; r < CH * 8; ++r) m = max(m, __float_as_uint(v[r]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    if constexpr (WAVES > 1) {
+        __shared__ uint32_t red[WAVES];
+        if ((t & 63) == 0) red[t >> 6] = m;
+        __syncthreads();
+        m = red[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = max(m, red[w]);
+    }
+    const bool finite = m < 0x7f800000u;
+    float s = __uint_as_float(m) / 127.0f;
+    if (s == 0.0f) s = 1.0f;
+    if (!finite) s = __uint_as_float(0x7fc00000u);
+    if (t == 0) a.sx[row] = s;
+
+    // rne(fl32(S / s)) without a division but near a half-integer (HATQ_NEAR_TIE)
+    const float r = sigma * (1.0f / s);
+    const bool plain = s >= 0x1p-125f && s <= 0x1p125f;
+    int8_t *q = a.xq + (int64_t)row * a.k_stride;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = i * RT + t;
+        uint32_t u[8];
+        bool near = !plain;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float p = v[8 * i + j] * r, k = p + HATQ_MAGIC;
+            near |= fabsf(p - (k - HATQ_MAGIC)) > HATQ_NEAR_TIE;
+            u[j] = __float_as_uint(k);   // |p| <= 127 (1 + 2^-22): within the code range after rounding
+        }
+        if (near) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = clamp127(rintf((sigma * v[8 * i + j]) / s));
+                u[j] = (uint32_t)(int32_t)d;
+            }
+        }
+        if (!finite) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] = 0;
+        }
+        if (c < chunks)
+            *reinterpret_cast<uint2 *>(q + c * 8) =
+                make_uint2(pack_low_bytes(u[0], u[1], u[2], u[3]), pack_low_bytes(u[4], u[5], u[6], u[7]));
+    }
+}
+
+template <int WAVES, int CH>
+hipError_t token_launch(const TokenArgs &a, hipStream_t st) {
+    const dim3 grid = grid_of(WAVES == 1 ? (a.rows + 3) / 4 : a.rows);
+    const int threads = WAVES == 1 ? kThreads : 64 * WAVES;
+    const int size = a.x_type == kF32 ? 4 : 2;
+    const int vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride * size % 16 == 0;
+    if (a.x_type == kF32) token_quant_kernel<WAVES, CH, float><<<grid, threads, 0, st>>>(a, vec);
+    else if (a.x_type == kBf16) token_quant_kernel<WAVES, CH, bf16_t><<<grid, threads, 0, st>>>(a, vec);
+    else token_quant_kernel<WAVES, CH, _Float16><<<grid, threads, 0, st>>>(a, vec);
+    return hipGetLastError();
+}
+
+// ---- weights --------------------------------------------------------------------
+// Held channel of packed column p, or -1 in the padding.  A gated layer's columns
+// go 32 gates, 32 values in turn, so one wave's accumulators hold both.
+__device__ __forceinline__ int held_channel(const LinearPrepArgs &a, int p) {
+    if (!a.gated) return p < a.cout ? p : -1;
+    const int c = (p >> 6) * 32 + (p & 31);
+    return c >= a.cout ? -1 : (p & 32) ? a.cout + c : c;
+}
+
+template <typename T>
+__device__ double transformed(const T *w, int d, int b) {
+    const int first = d & ~(b - 1), i = d & (b - 1);
+    double acc = 0.0;
+    for (int j = 0; j < b; ++j) {
+        const double e = (double)to_float(w[first + j]);
+        acc += (__popc(i & j) & 1) ? -e : e;
+    }
+    return acc;
+}
+
+// One block per packed column of an expert.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) linear_prepare_kernel(const LinearPrepArgs a) {
+    const int p = blockIdx.x, e = blockIdx.y;
+    const int held = a.gated ? 2 * a.cout : a.cout;
+    const int ch = held_channel(a, p);
+    const int64_t row = (int64_t)e * held + ch;
+    const T *w = ch >= 0 && !a.codes ? static_cast<const T *>(a.w) + row * a.cin : nullptr;
+    float s = 0.0f;
+    if (ch >= 0) {
+        if (a.codes) {
+            s = a.scale_in[row];
+        } else {
+            float m = 0.0f;
+            for (int d = threadIdx.x; d < a.cin; d += kThreads)
+                m = fmaxf(m, fabsf((float)transformed(w, d, a.hblock)));
+            m = wave_max(m);
+            __shared__ float red[kThreads / 64];
+            if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+            __syncthreads();
+            s = act_scale_from_absmax(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+        }
+    }
+    int8_t *out = a.wpack + ((int64_t)e * a.cout_pad + (p & ~15)) * a.k_stride + (p & 15) * 16;
+    for (int d = threadIdx.x; d < a.k_stride; d += kThreads) {
+        int8_t q = 0;
+        if (ch >= 0 && d < a.cin)
+            q = a.codes ? a.codes[row * a.cin + d]
+                        : (int8_t)(int)rintf(clamp127((float)transformed(w, d, a.hblock) / s));
+        out[(int64_t)(d >> 6) * 1024 + ((d >> 4) & 3) * 256 + (d & 15)] = q;
+    }
+    if (threadIdx.x == 0) {
+        a.w_scale[(int64_t)e * a.cout_pad + p] = s;
+        a.bias[(int64_t)e * a.cout_pad + p] = ch >= 0 && a.bias_in ? a.bias_in[row] : 0.0f;
+    }
+}
+
+// ---- the order of expert rows -----------------------------------------------------
+// A stable counting sort of `pairs` ids.  Block b owns a contiguous segment, wave w
+// of it a contiguous part: counts per wave in LDS, a block's first row of expert e =
+// rows of the experts before + rows of e in the blocks before, then each wave ranks
+// its pairs 64 at a time in order.  Ranks come from ballots, not from atomics, so
+// equal ids keep their order.
+constexpr int kOrderWaves = 4;
+constexpr int kOrderBlocks = 256;
+constexpr int kOrderSegment = 1024;   // pairs of a block, more when that would take over kOrderBlocks
+
+__host__ __device__ __forceinline__ int64_t order_segment(int64_t pairs) {
+    const int64_t per = (pairs + kOrderBlocks - 1) / kOrderBlocks;
+    const int64_t seg = per > kOrderSegment ? per : kOrderSegment;
+    return (seg + 255) / 256 * 256;
+}
+
+struct WaveSpan {
+    int64_t begin, end;
+};
+__device__ __forceinline__ WaveSpan order_span(int64_t pairs, int block, int wave) {
+    const int64_t seg = order_segment(pairs), part = seg / kOrderWaves;
+    const int64_t b = block * seg + wave * part;
+    const int64_t e = b + part;
+    return {b < pairs ? b : pairs, e < pairs ? e : pairs};
+}
+
+// counts[w][e] of this block's waves.
+__device__ void order_counts(const OrderArgs &a, int64_t pairs, int *counts) {
+    for (int i = threadIdx.x; i < kOrderWaves * a.experts; i += kThreads) counts[i] = 0;
+    __syncthreads();
+    const int w = threadIdx.x >> 6;
+    const WaveSpan s = order_span(pairs, blockIdx.x, w);
+    for (int64_t i = s.begin + (threadIdx.x & 63); i < s.end; i += 64) {
+        const int id = a.ids[i];
+        if ((unsigned)id < (unsigned)a.experts) atomicAdd(&counts[w * a.experts + id], 1);
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kThreads) order_count_kernel(const OrderArgs a) {
+    extern __shared__ int lds[];
+    order_counts(a, (int64_t)a.tokens * a.topk, lds);
+    for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+        int n = 0;
+        for (int w = 0; w < kOrderWaves; ++w) n += lds[w * a.experts + e];
+        a.ws[(int64_t)blockIdx.x * a.experts + e] = n;
+    }
+}
+
+// Several blocks read the table of order_count_kernel; one block (ws unused) has
+// every pair itself.
+__global__ void __launch_bounds__(kThreads) order_place_kernel(const OrderArgs a) {
+    extern __shared__ int lds[];   // counts [waves][experts], then ends [experts]
+    const int64_t pairs = (int64_t)a.tokens * a.topk;
+    int *counts = lds, *ends = lds + kOrderWaves * a.experts;
+    order_counts(a, pairs, counts);
+    // rows of each expert in all blocks, and in those before this one
+    constexpr int PER = kMaxExperts / kThreads;
+    int total[PER], before[PER];
+    for (int k = 0; k < PER; ++k) {
+        const int e = threadIdx.x * PER + k;
+        total[k] = before[k] = 0;
+        if (e >= a.experts) continue;
+        if (gridDim.x == 1) {
+            for (int w = 0; w < kOrderWaves; ++w) total[k] += counts[w * a.experts + e];
+        } else {
+            for (int b = 0; b < (int)gridDim.x; ++b) {
+                const int n = a.ws[(int64_t)b * a.experts + e];
+                total[k] += n;
+                before[k] += b < (int)blockIdx.x ? n : 0;
+            }
+        }
+    }
+    // exclusive scan over the block's threads, each with PER experts in a row
+    int sum = 0;
+    for (int k = 0; k < PER; ++k) sum += total[k];
+    int scan = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(scan, o, 64);
+        if ((int)(threadIdx.x & 63) >= o) scan += u;
+    }
+    __shared__ int wave_sum[kOrderWaves];
+    if ((threadIdx.x & 63) == 63) wave_sum[threadIdx.x >> 6] = scan;
+    __syncthreads();
+    int first = scan - sum;
+    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) first += wave_sum[w];
+    int all = 0;
+    for (int w = 0; w < kOrderWaves; ++w) all += wave_sum[w];
+    for (int k = 0; k < PER; ++k) {
+        const int e = threadIdx.x * PER + k;
+        if (e >= a.experts) break;
+        // the waves' first rows of this expert
+        int at = first + before[k];
+        for (int w = 0; w < kOrderWaves; ++w) {
+            const int n = counts[w * a.experts + e];
+            counts[w * a.experts + e] = at;
+            at += n;
+        }
+        first += total[k];
+        ends[e] = first;
+        if (blockIdx.x == 0) a.ends[e] = first;
+    }
+    __syncthreads();
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    volatile int *next = counts + w * a.experts;   // read and written by turns within the wave
+    const WaveSpan s = order_span(pairs, blockIdx.x, w);
+    for (int64_t b = s.begin; b < s.end; b += 64) {
+        const int64_t i = b + lane;
+        const int id = i < s.end ? a.ids[i] : -1;
+        const bool in = (unsigned)id < (unsigned)a.experts;
+        uint64_t same = __ballot(in);
+#pragma unroll
+        for (int bit = 0; bit < 10; ++bit) {
+            const uint64_t set = __ballot((id >> bit) & 1);
+            same &= (id >> bit) & 1 ? set : ~set;
+        }
+        const int rank = __popcll(same & ((1ull << lane) - 1));
+        int row = -1;
+        if (in) row = next[id] + rank;
+        __builtin_amdgcn_wave_barrier();   // every lane has read before the last of each id writes
+        if (in && rank + 1 == __popcll(same)) next[id] = row + 1;
+        __builtin_amdgcn_wave_barrier();
+        if (in) a.src[row] = (int)(i / a.topk);
+        if (i < s.end) a.pos[i] = row;
+    }
+    for (int64_t i = all + (int64_t)blockIdx.x * kThreads + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * kThreads)
+        a.src[i] = -1;
+}
+
+// ---- the weighted sum of expert rows ------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a, int vec) {
+    const int groups = (a.cols + 3) / 4;
+    const int64_t n = (int64_t)a.tokens * groups;
+    for (int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x; u < n; u += (int64_t)gridDim.x * kThreads) {
+        const int tok = (int)(u / groups), c = (int)(u - (int64_t)tok * groups) * 4;
+        const int32_t *pos = a.pos + (int64_t)tok * a.topk;
+        const float *wt = a.weights + (int64_t)tok * a.topk;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j = 0; j < a.topk; ++j) {
+            const int p = pos[j];
+            if ((unsigned)p >= (unsigned)a.h_rows) continue;
+            const float g = wt[j];
+            const float *h = a.h + p * a.h_stride + c;
+            if (vec) {
+                const float4 f = *reinterpret_cast<const float4 *>(h);
+                s[0] = __builtin_fmaf(g, f.x, s[0]);
+                s[1] = __builtin_fmaf(g, f.y, s[1]);
+                s[2] = __builtin_fmaf(g, f.z, s[2]);
+                s[3] = __builtin_fmaf(g, f.w, s[3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < a.cols) s[k] = __builtin_fmaf(g, h[k], s[k]);
+            }
+        }
+        T *y = static_cast<T *>(a.y) + tok * a.y_stride + c;
+        if (vec) {
+            store4(y, s);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < a.cols) y[k] = from_float<T>(s[k]);
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_token_quant(const TokenArgs &a, hipStream_t st) {
+    const int chunks = a.k_stride >> 3;
+    // A wave a row where the rows fill the card; else a row over more waves, so that
+    // a few tokens' loads are in flight at once.
+    if (chunks <= 64) return token_launch<1, 1>(a, st);
+    const bool many = a.rows >= 1024;
+    if (many || chunks <= 128) {
+        if (chunks <= 128) return token_launch<1, 2>(a, st);
+        if (chunks <= 256) return token_launch<1, 4>(a, st);
+        if (chunks <= 512) return token_launch<1, 8>(a, st);
+    }
+    if (many || chunks <= 1024) {
+        if (chunks <= 256) return token_launch<4, 1>(a, st);
+        if (chunks <= 512) return token_launch<4, 2>(a, st);
+        if (chunks <= 1024) return token_launch<4, 4>(a, st);
+        if (chunks <= 2048) return token_launch<4, 8>(a, st);
+    }
+    if (chunks <= 2048) return token_launch<16, 2>(a, st);
+    if (chunks <= 4096) return token_launch<16, 4>(a, st);
+    return token_launch<16, 8>(a, st);
+}
+
+hipError_t launch_linear_prepare(const LinearPrepArgs &a, hipStream_t st) {
+    const dim3 grid(a.cout_pad, a.experts);
+    if (a.w_type == kBf16) linear_prepare_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a);
+    else if (a.w_type == kF16) linear_prepare_kernel<_Float16><<<grid, kThreads, 0, st>>>(a);
+    else linear_prepare_kernel<float><<<grid, kThreads, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_order(const OrderArgs &a, hipStream_t st) {
+    const int64_t pairs = (int64_t)a.tokens * a.topk, seg = order_segment(pairs);
+    const int blocks = pairs > seg ? (int)((pairs + seg - 1) / seg) : 1;
+    const size_t counts = sizeof(int) * kOrderWaves * a.experts;
+    if (blocks > 1) order_count_kernel<<<blocks, kThreads, counts, st>>>(a);
+    order_place_kernel<<<blocks, kThreads, counts + sizeof(int) * a.experts, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_combine(const CombineArgs &a, hipStream_t st) {
+    const int size = a.y_type == kF32 ? 4 : 2;
+    const int vec = a.cols % 4 == 0 && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_stride % 4 == 0 &&
+                    (reinterpret_cast<uintptr_t>(a.y) & (4 * size - 1)) == 0 && a.y_stride % 4 == 0;
+    const int64_t n = (int64_t)a.tokens * ((a.cols + 3) / 4);
+    const int64_t blocks = (n + kThreads - 1) / kThreads;
+    const int grid = (int)(blocks < 65536 ? blocks : 65536);
+    if (a.y_type == kF32) combine_kernel<float><<<grid, kThreads, 0, st>>>(a, vec);
+    else if (a.y_type == kBf16) combine_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a, vec);
+    else combine_kernel<_Float16><<<grid, kThreads, 0, st>>>(a, vec);
+    return hipGetLastError();
+}
+
+size_t expert_order_ws_ints(int64_t pairs, int32_t experts) {
+    const int64_t seg = order_segment(pairs);
+    return pairs > seg ? (size_t)((pairs + seg - 1) / seg) * experts : 0;
+}
+
+}  // namespace hatq

@@ -10,6 +10,7 @@ The function names mirror the C ABI in ``include/hatq.h``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -45,6 +46,13 @@ class Weights(ctypes.Structure):
                 ("wpack", ctypes.c_void_p), ("pack_stride", ctypes.c_int32)]
 
 
+class LinearWeights(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("cin", ctypes.c_int32), ("cout", ctypes.c_int32),
+                ("gated", ctypes.c_int32), ("hblock", ctypes.c_int32), ("k_stride", ctypes.c_int32),
+                ("cout_pad", ctypes.c_int32), ("wpack", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p)]
+
+
 EXPORTS = ["hatq_status_string", "hatq_conv_out_hw", "hatq_weights_bytes", "hatq_prepare_weights",
            "hatq_export_weights", "hatq_pack_weights", "hatq_fwht_quant_ws_bytes", "hatq_fwht_quant_act",
            "hatq_fwht_quant_act_noalloc", "hatq_fwht_quant_act_c64", "hatq_conv_int8",
@@ -52,7 +60,10 @@ EXPORTS = ["hatq_status_string", "hatq_conv_out_hw", "hatq_weights_bytes", "hatq
            "hatq_conv_int8_int_transition", "hatq_range_expansion", "hatq_select_form", "hatq_hadamard_order",
            "hatq_fwht_quant_affine_ws_bytes", "hatq_fwht_quant_act_affine", "hatq_tapsum_len",
            "hatq_weight_tapsums", "hatq_conv_int8_affine",
-           "hatq_layer_ws_bytes", "hatq_layer_forward"]
+           "hatq_layer_ws_bytes", "hatq_layer_forward",
+           "hatq_linear_weights_bytes", "hatq_prepare_linear", "hatq_pack_linear", "hatq_token_quant",
+           "hatq_linear_int8", "hatq_linear_ws_bytes", "hatq_linear_forward", "hatq_experts_int8",
+           "hatq_experts_forward", "hatq_expert_order_ws_bytes", "hatq_expert_order", "hatq_expert_combine"]
 
 _lib = None
 
@@ -124,6 +135,31 @@ def load(build_if_missing: bool = False):
     L.hatq_layer_forward.argtypes = [ctypes.POINTER(Weights), i32, P, i32, i32, i32, P, P, P, i32, P, P,
                                      sz, P]
     L.hatq_layer_forward.restype = i32
+    i64, W = ctypes.c_int64, ctypes.POINTER(LinearWeights)
+    L.hatq_linear_weights_bytes.argtypes = [i32] * 5
+    L.hatq_linear_weights_bytes.restype = sz
+    L.hatq_prepare_linear.argtypes = [i32] * 5 + [P, i32, P, P, sz, W, P]
+    L.hatq_prepare_linear.restype = i32
+    L.hatq_pack_linear.argtypes = [i32] * 5 + [P, P, P, P, sz, W, P]
+    L.hatq_pack_linear.restype = i32
+    L.hatq_token_quant.argtypes = [P, i32, i32, i32, i64, i32, P, P, P]
+    L.hatq_token_quant.restype = i32
+    L.hatq_linear_int8.argtypes = [W, P, P, i32, P, i32, i64, P]
+    L.hatq_linear_int8.restype = i32
+    L.hatq_linear_ws_bytes.argtypes = [W, i32]
+    L.hatq_linear_ws_bytes.restype = sz
+    L.hatq_linear_forward.argtypes = [W, P, i32, i32, i64, P, i32, i64, P, sz, P]
+    L.hatq_linear_forward.restype = i32
+    L.hatq_experts_int8.argtypes = [W, P, P, i32, P, P, i32, P, i32, i64, P]
+    L.hatq_experts_int8.restype = i32
+    L.hatq_experts_forward.argtypes = [W, P, i32, i32, i64, P, P, i32, P, i32, i64, P, sz, P]
+    L.hatq_experts_forward.restype = i32
+    L.hatq_expert_order_ws_bytes.argtypes = [i32] * 3
+    L.hatq_expert_order_ws_bytes.restype = sz
+    L.hatq_expert_order.argtypes = [P, i32, i32, i32, P, P, P, P, sz, P]
+    L.hatq_expert_order.restype = i32
+    L.hatq_expert_combine.argtypes = [P, i32, i32, i64, P, P, i32, i32, P, i32, i64, P]
+    L.hatq_expert_combine.restype = i32
     _lib = L
     return L
 
@@ -587,4 +623,277 @@ def hatq_layer_forward(layer: PreparedLayer, form, x: torch.Tensor, x_absmax: Op
                                      _ptr(x_absmax), _ptr(y), _ptr(act_scale), int(next_hblock),
                                      _ptr(next_absmax), _ptr(ws), ws.numel(), _stream(stream)),
            "hatq_layer_forward")
+    return y
+
+
+# ---- linear layers over tokens ------------------------------------------------
+
+# Every function here takes stream=, a torch.cuda.Stream: the call, what it allocates and
+# the copies it makes of its arguments are then that stream's, not the current one's.
+def _on_stream(f):
+    @functools.wraps(f)
+    def g(*args, stream=None, **named):
+        if stream is None:
+            return f(*args, **named)
+        with torch.cuda.stream(stream):
+            return f(*args, **named)
+    return g
+
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+@dataclass
+class PreparedLinear:
+    """Prepared linear weights: the device buffer and the C view into it."""
+    buf: torch.Tensor
+    w: LinearWeights
+    experts: int
+    cin: int
+    cout: int
+    k_stride: int
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.w)
+
+    @property
+    def held(self) -> int:
+        """Channels an expert holds: cout, or a gated layer's gates and values."""
+        return self.cout * (2 if self.w.gated else 1)
+
+
+def _dtype(t: torch.dtype, name: str) -> int:
+    d = DTYPES.get(t)
+    if d is None:
+        raise ValueError(f"{name}: float32, bfloat16 or float16 expected, got {t}")
+    return d
+
+
+def _rows(t: torch.Tensor, name: str, cols: Optional[int] = None):
+    """(rows, cols, stride, dtype code) of a 2-d device tensor whose rows are dense."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name}: 2-d tensor expected")
+    n, c = t.shape
+    if not t.is_cuda:
+        raise ValueError(f"{name}: device tensor expected")
+    if cols is not None and c != cols:
+        raise ValueError(f"{name}: {cols} columns expected, got {c}")
+    stride, inner = t.stride()
+    if inner != 1 and c > 1:
+        raise ValueError(f"{name}: adjacent elements expected within a row")
+    if n <= 1 or stride < c:
+        # (one row has no stride, and rows that overlap are for reading only)
+        if n > 1:
+            raise ValueError(f"{name}: rows that do not overlap expected")
+        stride = c
+    return n, c, stride, _dtype(t.dtype, name)
+
+
+def _held(w: torch.Tensor, gated: bool, name: str):
+    if w.dim() == 2:
+        w = w.unsqueeze(0)
+    if w.dim() != 3:
+        raise ValueError(f"{name}: [channels, cin] or [experts, channels, cin] expected, got {tuple(w.shape)}")
+    e, held, cin = w.shape
+    if gated and held % 2:
+        raise ValueError(f"{name}: a gated layer holds its gates and as many values, got {held} channels")
+    return w.contiguous(), e, held, cin
+
+
+def _linear(call: str, e: int, held: int, cin: int, gated: bool, hblock: int, device, run) -> PreparedLinear:
+    cout = held // 2 if gated else held
+    nbytes = int(load().hatq_linear_weights_bytes(e, cin, cout, int(gated), hblock))
+    buf = torch.empty(max(nbytes, 1), dtype=torch.int8, device=device)
+    out = LinearWeights()
+    _check(run((e, cin, cout, int(gated), hblock), buf.data_ptr(), nbytes, ctypes.byref(out)), call)
+    return PreparedLinear(buf, out, e, cin, cout, out.k_stride)
+
+
+@_on_stream
+def hatq_prepare_linear(w: torch.Tensor, bias: Optional[torch.Tensor] = None, hblock: int = 1, gated: bool = False) -> PreparedLinear:
+    """A layer from float weights [held, cin], or experts from [experts, held, cin]
+    (bias accordingly).  gated: held = 2 cout, gates first."""
+    w, e, held, cin = _held(w, gated, "w")
+    t = _dtype(w.dtype, "w")
+    _need(w, "w", w.dtype, 0)
+    b = None if bias is None else bias.contiguous().float()
+    _need(b, "bias", torch.float32, e * held, optional=True)
+    return _linear("hatq_prepare_linear", e, held, cin, gated, int(hblock), w.device,
+                   lambda shape, dst, n, out: load().hatq_prepare_linear(*shape, _ptr(w), t, _ptr(b), dst, n, out,
+                                                                         _stream()))
+
+
+@_on_stream
+def hatq_pack_linear(codes: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                     hblock: int = 1, gated: bool = False) -> PreparedLinear:
+    """The same from int8 codes of the transformed weights and their fp32 scales, one
+    for each channel (quantized elsewhere)."""
+    codes, e, held, cin = _held(codes, gated, "codes")
+    _need(codes, "codes", torch.int8, 0)
+    s = w_scale.contiguous()
+    b = None if bias is None else bias.contiguous()
+    _need(s, "w_scale", torch.float32, e * held)
+    _need(b, "bias", torch.float32, e * held, optional=True)
+    return _linear("hatq_pack_linear", e, held, cin, gated, int(hblock), codes.device,
+                   lambda shape, dst, n, out: load().hatq_pack_linear(*shape, _ptr(codes), _ptr(s), _ptr(b), dst, n,
+                                                                      out, _stream()))
+
+
+@_on_stream
+def hatq_token_quant(x: torch.Tensor, hblock: int = 1, xq: Optional[torch.Tensor] = None,
+                     scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Tokens x [rows, cin] -> (int8 codes [rows, cin rounded up to 64], a scale for
+    each token, fp32 [rows])."""
+    n, c, stride, t = _rows(x, "x")
+    ks = (c + 63) // 64 * 64
+    if xq is None:
+        xq = torch.empty((n, ks), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    _need(xq, "xq", torch.int8, n * ks)
+    _need(scale, "scale", torch.float32, n)
+    _check(load().hatq_token_quant(x.data_ptr(), t, n, c, stride, int(hblock), xq.data_ptr(), scale.data_ptr(),
+                                   _stream()), "hatq_token_quant")
+    return xq, scale
+
+
+def _out_rows(y: Optional[torch.Tensor], rows: int, cout: int, dtype: torch.dtype, device):
+    """(y, stride, dtype code) of the output rows, allocated if y is None."""
+    if y is None:
+        return torch.empty((rows, cout), dtype=dtype, device=device), cout, _dtype(dtype, "out_dtype")
+    n, _, stride, t = _rows(y, "y", cout)
+    if n != rows:
+        raise ValueError(f"y: {rows} rows expected, got {n}")
+    return y, stride, t
+
+
+def _codes(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor) -> int:
+    if xq.dim() != 2 or xq.shape[1] != lin.k_stride:
+        raise ValueError(f"xq: [rows, {lin.k_stride}] expected, got {tuple(xq.shape)}")
+    _need(xq, "xq", torch.int8, 0)
+    _need(scale, "scale", torch.float32, xq.shape[0])
+    return xq.shape[0]
+
+
+@_on_stream
+def hatq_linear_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor,
+                     out_dtype: torch.dtype = torch.float32, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Token codes through one layer: y [rows, cout] of out_dtype (or of the given y)."""
+    n = _codes(lin, xq, scale)
+    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype, xq.device)
+    _check(load().hatq_linear_int8(lin.ref, xq.data_ptr(), scale.data_ptr(), n, y.data_ptr(), yt, ys,
+                                   _stream()), "hatq_linear_int8")
+    return y
+
+
+def hatq_linear_ws_bytes(lin: PreparedLinear, rows: int) -> int:
+    return int(load().hatq_linear_ws_bytes(lin.ref, rows))
+
+
+def _linear_ws(lin: PreparedLinear, rows: int, ws: Optional[torch.Tensor], device) -> torch.Tensor:
+    if ws is None:
+        # hatq_linear_ws_bytes, without the call
+        return torch.empty(((rows * lin.k_stride + 255) & -256) + ((4 * rows + 255) & -256) or 256,
+                           dtype=torch.int8, device=device)
+    _need(ws, "ws", torch.int8, 0)
+    return ws
+
+
+@_on_stream
+def hatq_linear_forward(lin: PreparedLinear, x: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
+                        y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tokens x [rows, cin] through one layer: y [rows, cout] of out_dtype (default: x's)."""
+    n, _, xs, xt = _rows(x, "x", lin.cin)
+    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x.device)
+    ws = _linear_ws(lin, n, ws, x.device)
+    _check(load().hatq_linear_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, ws.data_ptr(),
+                                      ws.numel(), _stream()), "hatq_linear_forward")
+    return y
+
+
+def _grouping(lin: PreparedLinear, ends: torch.Tensor, src: Optional[torch.Tensor], x_rows: int) -> int:
+    """The output rows of a grouped call."""
+    _need(ends, "ends", torch.int32, lin.experts)
+    if src is None:
+        return x_rows
+    if src.dim() != 1:
+        raise ValueError(f"src: 1-d tensor expected, got shape {tuple(src.shape)}")
+    _need(src, "src", torch.int32, 0)
+    return src.shape[0]
+
+
+@_on_stream
+def hatq_experts_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor, ends: torch.Tensor,
+                      src: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                      y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Token codes grouped by expert: row i of y is token src[i] (or i) through the first
+    expert e with i < ends[e] (int32 [experts], on the device)."""
+    n = _codes(lin, xq, scale)
+    rows = _grouping(lin, ends, src, n)
+    y, ys, yt = _out_rows(y, rows, lin.cout, out_dtype, xq.device)
+    _check(load().hatq_experts_int8(lin.ref, xq.data_ptr(), scale.data_ptr(), n, ends.data_ptr(), _ptr(src), rows,
+                                    y.data_ptr(), yt, ys, _stream()), "hatq_experts_int8")
+    return y
+
+
+@_on_stream
+def hatq_experts_forward(lin: PreparedLinear, x: torch.Tensor, ends: torch.Tensor,
+                         src: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                         y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """hatq_experts_int8 of tokens x [x_rows, cin], each quantized once."""
+    n, _, xs, xt = _rows(x, "x", lin.cin)
+    rows = _grouping(lin, ends, src, n)
+    y, ys, yt = _out_rows(y, rows, lin.cout, out_dtype or x.dtype, x.device)
+    ws = _linear_ws(lin, n, ws, x.device)
+    _check(load().hatq_experts_forward(lin.ref, x.data_ptr(), xt, n, xs, ends.data_ptr(), _ptr(src), rows,
+                                       y.data_ptr(), yt, ys, ws.data_ptr(), ws.numel(), _stream()),
+           "hatq_experts_forward")
+    return y
+
+
+@_on_stream
+def hatq_expert_order(ids: torch.Tensor, experts: int, ends: Optional[torch.Tensor] = None,
+                      src: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None):
+    """Chosen experts ids (int32 [tokens, topk]) -> (ends [experts], src [tokens * topk],
+    pos [tokens, topk]): the rows of the grouped calls, sorted by expert.  An id outside
+    [0, experts) masks its pair (pos -1)."""
+    if ids.dim() != 2:
+        raise ValueError(f"ids: [tokens, topk] expected, got shape {tuple(ids.shape)}")
+    _need(ids, "ids", torch.int32, 0)
+    t, k = ids.shape
+    nbytes = int(load().hatq_expert_order_ws_bytes(t, k, experts))
+    if ends is None:
+        ends = torch.empty(experts, dtype=torch.int32, device=ids.device)
+    if src is None:
+        src = torch.empty(t * k, dtype=torch.int32, device=ids.device)
+    if pos is None:
+        pos = torch.empty((t, k), dtype=torch.int32, device=ids.device)
+    if ws is None:
+        ws = torch.empty(max(nbytes, 1), dtype=torch.int8, device=ids.device)
+    _need(ends, "ends", torch.int32, experts)
+    _need(src, "src", torch.int32, t * k)
+    _need(pos, "pos", torch.int32, t * k)
+    _need(ws, "ws", torch.int8, 0)
+    _check(load().hatq_expert_order(ids.data_ptr(), t, k, experts, ends.data_ptr(), src.data_ptr(), pos.data_ptr(),
+                                    ws.data_ptr(), ws.numel(), _stream()), "hatq_expert_order")
+    return ends, src, pos
+
+
+@_on_stream
+def hatq_expert_combine(h: torch.Tensor, pos: torch.Tensor, weights: torch.Tensor,
+                        out_dtype: torch.dtype = torch.float32, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y[t] = sum over j of weights[t, j] h[pos[t, j]]: h fp32 [rows, cols], pos int32 and
+    weights fp32 [tokens, topk]; a pos outside the rows adds nothing."""
+    n, c, hs, ht = _rows(h, "h")
+    if ht != 0:
+        raise ValueError(f"h: float32 expected, got {h.dtype}")
+    if pos.dim() != 2 or weights.shape != pos.shape:
+        raise ValueError(f"pos, weights: [tokens, topk] expected, got {tuple(pos.shape)}, {tuple(weights.shape)}")
+    _need(pos, "pos", torch.int32, 0)
+    _need(weights, "weights", torch.float32, 0)
+    t, k = pos.shape
+    y, ys, yt = _out_rows(y, t, c, out_dtype, h.device)
+    _check(load().hatq_expert_combine(h.data_ptr(), n, c, hs, pos.data_ptr(), weights.data_ptr(), t, k, y.data_ptr(),
+                                      yt, ys, _stream()), "hatq_expert_combine")
     return y
