@@ -229,26 +229,74 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) 
 }
 
 // ---- many rows --------------------------------------------------------------------------
+// Block index -> tile.  Blocks bid, bid + 8, ... run on one XCD; each XCD takes a
+// contiguous range of v, and v goes down 8 row tiles before the next column tile, so
+// the 32 tiles that an XCD's CUs hold at once read 8 row and 4 column operands.
+struct TileIndex {
+    int t, tn;
+};
+__device__ __forceinline__ TileIndex tile_index(int bid, int tiles_m, int tiles_n) {
+    const int nt = tiles_m * tiles_n, xcd = bid & 7, q = nt >> 3, rest = nt & 7;
+    const int v = xcd * q + min(xcd, rest) + (bid >> 3);
+    const int band = v / (8 * tiles_n), in = v - band * 8 * tiles_n;
+    const int high = min(8, tiles_m - band * 8);
+    const int tn = in / high;
+    return {band * 8 + in - tn * high, tn};
+}
+
+// Stores 32 rows of COLS outputs, fp32 in a wave's LDS rows of COLS + 4, to y: lanes take
+// 16-byte pieces, so a store instruction writes whole runs of rows.
+template <typename T, int COLS>
+__device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0, int rows, int c0, int lane) {
+    constexpr int E = 16 / sizeof(T), PER = COLS / E;   // elements of a piece, pieces of a row
+    T *y = static_cast<T *>(a.y);
+    const bool vec = (reinterpret_cast<uintptr_t>(y) & 15) == 0 && (a.y_stride & (E - 1)) == 0;
+    if (vec && c0 + COLS <= a.cout) {
+#pragma unroll
+        for (int u = 0; u < 32 * PER / 64; ++u) {
+            const int r = (u * 64 + lane) / PER, c = lane % PER * E;
+            float z[E];
+#pragma unroll
+            for (int k = 0; k < E; k += 4) *reinterpret_cast<float4 *>(z + k) = *reinterpret_cast<const float4 *>(from + r * (COLS + 4) + c + k);
+            if (r < rows) store16(y + (row0 + r) * a.y_stride + c0 + c, z);
+        }
+    } else {
+        for (int u = lane; u < 32 * COLS; u += 64) {
+            const int r = u / COLS, c = u % COLS;
+            if (r < rows && c0 + c < a.cout) y[(row0 + r) * a.y_stride + c0 + c] = from_float<T>(from[r * (COLS + 4) + c]);
+        }
+    }
+}
+
 // Tiles of BM rows x BN packed columns by WM x WN waves of FM x FN MFMAs of 32 x 32,
 // the contraction in steps of 64 bytes through a ring of STAGES LDS buffers that are
 // filled by direct-to-LDS loads.  A row's four 16-byte pieces of a step are permuted
 // by the row (piece c of row m at place c ^ (m >> 1 & 3)), so the reads of 32 rows'
 // fragments do not meet in a bank; the weights lie in memory as they are read.
+//
+// Each half step's fragments are read while the half before runs on the matrix
+// cores, and the one barrier of a step stands between its halves: the reads of a
+// buffer end before it, the loads that refill that buffer and the reads of the next
+// one begin after it.
 template <int WM, int WN, int FM, int FN, int STAGES, int G>
 __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearArgs a) {
     constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
     constexpr int A_INSTR = BM / 16 / NW, B_INSTR = BN / 16 / NW, PER_STAGE = A_INSTR + B_INSTR;
     constexpr int STAGE_BYTES = (BM + BN) * 64;
+    constexpr int COLS = FN / G * 32;   // outputs of a wave's row
     static_assert(A_INSTR * NW * 16 == BM && B_INSTR * NW * 16 == BN && FN % G == 0, "tile");
+    static_assert(NW * 32 * (COLS + 4) * 4 <= STAGES * STAGE_BYTES, "output staging");
     __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
     const int tiles_n = (a.cout_pad + BN - 1) / BN;
     const int bid = blockIdx.y * gridDim.x + blockIdx.x;
-    const int t = bid / tiles_n, tn = bid - t * tiles_n;
+    if (bid >= a.tiles_m * tiles_n) return;
+    const TileIndex ti = tile_index(bid, a.tiles_m, tiles_n);
+    const int tn = ti.tn;
     RowTile r;
-    if (!row_tile<BM>(a, t, r)) return;
+    if (!row_tile<BM>(a, ti.t, r)) return;
     const int rows = min(r.end - r.row0, BM);
     if (r.expert < 0) return zero_tile(a, r.row0, rows, tn * BN / G, BN / G);
 
@@ -265,29 +313,33 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
         const int block = min(tn * (BN / 16) + wave + NW * j, a.cout_pad / 16 - 1);
         pb[j] = a.wp + ((int64_t)r.expert * a.cout_pad + block * 16) * a.k_stride + lane * 16;
     }
-    auto issue = [&](int ks) {
-        int8_t *to = lds + (ks % STAGES) * STAGE_BYTES;
+    // Loads the step that the pointers are at into a buffer; `more`: go on to the next.
+    // (Past the last step the last one is loaded again, so that every step has the same
+    // loads and waits; nothing reads those copies.)
+    auto issue = [&](int8_t *to, bool more) {
 #pragma unroll
-        for (int j = 0; j < A_INSTR; ++j)
-            __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(pa[j] + ks * 64), HATQ_LDS(to + 1024 * (wave + NW * j)), 16, 0, 0);
-#pragma unroll
-        for (int j = 0; j < B_INSTR; ++j)
-            __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(pb[j] + (int64_t)ks * 1024),
-                                             HATQ_LDS(to + BM * 64 + 1024 * (wave + NW * j)), 16, 0, 0);
-    };
-    int fa[FM][2], fb[FN][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int c = 2 * h + (lane >> 5);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const int m = (wm * FM + i) * 32 + (lane & 31);
-            fa[i][h] = m * 64 + 16 * (c ^ ((m >> 1) & 3));
+        for (int j = 0; j < A_INSTR; ++j) {
+            __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(pa[j]), HATQ_LDS(to + 1024 * (wave + NW * j)), 16, 0, 0);
+            pa[j] += more ? 64 : 0;
         }
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-            fb[j][h] = BM * 64 + ((wn * FN + j) * 2 + ((lane >> 4) & 1)) * 1024 + c * 256 + (lane & 15) * 16;
+        for (int j = 0; j < B_INSTR; ++j) {
+            __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(pb[j]), HATQ_LDS(to + BM * 64 + 1024 * (wave + NW * j)), 16, 0, 0);
+            pb[j] += more ? 1024 : 0;
+        }
+    };
+    int fa[2], fb[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int c = 2 * h + (lane >> 5), m = wm * FM * 32 + (lane & 31);
+        fa[h] = m * 64 + 16 * (c ^ ((m >> 1) & 3));
+        fb[h] = BM * 64 + (wn * FN * 2 + ((lane >> 4) & 1)) * 1024 + c * 256 + (lane & 15) * 16;
     }
+    v4i xa[2][FM], wb[2][FN];
+    auto read = [&](const int8_t *from, int h, int k) {
+        if (k < FN) wb[h][k] = *reinterpret_cast<const v4i *>(from + fb[h] + k * 2048);
+        else if (k < FN + FM) xa[h][k - FN] = *reinterpret_cast<const v4i *>(from + fa[h] + (k - FN) * 2048);
+    };
     v16i acc[FN][FM];
 #pragma unroll
     for (int j = 0; j < FN; ++j)
@@ -295,47 +347,58 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[j][i][e] = 0;
-
+    // The MFMAs of half h, with the reads of the other half's fragments two by two between
+    // the first of them (left to itself the compiler moves the reads down to their use).
+    auto half = [&](int h, const int8_t *next) {
 #pragma unroll
-    for (int k = 0; k < STAGES - 1; ++k)
-        if (k < nks) issue(k);
-    for (int ks = 0; ks < nks; ++ks) {
-        // this step's loads have landed (those of up to STAGES - 2 later steps may be under way)
-        if (ks + STAGES - 2 < nks) wait_vmcnt_lds<(STAGES - 2) * PER_STAGE>();
-        else wait_vmcnt_lds<0>();
-        __builtin_amdgcn_s_barrier();   // for every wave; and every wave has left the buffer filled next
-        if (ks + STAGES - 1 < nks) issue(ks + STAGES - 1);
-        const int8_t *from = lds + (ks % STAGES) * STAGE_BYTES;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            v4i xa[FM], wb[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) xa[i] = *reinterpret_cast<const v4i *>(from + fa[i][h]);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) wb[j] = *reinterpret_cast<const v4i *>(from + fb[j][h]);
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-                    acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wb[j], xa[i], acc[j][i], 0, 0, 0);
+        for (int k = 0; k < FM * FN; ++k) {
+            const int j = k / FM, i = k % FM;
+            acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wb[h][j], xa[h][i], acc[j][i], 0, 0, 0);
+            if (2 * k < FM + FN) {
+                read(next, 1 - h, 2 * k);
+                read(next, 1 - h, 2 * k + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-    }
+    };
 
-    const bool vec = vector_rows(a);
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k) issue(lds + k * STAGE_BYTES, k + 1 < nks);
+    wait_vmcnt_lds<(STAGES - 1) * PER_STAGE>();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int k = 0; k < FM + FN; ++k) read(lds, 0, k);
+    int at = 0;   // this step's buffer
+    for (int ks = 0; ks < nks; ++ks) {
+        int8_t *now = lds + at;
+        at = at + STAGE_BYTES == STAGES * STAGE_BYTES ? 0 : at + STAGE_BYTES;
+        half(0, now);
+        // the next step's loads have landed (STAGES - 2 later ones under way), this buffer
+        // has been read: by every wave, past the barrier
+        wait_vmcnt_lds<(STAGES - 2) * PER_STAGE>();
+        __builtin_amdgcn_s_barrier();
+        issue(now, ks + STAGES + 1 < nks);
+        half(1, lds + at);
+    }
+    wait_vmcnt_lds<0>();
+    __builtin_amdgcn_s_barrier();   // no load is under way into the buffers that stage the outputs
+
     const float *w_scale = a.w_scale + (int64_t)r.expert * a.cout_pad, *bias = a.bias + (int64_t)r.expert * a.cout_pad;
+    float *mine = reinterpret_cast<float *>(lds) + wave * 32 * (COLS + 4);
+    const int c0 = (tn * BN + wn * FN * 32) / G;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-        const int row = (wm * FM + i) * 32 + (lane & 31);
-        if (row >= rows) continue;
-        const int tok = token_of(a, r.row0 + row);
+        const int first = (wm * FM + i) * 32;
+        if (first >= rows) break;
+        const int tok = token_of(a, r.row0 + min(first + (lane & 31), rows - 1));
         const float s = tok < 0 ? 0.0f : a.sx[tok];
 #pragma unroll
         for (int j = 0; j < FN; j += G)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 // packed column of element 0: rows 8 q + 4 (lane / 32) of the 32 x 32 tile
-                const int in = 8 * q + 4 * (lane >> 5), p = tn * BN + (wn * FN + j) * 32 + in;
-                if (p >= a.cout_pad) continue;
+                const int in = 8 * q + 4 * (lane >> 5);
+                const int p = min(tn * BN + (wn * FN + j) * 32, a.cout_pad - 32 * G) + in;
                 float z[2][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
@@ -347,9 +410,14 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
 #pragma unroll
                     for (int e = 0; e < 4; ++e) z[0][e] = gated_unit(z[0][e], z[1][e]);
                 }
-                const int c = G == 1 ? p : (tn * BN + (wn * FN + j) * 32) / 2 + in;
-                if (c < a.cout) put4(a, r.row0 + row, c, z[0], vec);
+                *reinterpret_cast<float4 *>(mine + (lane & 31) * (COLS + 4) + j / G * 32 + in) =
+                    make_float4(z[0][0], z[0][1], z[0][2], z[0][3]);
             }
+        // (a wave's LDS accesses are in order: its rows are whole when it reads them)
+        const int n = min(rows - first, 32);
+        if (a.y_type == kBf16) store_rows<bf16_t, COLS>(a, mine, r.row0 + first, n, c0, lane);
+        else if (a.y_type == kF16) store_rows<_Float16, COLS>(a, mine, r.row0 + first, n, c0, lane);
+        else store_rows<float, COLS>(a, mine, r.row0 + first, n, c0, lane);
     }
 }
 
@@ -361,9 +429,11 @@ void stream(const LinearArgs &a, hipStream_t st) {
 }
 
 template <int WM, int WN, int FM, int FN, int STAGES>
-void tile(const LinearArgs &a, hipStream_t st) {
+void tile(const LinearArgs &b, hipStream_t st) {
     constexpr int BM = WM * FM * 32, BN = WN * FN * 32;
-    const dim3 grid = grid_of(row_tiles(a, BM) * ((a.cout_pad + BN - 1) / BN));
+    LinearArgs a = b;
+    a.tiles_m = (int32_t)row_tiles(a, BM);
+    const dim3 grid = grid_of((int64_t)a.tiles_m * ((a.cout_pad + BN - 1) / BN));
     if (a.gated) linear_tile_kernel<WM, WN, FM, FN, STAGES, 2><<<grid, 64 * WM * WN, 0, st>>>(a);
     else linear_tile_kernel<WM, WN, FM, FN, STAGES, 1><<<grid, 64 * WM * WN, 0, st>>>(a);
 }

@@ -66,4 +66,18 @@ __device__ __forceinline__ void store4(_Float16 *p, const float *v) {
     *reinterpret_cast<v4h *>(p) = v4h{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
 }
 
+// One 16-byte piece.
+__device__ __forceinline__ void store16(float *p, const float *v) { store4(p, v); }
+__device__ __forceinline__ void store16(bf16_t *p, const float *v) {
+    *reinterpret_cast<uint4 *>(p) =
+        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+}
+__device__ __forceinline__ void store16(_Float16 *p, const float *v) {
+    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+    v8h h;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = (_Float16)v[j];
+    *reinterpret_cast<v8h *>(p) = h;
+}
+
 }  // namespace hatq
