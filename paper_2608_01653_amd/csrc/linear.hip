@@ -101,10 +101,10 @@ __device__ __forceinline__ float gated_unit(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
 }
 
-// z of four adjacent packed columns, at column p of the expert's factors.
-__device__ __forceinline__ void dequant4(const LinearArgs &a, const float *w_scale, const float *bias, int p,
-                                         const int *acc, float s, float *z) {
-    const float4 w = *reinterpret_cast<const float4 *>(w_scale + p), b = *reinterpret_cast<const float4 *>(bias + p);
+// z of four adjacent packed columns with factors at w_scale and bias (memory or LDS).
+__device__ __forceinline__ void dequant4(const LinearArgs &a, const float *w_scale, const float *bias, const int *acc,
+                                         float s, float *z) {
+    const float4 w = *reinterpret_cast<const float4 *>(w_scale), b = *reinterpret_cast<const float4 *>(bias);
     z[0] = __builtin_fmaf((float)acc[0], s * w.x * a.inv_b, b.x);
     z[1] = __builtin_fmaf((float)acc[1], s * w.y * a.inv_b, b.y);
     z[2] = __builtin_fmaf((float)acc[2], s * w.z * a.inv_b, b.z);
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) 
 #pragma unroll
             for (int k = 1; k < WAVES; ++k) sum += part[k][m][g][lane];
             const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
-            dequant4(a, w_scale, bias, p + 32 * g, q, s[m], z[g]);
+            dequant4(a, w_scale + p + 32 * g, bias + p + 32 * g, q, s[m], z[g]);
         }
         if (G == 2) {
 #pragma unroll
@@ -271,8 +271,8 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
 // Tiles of BM rows x BN packed columns by WM x WN waves of FM x FN MFMAs of 32 x 32,
 // the contraction in steps of 64 bytes through a ring of STAGES LDS buffers that are
 // filled by direct-to-LDS loads.  A row's four 16-byte pieces of a step are permuted
-// by the row (piece c of row m at place c ^ (m >> 1 & 3)), so the reads of 32 rows'
-// fragments do not meet in a bank; the weights lie in memory as they are read.
+// by the row (piece c of row m at place c ^ (m >> 2 & 3)), so 16 rows' pieces, what the
+// 64 banks deliver at once, do not meet in a bank; the weights lie in memory as they are read.
 //
 // Each half step's fragments are read while the half before runs on the matrix
 // cores, and the one barrier of a step stands between its halves: the reads of a
@@ -286,7 +286,11 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
     constexpr int COLS = FN / G * 32;   // outputs of a wave's row
     static_assert(A_INSTR * NW * 16 == BM && B_INSTR * NW * 16 == BN && FN % G == 0, "tile");
     static_assert(NW * 32 * (COLS + 4) * 4 <= STAGES * STAGE_BYTES, "output staging");
-    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE_BYTES];
+    static_assert(BN / 4 <= 64 * NW, "column factors");
+    // the ring, then the columns' scales and biases, [2][BN] floats.  (One array: with a
+    // second LDS object the compiler waits for every load under way before each read.)
+    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE_BYTES + 8 * BN];
+    float4 *factor = reinterpret_cast<float4 *>(lds + STAGES * STAGE_BYTES);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
@@ -300,13 +304,24 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
     const int rows = min(r.end - r.row0, BM);
     if (r.expert < 0) return zero_tile(a, r.row0, rows, tn * BN / G, BN / G);
 
+    if (threadIdx.x < BN / 4) {
+        const int64_t p = (int64_t)r.expert * a.cout_pad + min(tn * BN + (int)threadIdx.x * 4, a.cout_pad - 4);
+        factor[threadIdx.x] = *reinterpret_cast<const float4 *>(a.w_scale + p);
+        factor[BN / 4 + threadIdx.x] = *reinterpret_cast<const float4 *>(a.bias + p);
+    }
+    float scale[FM];   // of this lane's tokens
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        const int tok = token_of(a, r.row0 + min((wm * FM + i) * 32 + (lane & 31), rows - 1));
+        scale[i] = tok < 0 ? 0.0f : a.sx[tok];
+    }
     const int nks = a.k_stride >> 6;
     const int8_t *pa[A_INSTR], *pb[B_INSTR];
 #pragma unroll
     for (int j = 0; j < A_INSTR; ++j) {
         const int m = 16 * (wave + NW * j) + (lane >> 2);
         const int tok = token_of(a, r.row0 + min(m, rows - 1));
-        pa[j] = a.xq + (int64_t)max(tok, 0) * a.k_stride + 16 * ((lane & 3) ^ ((m >> 1) & 3));
+        pa[j] = a.xq + (int64_t)max(tok, 0) * a.k_stride + 16 * ((lane & 3) ^ ((m >> 2) & 3));
     }
 #pragma unroll
     for (int j = 0; j < B_INSTR; ++j) {
@@ -332,7 +347,7 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int c = 2 * h + (lane >> 5), m = wm * FM * 32 + (lane & 31);
-        fa[h] = m * 64 + 16 * (c ^ ((m >> 1) & 3));
+        fa[h] = m * 64 + 16 * (c ^ ((m >> 2) & 3));
         fb[h] = BM * 64 + (wn * FN * 2 + ((lane >> 4) & 1)) * 1024 + c * 256 + (lane & 15) * 16;
     }
     v4i xa[2][FM], wb[2][FN];
@@ -383,28 +398,26 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
     wait_vmcnt_lds<0>();
     __builtin_amdgcn_s_barrier();   // no load is under way into the buffers that stage the outputs
 
-    const float *w_scale = a.w_scale + (int64_t)r.expert * a.cout_pad, *bias = a.bias + (int64_t)r.expert * a.cout_pad;
     float *mine = reinterpret_cast<float *>(lds) + wave * 32 * (COLS + 4);
     const int c0 = (tn * BN + wn * FN * 32) / G;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int first = (wm * FM + i) * 32;
         if (first >= rows) break;
-        const int tok = token_of(a, r.row0 + min(first + (lane & 31), rows - 1));
-        const float s = tok < 0 ? 0.0f : a.sx[tok];
 #pragma unroll
         for (int j = 0; j < FN; j += G)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                // packed column of element 0: rows 8 q + 4 (lane / 32) of the 32 x 32 tile
+                // element 0's column: rows 8 q + 4 (lane / 32) of the 32 x 32 tile
                 const int in = 8 * q + 4 * (lane >> 5);
-                const int p = min(tn * BN + (wn * FN + j) * 32, a.cout_pad - 32 * G) + in;
+                const float4 *f = factor + ((wn * FN + j) * 32 + in) / 4;
                 float z[2][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const int v[4] = {acc[j + g][i][4 * q], acc[j + g][i][4 * q + 1], acc[j + g][i][4 * q + 2],
                                       acc[j + g][i][4 * q + 3]};
-                    dequant4(a, w_scale, bias, p + 32 * g, v, s, z[g]);
+                    dequant4(a, reinterpret_cast<const float *>(f + 8 * g), reinterpret_cast<const float *>(f + BN / 4 + 8 * g), v,
+                             scale[i], z[g]);
                 }
                 if (G == 2) {
 #pragma unroll
