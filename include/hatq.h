@@ -520,7 +520,8 @@ int32_t hatq_linear_int8(const hatq_linear_weights *W, const int8_t *xq, const f
                          void *y, int32_t y_type, int64_t y_stride, void *stream);
 
 /* The whole layer, floats in: hatq_token_quant into the workspace, then
- * hatq_linear_int8.  ws: device memory, 256-byte aligned, of at least
+ * hatq_linear_int8 (for a few tokens one kernel that does both, with the same
+ * result).  ws: device memory, 256-byte aligned, of at least
  * hatq_linear_ws_bytes(W, rows) bytes. */
 size_t hatq_linear_ws_bytes(const hatq_linear_weights *W, int32_t rows);
 int32_t hatq_linear_forward(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t rows,
@@ -570,6 +571,21 @@ int32_t hatq_expert_order(const int32_t *ids, int32_t tokens, int32_t topk, int3
 int32_t hatq_expert_combine(const float *h, int32_t h_rows, int32_t cols, int64_t h_stride, const int32_t *pos,
                             const float *weights, int32_t tokens, int32_t topk, void *y, int32_t y_type,
                             int64_t y_stride, void *stream);
+
+/* A feed-forward block of gated experts, the calls above in one: hatq_expert_order
+ * of ids; hatq_experts_forward of x through the gated W_in into fp32 hidden rows;
+ * of those through W_out into fp32 rows; hatq_expert_combine with the weights.
+ *   W_in, W_out: as many experts, W_in gated, W_out plain, W_in->cout == W_out->cin.
+ *   x: device [tokens][W_in->cin] of x_type; ids int32, weights fp32, device
+ *   [tokens][topk]; y: device [tokens][W_out->cout] of y_type.
+ *   ws: device memory, 256-byte aligned, of at least hatq_expert_mlp_ws_bytes bytes
+ *       (0 for weights that do not fit together, or sizes that are not supported). */
+size_t hatq_expert_mlp_ws_bytes(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out, int32_t tokens,
+                                int32_t topk);
+int32_t hatq_expert_mlp(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out, const void *x,
+                        int32_t x_type, int32_t tokens, int64_t x_stride, const int32_t *ids, const float *weights,
+                        int32_t topk, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,
+                        void *stream);
 
 #ifdef __cplusplus
 }

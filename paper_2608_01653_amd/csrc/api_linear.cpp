@@ -123,8 +123,9 @@ int32_t check_product(const hatq_linear_weights *W, bool grouped, const int32_t 
     return check_rows(y, y_type, rows, W->cout, y_stride);
 }
 
-int32_t product(const hatq_linear_weights *W, const int8_t *xq, const float *sx, int32_t x_rows, const int32_t *ends,
-                const int32_t *src, int32_t rows, void *y, int32_t y_type, int64_t y_stride, hipStream_t st) {
+hatq::LinearArgs product_args(const hatq_linear_weights *W, const int8_t *xq, const float *sx, int32_t x_rows,
+                              const int32_t *ends, const int32_t *src, int32_t rows, void *y, int32_t y_type,
+                              int64_t y_stride) {
     hatq::LinearArgs a{};
     a.xq = xq;
     a.sx = sx;
@@ -144,11 +145,17 @@ int32_t product(const hatq_linear_weights *W, const int8_t *xq, const float *sx,
     a.k_stride = W->k_stride;
     a.gated = W->gated;
     a.inv_b = 1.0f / (float)W->hblock;
-    return hip_status(hatq::launch_linear(a, st));
+    return a;
 }
 
-int32_t quantize(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t rows, int64_t x_stride,
-                 int8_t *xq, float *sx, hipStream_t st) {
+int32_t product(const hatq_linear_weights *W, const int8_t *xq, const float *sx, int32_t x_rows, const int32_t *ends,
+                const int32_t *src, int32_t rows, void *y, int32_t y_type, int64_t y_stride, hipStream_t st) {
+    return hip_status(hatq::launch_linear(
+        product_args(W, xq, sx, x_rows, ends, src, rows, y, y_type, y_stride), st));
+}
+
+hatq::TokenArgs token_args(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t rows,
+                           int64_t x_stride, int8_t *xq, float *sx) {
     hatq::TokenArgs a{};
     a.x = x;
     a.xq = xq;
@@ -159,7 +166,20 @@ int32_t quantize(const hatq_linear_weights *W, const void *x, int32_t x_type, in
     a.cin = W->cin;
     a.k_stride = W->k_stride;
     a.log_b = log_block(W->hblock);
-    return hip_status(hatq::launch_token_quant(a, st));
+    return a;
+}
+
+// Floats in, after the checks.  ws: hatq_linear_ws_bytes(W, x_rows).
+int32_t enqueue(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t x_rows, int64_t x_stride,
+                const int32_t *ends, const int32_t *src, int32_t rows, void *y, int32_t y_type, int64_t y_stride,
+                void *ws, hipStream_t st) {
+    int8_t *xq = static_cast<int8_t *>(ws);
+    float *sx = reinterpret_cast<float *>(xq + align256((size_t)x_rows * W->k_stride));
+    const hatq::TokenArgs t = token_args(W, x, x_type, x_rows, x_stride, xq, sx);
+    const hatq::LinearArgs a = product_args(W, xq, sx, x_rows, ends, src, rows, y, y_type, y_stride);
+    if (hatq::linear_takes_tokens(a)) return hip_status(hatq::launch_linear_tokens(a, t, st));
+    if (hatq::launch_token_quant(t, st) != hipSuccess) return HATQ_EHIP;
+    return hip_status(hatq::launch_linear(a, st));
 }
 
 int32_t forward(const hatq_linear_weights *W, bool grouped, const void *x, int32_t x_type, int32_t x_rows,
@@ -170,11 +190,38 @@ int32_t forward(const hatq_linear_weights *W, bool grouped, const void *x, int32
     if ((s = check_rows(x, x_type, x_rows, W->cin, x_stride)) != HATQ_OK) return s;
     if (!ws || !aligned(ws, 256)) return HATQ_EINVAL;
     if (ws_bytes < hatq_linear_ws_bytes(W, x_rows)) return HATQ_EWORKSPACE;
-    int8_t *xq = static_cast<int8_t *>(ws);
-    float *sx = reinterpret_cast<float *>(xq + align256((size_t)x_rows * W->k_stride));
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    if ((s = quantize(W, x, x_type, x_rows, x_stride, xq, sx, st)) != HATQ_OK) return s;
-    return product(W, xq, sx, x_rows, ends, src, rows, y, y_type, y_stride, st);
+    return enqueue(W, x, x_type, x_rows, x_stride, ends, src, rows, y, y_type, y_stride, ws,
+                   static_cast<hipStream_t>(stream));
+}
+
+int32_t check_mlp(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out) {
+    int32_t s = check_weights(W_in);
+    if (s == HATQ_OK) s = check_weights(W_out);
+    if (s != HATQ_OK) return s;
+    const bool fit = W_in->gated && !W_out->gated && W_in->experts == W_out->experts && W_in->cout == W_out->cin;
+    return fit ? HATQ_OK : HATQ_EINVAL;
+}
+
+// hatq_expert_mlp's workspace: ends (at 0), src, pos, hidden and output rows, and what
+// one call at a time needs.  bytes = 0 for sizes that are not supported.
+struct MlpPlaces {
+    size_t src, pos, hidden, rows, scratch, bytes;
+};
+MlpPlaces mlp_places(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out, int32_t tokens, int32_t topk) {
+    MlpPlaces p{};
+    const size_t order = hatq_expert_order_ws_bytes(tokens, topk, W_in->experts);
+    if (order == 0 || tokens <= 0) return p;
+    const size_t pairs = (size_t)tokens * topk;
+    p.src = align256((size_t)W_in->experts * 4);
+    p.pos = p.src + align256(pairs * 4);
+    p.hidden = p.pos + align256(pairs * 4);
+    p.rows = p.hidden + align256(pairs * W_in->cout * 4);
+    p.scratch = p.rows + align256(pairs * W_out->cout * 4);
+    size_t most = order;
+    for (size_t n : {hatq_linear_ws_bytes(W_in, tokens), hatq_linear_ws_bytes(W_out, (int32_t)pairs)})
+        if (n > most) most = n;
+    p.bytes = p.scratch + most;
+    return p;
 }
 
 }  // namespace
@@ -213,7 +260,8 @@ int32_t hatq_token_quant(const void *x, int32_t x_type, int32_t rows, int32_t ci
     W.cin = cin;
     W.k_stride = k_stride_of(cin);
     W.hblock = hblock;
-    return quantize(&W, x, x_type, rows, x_stride, xq, act_scale, static_cast<hipStream_t>(stream));
+    return hip_status(hatq::launch_token_quant(token_args(&W, x, x_type, rows, x_stride, xq, act_scale),
+                                               static_cast<hipStream_t>(stream)));
 }
 
 int32_t hatq_linear_int8(const hatq_linear_weights *W, const int8_t *xq, const float *act_scale, int32_t rows,
@@ -296,6 +344,47 @@ int32_t hatq_expert_combine(const float *h, int32_t h_rows, int32_t cols, int64_
     a.tokens = tokens;
     a.topk = topk;
     return hip_status(hatq::launch_expert_combine(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t hatq_expert_mlp_ws_bytes(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out, int32_t tokens,
+                                int32_t topk) {
+    if (check_mlp(W_in, W_out) != HATQ_OK) return 0;
+    const MlpPlaces p = mlp_places(W_in, W_out, tokens, topk);
+    return p.bytes;
+}
+
+int32_t hatq_expert_mlp(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out, const void *x,
+                        int32_t x_type, int32_t tokens, int64_t x_stride, const int32_t *ids, const float *weights,
+                        int32_t topk, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,
+                        void *stream) {
+    int32_t s = check_mlp(W_in, W_out);
+    if (s != HATQ_OK) return s;
+    if (tokens < 0 || topk <= 0) return HATQ_EINVAL;
+    if (tokens == 0) return HATQ_OK;
+    const MlpPlaces p = mlp_places(W_in, W_out, tokens, topk);
+    if (p.bytes == 0) return HATQ_EUNSUPPORTED;
+    if ((s = check_rows(x, x_type, tokens, W_in->cin, x_stride)) != HATQ_OK) return s;
+    if ((s = check_rows(y, y_type, tokens, W_out->cout, y_stride)) != HATQ_OK) return s;
+    if (!ids || !weights || !aligned(ids, 4) || !aligned(weights, 4)) return HATQ_EINVAL;
+    if (!ws || !aligned(ws, 256)) return HATQ_EINVAL;
+    if (ws_bytes < p.bytes) return HATQ_EWORKSPACE;
+    int8_t *base = static_cast<int8_t *>(ws);
+    int32_t *ends = reinterpret_cast<int32_t *>(base), *src = reinterpret_cast<int32_t *>(base + p.src),
+            *pos = reinterpret_cast<int32_t *>(base + p.pos);
+    float *hidden = reinterpret_cast<float *>(base + p.hidden), *rows = reinterpret_cast<float *>(base + p.rows);
+    const int32_t pairs = tokens * topk;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const hatq::OrderArgs o{ids, ends, src, pos, reinterpret_cast<int32_t *>(base + p.scratch), tokens, topk,
+                            W_in->experts};
+    if (hatq::launch_expert_order(o, st) != hipSuccess) return HATQ_EHIP;
+    if ((s = enqueue(W_in, x, x_type, tokens, x_stride, ends, src, pairs, hidden, HATQ_F32, W_in->cout,
+                     base + p.scratch, st)) != HATQ_OK)
+        return s;
+    if ((s = enqueue(W_out, hidden, HATQ_F32, pairs, W_in->cout, ends, nullptr, pairs, rows, HATQ_F32, W_out->cout,
+                     base + p.scratch, st)) != HATQ_OK)
+        return s;
+    const hatq::CombineArgs c{rows, pos, weights, y, W_out->cout, y_stride, y_type, pairs, W_out->cout, tokens, topk};
+    return hip_status(hatq::launch_expert_combine(c, st));
 }
 
 }  // extern "C"

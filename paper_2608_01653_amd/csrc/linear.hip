@@ -145,24 +145,26 @@ __device__ void zero_tile(const LinearArgs &a, int row0, int rows, int c0, int c
 }
 
 // ---- few rows -------------------------------------------------------------------------
-// A block takes 16 output channels (gated: of their gates and their values) and 16 MT
-// rows; its waves share the contraction, 64 bytes in turn, and add up in LDS.  The
-// weights go from memory to registers in runs of 1 KB, U of them in flight a wave:
-// the kernel is bound by their bytes.
+// Eight waves, WK of them on one group of 16 output channels (gated: of their gates and
+// their values) by 16 MT rows: they take the contraction 64 bytes in turn and add up in
+// LDS; 8 / WK groups a block.  The weights go from memory to registers in runs of 1 KB,
+// U of them in flight a wave: the kernel is bound by their bytes.  WK is large where the
+// groups alone would not fill the card.
 template <int MT, int G, int U>
-__global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) {
+__global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, int wk) {
     constexpr int WAVES = 8;
     __shared__ v4i part[WAVES][MT][G][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int groups = (a.cout + 15) / 16;
+    const int per = WAVES / wk, groups = (a.cout + 16 * per - 1) / (16 * per);
     const int bid = blockIdx.y * gridDim.x + blockIdx.x;
-    const int t = bid / groups, c16 = bid - t * groups;
+    const int t = bid / groups, g0 = (bid - t * groups) * per;
     RowTile r;
     if (!row_tile<16 * MT>(a, t, r)) return;
     const int rows = min(r.end - r.row0, 16 * MT);
-    if (r.expert < 0) return zero_tile(a, r.row0, rows, c16 * 16, 16);
+    if (r.expert < 0) return zero_tile(a, r.row0, rows, g0 * 16, 16 * per);
 
-    const int nks = a.k_stride >> 6;
+    const int nks = a.k_stride >> 6, first = wave & (wk - 1);
+    const int c16 = min(g0 + wave / wk, (a.cout + 15) / 16 - 1);    // (a wave past the last group repeats it)
     const int block0 = G == 1 ? c16 : (c16 >> 1) * 4 + (c16 & 1);   // of 16 packed columns
     const int8_t *w = a.wp + ((int64_t)r.expert * a.cout_pad + block0 * 16) * a.k_stride + lane * 16;
     const int64_t value = (int64_t)32 * a.k_stride;   // from the gates' columns to the values'
@@ -179,11 +181,11 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) 
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int g = 0; g < G; ++g) acc[m][g] = v4i{0, 0, 0, 0};
-    for (int k0 = wave; k0 < nks; k0 += WAVES * U) {
+    for (int k0 = first; k0 < nks; k0 += wk * U) {
         v4i fw[U][G], fx[U][MT];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int k = min(k0 + WAVES * u, nks - 1);
+            const int k = min(k0 + wk * u, nks - 1);
 #pragma unroll
             for (int g = 0; g < G; ++g) fw[u][g] = *reinterpret_cast<const v4i *>(w + g * value + (int64_t)k * 1024);
 #pragma unroll
@@ -191,7 +193,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) 
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (k0 + WAVES * u >= nks) break;
+            if (k0 + wk * u >= nks) break;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -199,23 +201,27 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) 
                     acc[m][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][g], fx[u][m], acc[m][g], 0, 0, 0);
         }
     }
+    if (wk > 1) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int g = 0; g < G; ++g) part[wave][m][g][lane] = acc[m][g];
-    __syncthreads();
+            for (int g = 0; g < G; ++g) part[wave][m][g][lane] = acc[m][g];
+        __syncthreads();
+    }
     const bool vec = vector_rows(a);
     const float *w_scale = a.w_scale + (int64_t)r.expert * a.cout_pad, *bias = a.bias + (int64_t)r.expert * a.cout_pad;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-        if (m % WAVES != wave) continue;
+        if ((m & (wk - 1)) != first) continue;   // a group's waves share its row tiles
         float z[2][4];
         const int p = block0 * 16 + (lane >> 4) * 4;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            v4i sum = part[0][m][g][lane];
-#pragma unroll
-            for (int k = 1; k < WAVES; ++k) sum += part[k][m][g][lane];
+            v4i sum = acc[m][g];
+            if (wk > 1) {
+                sum = part[wave - first][m][g][lane];
+                for (int k = 1; k < wk; ++k) sum += part[wave - first + k][m][g][lane];
+            }
             const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
             dequant4(a, w_scale + p + 32 * g, bias + p + 32 * g, q, s[m], z[g]);
         }
@@ -224,8 +230,121 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a) 
             for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
         }
         const int row = 16 * m + (lane & 15), c = c16 * 16 + (lane >> 4) * 4;
-        if (row < rows && c < a.cout) put4(a, r.row0 + row, c, z[0], vec);
+        if (row < rows && c < a.cout && c16 == g0 + wave / wk) put4(a, r.row0 + row, c, z[0], vec);
     }
+}
+
+// ---- few tokens, floats in ------------------------------------------------------------
+// At most 16 rows, one layer, with the tokens' quantization in front: every block makes the codes of its
+// rows itself, in LDS, while its first weights are on their way.  WR waves share a row
+// (and 8 / WR rows are taken at once), a lane CH chunks of 8 elements.  It pays where a
+// block has few elements to quantize: one launch instead of two, and no codes in memory.
+template <typename T, int G, int CH, int WR>
+__global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, const TokenArgs x, int vec) {
+    constexpr int WAVES = 8, U = 8, RT = 64 * WR;
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    v4i(*part)[G][64] = reinterpret_cast<v4i(*)[G][64]>(lds);                // [WAVES][G][64]
+    float *scale = reinterpret_cast<float *>(lds + WAVES * G * 1024);          // [16]
+    float *most = scale + 16;                                                  // [WAVES]
+    int8_t *codes = lds + WAVES * G * 1024 + 128;                              // [rows][k_stride + 16]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c16 = blockIdx.x, rows = a.rows;
+    const int pitch = a.k_stride + 16;   // 16 rows' pieces then lie in different banks
+
+    const int rt = (wave % WR) * 64 + lane;
+    float v[8 * CH];
+    auto load = [&](int row) {
+        const T *p = static_cast<const T *>(x.x) + min(row, rows - 1) * x.x_stride;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int e = (i * RT + rt) * 8;
+            if (vec && e + 8 <= x.cin) {
+                load8(p + e, &v[8 * i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < x.cin ? to_float(p[e + j]) : 0.0f;
+            }
+        }
+    };
+    load(wave / WR);
+
+    const int nks = a.k_stride >> 6;
+    const int block0 = G == 1 ? c16 : (c16 >> 1) * 4 + (c16 & 1);   // of 16 packed columns
+    const int8_t *w = a.wp + (int64_t)block0 * 16 * a.k_stride + lane * 16;
+    const int64_t value = (int64_t)32 * a.k_stride;   // from the gates' columns to the values'
+    v4i fw[U][G];
+    auto weights = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+                fw[u][g] = *reinterpret_cast<const v4i *>(w + g * value + (int64_t)min(k0 + WAVES * u, nks - 1) * 1024);
+    };
+    weights(wave);
+    __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
+
+    for (int first = 0; first < rows; first += WAVES / WR) {
+        const int row = first + wave / WR;
+        if (first) load(row);
+        const float sigma = token_butterfly(v, lane, x.log_b);
+        float m = token_max(v);
+        if constexpr (WR > 1) {
+            if (first) __syncthreads();   // the row before has been read
+            if (lane == 0) most[wave] = m;
+            __syncthreads();
+            m = most[0];
+#pragma unroll
+            for (int k = 1; k < WR; ++k) m = __builtin_elementwise_maximum(m, most[k]);
+        }
+        const float s = token_scale(m), rs = sigma * (1.0f / s);
+        const bool plain = token_plain(s);
+        if (row < rows) {
+            if (rt == 0) scale[row] = s;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int c = i * RT + rt;
+                const uint2 q = token_codes8(&v[8 * i], sigma, s, rs, plain);
+                if (c < a.k_stride >> 3) *reinterpret_cast<uint2 *>(codes + row * pitch + c * 8) = q;
+            }
+        }
+    }
+    __syncthreads();
+
+    const int mine = min(lane & 15, rows - 1);
+    const int8_t *from = codes + mine * pitch + (lane >> 4) * 16;
+    v4i acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) acc[g] = v4i{0, 0, 0, 0};
+    for (int k0 = wave; k0 < nks; k0 += WAVES * U) {
+        if (k0 != wave) weights(k0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k0 + WAVES * u >= nks) break;
+            const v4i fx = *reinterpret_cast<const v4i *>(from + (k0 + WAVES * u) * 64);
+#pragma unroll
+            for (int g = 0; g < G; ++g) acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][g], fx, acc[g], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) part[wave][g][lane] = acc[g];
+    __syncthreads();
+    if (wave != 0) return;
+    float z[2][4];
+    const int p = block0 * 16 + (lane >> 4) * 4;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        v4i sum = part[0][g][lane];
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) sum += part[k][g][lane];
+        const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
+        dequant4(a, a.w_scale + p + 32 * g, a.bias + p + 32 * g, q, scale[mine], z[g]);
+    }
+    if (G == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
+    }
+    const int c = c16 * 16 + (lane >> 4) * 4;
+    if ((lane & 15) < rows && c < a.cout) put4(a, lane & 15, c, z[0], vector_rows(a));
 }
 
 // ---- many rows --------------------------------------------------------------------------
@@ -435,10 +554,28 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
 }
 
 template <int MT, int U>
-void stream(const LinearArgs &a, hipStream_t st) {
-    const dim3 grid = grid_of(row_tiles(a, 16 * MT) * ((a.cout + 15) / 16));
-    if (a.gated) linear_stream_kernel<MT, 2, U><<<grid, 512, 0, st>>>(a);
-    else linear_stream_kernel<MT, 1, U><<<grid, 512, 0, st>>>(a);
+void stream(const LinearArgs &a, hipStream_t st, int wk) {
+    const int cols = 16 * 8 / wk;
+    const dim3 grid = grid_of(row_tiles(a, 16 * MT) * ((a.cout + cols - 1) / cols));
+    if (a.gated) linear_stream_kernel<MT, 2, U><<<grid, 512, 0, st>>>(a, wk);
+    else linear_stream_kernel<MT, 1, U><<<grid, 512, 0, st>>>(a, wk);
+}
+
+template <typename T, int CH, int WR>
+void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
+    const int grid = (a.cout + 15) / 16;
+    const size_t bytes = 8 * (a.gated ? 2 : 1) * 1024 + 128 + (size_t)a.rows * (a.k_stride + 16);
+    const int vec = (reinterpret_cast<uintptr_t>(x.x) & 15) == 0 && x.x_stride * (int)sizeof(T) % 16 == 0;
+    if (a.gated) linear_token_kernel<T, 2, CH, WR><<<grid, 512, bytes, st>>>(a, x, vec);
+    else linear_token_kernel<T, 1, CH, WR><<<grid, 512, bytes, st>>>(a, x, vec);
+}
+template <typename T>
+void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
+    if (a.k_stride <= 512) token<T, 1, 1>(a, x, st);
+    else if (a.k_stride <= 1024 && a.rows > 1) token<T, 2, 1>(a, x, st);
+    else if (a.k_stride <= 4096) token<T, 1, 8>(a, x, st);
+    else if (a.k_stride <= 8192) token<T, 2, 8>(a, x, st);
+    else token<T, 4, 8>(a, x, st);
 }
 
 template <int WM, int WN, int FM, int FN, int STAGES>
@@ -453,12 +590,23 @@ void tile(const LinearArgs &b, hipStream_t st) {
 
 }  // namespace
 
+bool linear_takes_tokens(const LinearArgs &a) {
+    return !a.ends && a.rows <= 16 && (int64_t)a.rows * a.k_stride <= 16384;
+}
+
+hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
+    if (x.x_type == kF32) token<float>(a, x, st);
+    else if (x.x_type == kBf16) token<bf16_t>(a, x, st);
+    else token<_Float16>(a, x, st);
+    return hipGetLastError();
+}
+
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st) {
     // rows a group has on average
     const int64_t per = a.ends ? (a.rows + a.experts - 1) / a.experts : a.rows;
-    if (per <= 16) stream<1, 8>(a, st);
-    else if (per <= 32) stream<2, 4>(a, st);
-    else if (per <= 64) stream<4, 4>(a, st);
+    if (per <= 16) stream<1, 8>(a, st, 8);
+    else if (per <= 32) stream<2, 4>(a, st, 8);
+    else if (per <= 64) stream<4, 4>(a, st, 8);
     else {
         const int64_t big = row_tiles(a, 256) * ((a.cout_pad + 255) / 256);
         if (big >= 256) tile<2, 4, 4, 2, 4>(a, st);

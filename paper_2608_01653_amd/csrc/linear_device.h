@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "hatq_device.h"
+
 namespace hatq {
 
 constexpr int kF32 = 0, kBf16 = 1, kF16 = 2;   // hatq_dtype
@@ -79,5 +81,97 @@ __device__ __forceinline__ void store16(_Float16 *p, const float *v) {
     for (int j = 0; j < 8; ++j) h[j] = (_Float16)v[j];
     *reinterpret_cast<v8h *>(p) = h;
 }
+
+// ---- token codes --------------------------------------------------------------------
+// A lane holds chunks of 8 adjacent elements, neighbouring lanes neighbouring chunks:
+// index bits 0-2 are registers, bits 3-6 lanes of one 16-lane row, so the butterflies of
+// a block of up to 128 stay inside a DPP row.
+
+// The order-2^lb butterfly of every chunk; returns the sign of the values held relative
+// to the transform's (hatq_device.h, cross_stage).
+template <int R>
+__device__ __forceinline__ float token_butterfly(float (&v)[R], int lane, int lb) {
+    float sigma = 1.0f;
+    if (lb >= 1) reg_stage<1>(v);
+    if (lb >= 2) reg_stage<2>(v);
+    if (lb >= 3) reg_stage<4>(v);
+    if (lb >= 4) {
+        const float c = (lane & 1) ? -1.0f : 1.0f;
+        cross_stage<1>(v, c);
+        sigma *= c;
+    }
+    if (lb >= 5) {
+        const float c = (lane & 2) ? -1.0f : 1.0f;
+        cross_stage<2>(v, c);
+        sigma *= c;
+    }
+    if (lb >= 6) {
+        const float c = (lane & 4) ? -1.0f : 1.0f;
+        cross_stage<4>(v, c);
+        sigma *= c;
+    }
+    if (lb >= 7) {
+        const float c = (lane & 8) ? -1.0f : 1.0f;
+        cross_stage<8>(v, c);
+        sigma *= c;
+    }
+    return sigma;
+}
+
+// max |v| of the wave, NaN where one of them is (v_maximum, not v_max).
+template <int R>
+__device__ __forceinline__ float token_max(const float (&v)[R]) {
+    float m = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; r += 2)
+        m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(v[r]), fabsf(v[r + 1])), m);
+    m = __builtin_elementwise_maximum(m, lane_xor<1>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<2>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<4>(m));
+    m = __builtin_elementwise_maximum(m, lane_xor<8>(m));
+    const uint32_t u = __float_as_uint(m);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    m = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const uint32_t w = __float_as_uint(m);
+    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    return __builtin_elementwise_maximum(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// s = fl32(m / 127), 1 where that is 0, NaN where m is not finite.
+__device__ __forceinline__ float token_scale(float m) {
+    const float s = m / 127.0f;
+    return !(m < __builtin_inff()) ? __builtin_nanf("") : s == 0.0f ? 1.0f : s;
+}
+
+// Codes of one chunk, rne(fl32(sigma v / s)), as 8 bytes.  u = fl(v r + 1.5 2^23), r =
+// sigma / s, rounds the exact product to the nearest integer k in one fma and d =
+// fl(v r - k) in another; |v r - v / s| <= 127 2^-24, d is within 2^-25 of its exact
+// value and fl(v / s) within 2^-18 of v / s, so |d| <= 0.5 - 2^-16 gives k = rne(fl(v /
+// s)).  A chunk with an element nearer to a half-integer, and any with s outside
+// [2^-125, 2^125] (`plain` false), divides.  Where s is NaN the codes are 0.
+__device__ __forceinline__ uint2 token_codes8(const float *v, float sigma, float s, float r, bool plain) {
+    uint32_t u[8];
+    float m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        float d[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float k = __builtin_fmaf(v[j + e], r, HATQ_MAGIC);
+            u[j + e] = __float_as_uint(k);   // |v r| < 127.5: a code
+            d[e] = __builtin_fmaf(v[j + e], r, -(k - HATQ_MAGIC));
+        }
+        m = fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), m);
+    }
+    if (!(plain && m <= 0.5f - 0x1p-16f)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float q = clamp127(rintf((sigma * v[j]) / s));
+            u[j] = s == s ? (uint32_t)(int32_t)q : 0u;
+        }
+    }
+    return make_uint2(pack_low_bytes(u[0], u[1], u[2], u[3]), pack_low_bytes(u[4], u[5], u[6], u[7]));
+}
+__device__ __forceinline__ bool token_plain(float s) { return s >= 0x1p-125f && s <= 0x1p125f; }
 
 }  // namespace hatq

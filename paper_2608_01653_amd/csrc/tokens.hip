@@ -13,12 +13,8 @@ constexpr int kThreads = 256;
 // S = B x per token, s = fl32(max|S| / 127), q = clamp(rne(fl32(S / s))).
 //
 // A token's row stays in registers between its maximum and its codes, so x is read
-// once.  A lane holds chunks of 8 adjacent elements, chunk i of row thread t being
-// number i * 64 * WAVES + t: index bits 0-2 are registers, bits 3-6 lanes of one
-// 16-lane row, so the butterflies of a block of up to 128 never leave a DPP row.
-//
-// The maximum is taken over the bits of |S| as integers, which puts infinities
-// and NaN above every number: such a token gets the scale NaN and codes 0.
+// once.  Chunk i of row thread t is number i * 64 * WAVES + t.  The maximum keeps NaN:
+// a token with a value that is not finite gets the scale NaN and codes 0.
 template <int WAVES, int CH, typename T>
 __global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quant_kernel(const TokenArgs a, int vec) {
     constexpr int RT = 64 * WAVES;   // threads of a row
@@ -40,79 +36,26 @@ __global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quan
             for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < a.cin ? to_float(x[e + j]) : 0.0f;
         }
     }
-    float sigma = 1.0f;
-    const int lb = a.log_b;
-    if (lb >= 1) reg_stage<1>(v);
-    if (lb >= 2) reg_stage<2>(v);
-    if (lb >= 3) reg_stage<4>(v);
-    if (lb >= 4) {
-        const float c = (t & 1) ? -1.0f : 1.0f;
-        cross_stage<1>(v, c);
-        sigma *= c;
-    }
-    if (lb >= 5) {
-        const float c = (t & 2) ? -1.0f : 1.0f;
-        cross_stage<2>(v, c);
-        sigma *= c;
-    }
-    if (lb >= 6) {
-        const float c = (t & 4) ? -1.0f : 1.0f;
-        cross_stage<4>(v, c);
-        sigma *= c;
-    }
-    if (lb >= 7) {
-        const float c = (t & 8) ? -1.0f : 1.0f;
-        cross_stage<8>(v, c);
-        sigma *= c;
-    }
-    uint32_t m = 0;
-#pragma unroll
-    for (int r = 0; r < CH * 8; ++r) m = max(m, __float_as_uint(v[r]) & 0x7fffffffu);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+    const float sigma = token_butterfly(v, t, a.log_b);
+    float m = token_max(v);
     if constexpr (WAVES > 1) {
-        __shared__ uint32_t red[WAVES];
+        __shared__ float red[WAVES];
         if ((t & 63) == 0) red[t >> 6] = m;
         __syncthreads();
         m = red[0];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) m = max(m, red[w]);
+        for (int w = 1; w < WAVES; ++w) m = __builtin_elementwise_maximum(m, red[w]);
     }
-    const bool finite = m < 0x7f800000u;
-    float s = __uint_as_float(m) / 127.0f;
-    if (s == 0.0f) s = 1.0f;
-    if (!finite) s = __uint_as_float(0x7fc00000u);
+    const float s = token_scale(m);
     if (t == 0) a.sx[row] = s;
-
-    // rne(fl32(S / s)) without a division but near a half-integer (HATQ_NEAR_TIE)
     const float r = sigma * (1.0f / s);
-    const bool plain = s >= 0x1p-125f && s <= 0x1p125f;
+    const bool plain = token_plain(s);
     int8_t *q = a.xq + (int64_t)row * a.k_stride;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * RT + t;
-        uint32_t u[8];
-        bool near = !plain;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float p = v[8 * i + j] * r, k = p + HATQ_MAGIC;
-            near |= fabsf(p - (k - HATQ_MAGIC)) > HATQ_NEAR_TIE;
-            u[j] = __float_as_uint(k);   // |p| <= 127 (1 + 2^-22): within the code range after rounding
-        }
-        if (near) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float d = clamp127(rintf((sigma * v[8 * i + j]) / s));
-                u[j] = (uint32_t)(int32_t)d;
-            }
-        }
-        if (!finite) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) u[j] = 0;
-        }
-        if (c < chunks)
-            *reinterpret_cast<uint2 *>(q + c * 8) =
-                make_uint2(pack_low_bytes(u[0], u[1], u[2], u[3]), pack_low_bytes(u[4], u[5], u[6], u[7]));
+        const uint2 codes = token_codes8(&v[8 * i], sigma, s, r, plain);
+        if (c < chunks) *reinterpret_cast<uint2 *>(q + c * 8) = codes;
     }
 }
 
@@ -357,21 +300,15 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a, 
 
 hipError_t launch_token_quant(const TokenArgs &a, hipStream_t st) {
     const int chunks = a.k_stride >> 3;
-    // A wave a row where the rows fill the card; else a row over more waves, so that
-    // a few tokens' loads are in flight at once.
+    // Two chunks a lane and the waves a row takes.  (bf16, order 128, us: 4096 rows of
+    // 4096 13.8 on four waves, 14.8 on two of four chunks, 15.4 on one of eight, 20.6 on
+    // eight of one; 1 row of 4096 3.1, 4.1, 6.1, 3.1; 4096 rows of 2048 7.7 on two waves,
+    // 7.8 on one, 11.5 on four.)
     if (chunks <= 64) return token_launch<1, 1>(a, st);
-    const bool many = a.rows >= 1024;
-    if (many || chunks <= 128) {
-        if (chunks <= 128) return token_launch<1, 2>(a, st);
-        if (chunks <= 256) return token_launch<1, 4>(a, st);
-        if (chunks <= 512) return token_launch<1, 8>(a, st);
-    }
-    if (many || chunks <= 1024) {
-        if (chunks <= 256) return token_launch<4, 1>(a, st);
-        if (chunks <= 512) return token_launch<4, 2>(a, st);
-        if (chunks <= 1024) return token_launch<4, 4>(a, st);
-        if (chunks <= 2048) return token_launch<4, 8>(a, st);
-    }
+    if (chunks <= 128) return token_launch<1, 2>(a, st);
+    if (chunks <= 256) return token_launch<2, 2>(a, st);
+    if (chunks <= 512) return token_launch<4, 2>(a, st);
+    if (chunks <= 1024) return token_launch<8, 2>(a, st);
     if (chunks <= 2048) return token_launch<16, 2>(a, st);
     if (chunks <= 4096) return token_launch<16, 4>(a, st);
     return token_launch<16, 8>(a, st);

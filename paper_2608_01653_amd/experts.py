@@ -1,16 +1,15 @@
 """A feed-forward block of gated experts on the INT8 linear layers over tokens.
 
-One pass for tokens x, their chosen experts and those experts' weights:
-  1. the pairs (token, expert) are sorted by expert (hatq_expert_order);
-  2. each token is quantized once and goes through the gated layer of each of its
-     experts (hatq_experts_forward: rows gathered from the tokens, silu(g) u in the
-     epilogue, float32 hidden rows);
-  3. each hidden row is quantized and goes through its expert's second layer
-     (hatq_experts_forward, float32 rows: they are summed before the one rounding);
-  4. a token's rows are summed with their weights (hatq_expert_combine).
+One pass for tokens x, their chosen experts and those experts' weights (one call of the
+library, hatq_expert_mlp):
+  1. the pairs (token, expert) are sorted by expert;
+  2. each token goes through the gated layer of each of its experts: rows gathered from
+     the tokens' codes, silu(g) u in the epilogue, float32 hidden rows;
+  3. each hidden row is quantized and goes through its expert's second layer, into
+     float32 rows: they are summed before the one rounding;
+  4. a token's rows are summed with their weights.
 
-Every step runs in the library's kernels; this module only allocates and sequences
-the calls.  With one expert and ids of 0 it is a plain gated feed-forward block.
+With one expert and ids of 0 it is a plain gated feed-forward block.
 """
 from __future__ import annotations
 
@@ -34,10 +33,4 @@ class ExpertMLP:
                  out_dtype: Optional[torch.dtype] = None, stream=None) -> torch.Tensor:
         """x [tokens, cin], ids int32 and weights float32 [tokens, topk] -> [tokens, cout]
         of out_dtype (default: x's).  An id outside the experts adds nothing."""
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return self(x, ids, weights, out_dtype)
-        ends, src, pos = hatq.hatq_expert_order(ids, self.w_in.experts)
-        hidden = hatq.hatq_experts_forward(self.w_in, x, ends, src, out_dtype=torch.float32)
-        rows = hatq.hatq_experts_forward(self.w_out, hidden, ends, out_dtype=torch.float32)
-        return hatq.hatq_expert_combine(rows, pos, weights, out_dtype=out_dtype or x.dtype)
+        return hatq.hatq_expert_mlp(self.w_in, self.w_out, x, ids, weights, out_dtype=out_dtype, stream=stream)

@@ -63,7 +63,8 @@ EXPORTS = ["hatq_status_string", "hatq_conv_out_hw", "hatq_weights_bytes", "hatq
            "hatq_layer_ws_bytes", "hatq_layer_forward",
            "hatq_linear_weights_bytes", "hatq_prepare_linear", "hatq_pack_linear", "hatq_token_quant",
            "hatq_linear_int8", "hatq_linear_ws_bytes", "hatq_linear_forward", "hatq_experts_int8",
-           "hatq_experts_forward", "hatq_expert_order_ws_bytes", "hatq_expert_order", "hatq_expert_combine"]
+           "hatq_experts_forward", "hatq_expert_order_ws_bytes", "hatq_expert_order", "hatq_expert_combine",
+           "hatq_expert_mlp_ws_bytes", "hatq_expert_mlp"]
 
 _lib = None
 
@@ -160,6 +161,10 @@ def load(build_if_missing: bool = False):
     L.hatq_expert_order.restype = i32
     L.hatq_expert_combine.argtypes = [P, i32, i32, i64, P, P, i32, i32, P, i32, i64, P]
     L.hatq_expert_combine.restype = i32
+    L.hatq_expert_mlp_ws_bytes.argtypes = [W, W, i32, i32]
+    L.hatq_expert_mlp_ws_bytes.restype = sz
+    L.hatq_expert_mlp.argtypes = [W, W, P, i32, i32, i64, P, P, i32, P, i32, i64, P, sz, P]
+    L.hatq_expert_mlp.restype = i32
     _lib = L
     return L
 
@@ -896,4 +901,30 @@ def hatq_expert_combine(h: torch.Tensor, pos: torch.Tensor, weights: torch.Tenso
     y, ys, yt = _out_rows(y, t, c, out_dtype, h.device)
     _check(load().hatq_expert_combine(h.data_ptr(), n, c, hs, pos.data_ptr(), weights.data_ptr(), t, k, y.data_ptr(),
                                       yt, ys, _stream()), "hatq_expert_combine")
+    return y
+
+
+def hatq_expert_mlp_ws_bytes(w_in: PreparedLinear, w_out: PreparedLinear, tokens: int, topk: int) -> int:
+    return int(load().hatq_expert_mlp_ws_bytes(w_in.ref, w_out.ref, tokens, topk))
+
+
+@_on_stream
+def hatq_expert_mlp(w_in: PreparedLinear, w_out: PreparedLinear, x: torch.Tensor, ids: torch.Tensor,
+                    weights: torch.Tensor, out_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None,
+                    ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Tokens x [tokens, cin] through their chosen gated experts, ids int32 and weights
+    fp32 [tokens, topk]: y [tokens, cout] of out_dtype (default: x's)."""
+    n, _, xs, xt = _rows(x, "x", w_in.cin)
+    if ids.dim() != 2 or ids.shape[0] != n or weights.shape != ids.shape:
+        raise ValueError(f"ids, weights: [{n}, topk] expected, got {tuple(ids.shape)}, {tuple(weights.shape)}")
+    _need(ids, "ids", torch.int32, 0)
+    _need(weights, "weights", torch.float32, 0)
+    y, ys, yt = _out_rows(y, n, w_out.cout, out_dtype or x.dtype, x.device)
+    topk = ids.shape[1]
+    if ws is None:
+        ws = torch.empty(max(hatq_expert_mlp_ws_bytes(w_in, w_out, n, topk), 256), dtype=torch.int8, device=x.device)
+    _need(ws, "ws", torch.int8, 0)
+    _check(load().hatq_expert_mlp(w_in.ref, w_out.ref, x.data_ptr(), xt, n, xs, ids.data_ptr(), weights.data_ptr(),
+                                  topk, y.data_ptr(), yt, ys, ws.data_ptr(), ws.numel(), _stream()),
+           "hatq_expert_mlp")
     return y

@@ -140,6 +140,22 @@ def test_refusals(L):
         assert comb(**bad) == EINVAL, bad
 
 
+@cpu_only
+def test_mlp_refusals(L):
+    def mlp(w_in=None, w_out=None, x=P, t=1, n=4, xs=192, ids=P, w=P, k=2, y=P, yt=1, ys=192, ws=P, size=1 << 20):
+        a, b = w_in or hatq.LinearWeights(5, 192, 64, 1, 64, 192, 128, P, P, P), w_out or hatq.LinearWeights(5, 64, 192, 0, 64, 64, 192, P, P, P)
+        return L.hatq_expert_mlp(ctypes.byref(a), ctypes.byref(b), x, t, n, xs, ids, w, k, y, yt, ys, ws, size, None)
+    assert mlp(n=0, x=None) == hatq.HATQ_OK
+    plain = hatq.LinearWeights(5, 192, 64, 0, 64, 192, 64, P, P, P)
+    other = hatq.LinearWeights(4, 64, 192, 0, 64, 64, 192, P, P, P)
+    wide = hatq.LinearWeights(5, 128, 192, 0, 64, 128, 192, P, P, P)
+    for bad in [dict(w_in=plain), dict(w_out=other), dict(w_out=wide), dict(x=None), dict(n=-1), dict(k=0), dict(xs=1), dict(ids=None),
+                dict(w=None), dict(w=P + 2), dict(y=None), dict(ys=5), dict(t=4), dict(ws=None), dict(ws=P + 32)]:
+        assert mlp(**bad) == hatq.HATQ_EINVAL, bad
+    assert mlp(size=100) == hatq.HATQ_EWORKSPACE
+    assert mlp(n=1 << 23, k=4) == hatq.HATQ_EUNSUPPORTED
+
+
 DRIVER = r"""
 #include <cstdio>
 #include <cstdlib>
@@ -149,6 +165,8 @@ namespace hatq {   // no launch may be reached
 hipError_t launch_token_quant(const TokenArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_linear_prepare(const LinearPrepArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_linear(const LinearArgs &, hipStream_t) { std::abort(); }
+bool linear_takes_tokens(const LinearArgs &) { std::abort(); }
+hipError_t launch_linear_tokens(const LinearArgs &, const TokenArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_expert_order(const OrderArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_expert_combine(const CombineArgs &, hipStream_t) { std::abort(); }
 size_t expert_order_ws_ints(int64_t pairs, int32_t experts) { return (size_t)pairs * experts; }
@@ -176,6 +194,10 @@ int main() {
                     if (!hatq_experts_forward(&W, F, 1, rows, c, i, i, rows, F, 0, d, F, 1, nullptr)) return 3;
                     if (!hatq_token_quant(F, 0, rows, c, INT64_MAX, 1, b, f, nullptr)) return 4;
                 }
+                hatq_linear_weights G = W;
+                G.gated = 1;
+                (void)hatq_expert_mlp_ws_bytes(&G, &W, c, d);
+                if (a > 0 && !hatq_expert_mlp(&G, &W, F, 0, a, c, i, f, d, F, 0, d, F, 1, nullptr)) return 9;
                 if (!hatq_prepare_linear(a, c, d, 0, 1, F, 0, nullptr, F, 1, &o, nullptr)) return 5;
                 if (!hatq_pack_linear(a, c, d, 1, 1, b, f, nullptr, F, 1, &o, nullptr)) return 6;
                 if (!hatq_expert_order(i, a, c, d, i, i, i, F, 1, nullptr)) return 7;

@@ -316,6 +316,44 @@ def test_forward(rows, cin, cout, b, gated, dtype):
     assert_close(wide, ref, err, torch.float32)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,cin,cout,b,pad", [
+    (1, 1, 1, 1, 0), (1, 64, 16, 64, 0), (2, 500, 40, 4, 1), (16, 512, 33, 128, 0), (9, 640, 20, 128, 8), (16, 1024, 50, 64, 0),
+    (1, 1024, 70, 64, 0), (3, 1100, 17, 2, 3), (4, 4096, 64, 128, 0), (3, 4097, 24, 1, 0), (2, 8192, 16, 128, 0), (1, 16384, 40, 128, 0),
+    (1, 16000, 16, 64, 8), (1, 20000, 16, 32, 0), (17, 256, 30, 64, 0)])
+def test_forward_is_its_two_steps(dtype, gated, rows, cin, cout, b, pad):
+    """Floats in and codes in give the same bits, whichever kernels a call takes."""
+    rng = np.random.default_rng(cin + rows)
+    lin = pack(make_layer(rng, 1, 2 * cout if gated else cout, cin), b, gated)
+    x, _ = tokens(rng, rows, cin, dtype, pad, pad // 2)
+    if rows > 1:
+        x[rows - 1, cin // 2] = float("inf")
+    g = Guarded((rows, cout), dtype)
+    hatq.hatq_linear_forward(lin, x, y=g.view)
+    g.check()
+    ref = hatq.hatq_linear_int8(lin, *hatq.hatq_token_quant(x, b), out_dtype=dtype)
+    assert torch.equal(g.view.nan_to_num(nan=7.0), ref.nan_to_num(nan=7.0))
+    assert rows == 1 or bool(torch.isnan(ref[rows - 1]).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("e,rows,cin,cout,gated", [(64, 48, 2048, 40, False), (32, 96, 512, 48, True), (8, 20, 256, 17, False), (4, 64, 960, 64, True),
+                                                   (200, 3, 4096, 16, False), (16, 300, 128, 16, False)])
+@pytest.mark.parametrize("skew", [False, True])
+def test_grouped_forward_is_its_two_steps(dtype, e, rows, cin, cout, gated, skew):
+    rng = np.random.default_rng(cin + rows)
+    lin = pack(make_layer(rng, e, 2 * cout if gated else cout, cin), 64, gated)
+    x, _ = tokens(rng, rows // 2 + 1, cin, dtype)
+    ends = np.cumsum(rng.multinomial(rows - rows // 8, rng.dirichlet(np.full(e, 0.05 if skew else 5.0)))).astype(np.int32)
+    src = rng.integers(-1, x.shape[0] + 1, rows).astype(np.int32)
+    g = Guarded((rows, cout), dtype)
+    hatq.hatq_experts_forward(lin, x, dev(ends), dev(src), y=g.view)
+    g.check()
+    ref = hatq.hatq_experts_int8(lin, *hatq.hatq_token_quant(x, 64), dev(ends), dev(src), out_dtype=dtype)
+    assert torch.equal(g.view, ref)
+
+
 # ---- grouped by expert ----------------------------------------------------------------------
 
 def grouped64(q, s, layer, ends, src, rows, b, gated):
