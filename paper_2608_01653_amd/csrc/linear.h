@@ -54,7 +54,6 @@ struct LinearArgs {
     int32_t rows, x_rows, experts;
     int32_t cout, cout_pad, k_stride;
     int32_t gated;
-    int32_t tiles_m;    // row tiles of the launch (set by it)
     float inv_b;
 };
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);

@@ -32,53 +32,74 @@ struct RowTile {
     int row0, end;  // rows [row0, min(row0 + BM, end))
 };
 
-// Row tiles of BM rows, each expert's rows starting a tile of their own: tile t of
-// them, or false past the last.  Every lane of the wave takes part; the ends are
-// clamped here, so any contents give rows in [0, rows).
+// Inclusive scans over the wave, of values >= 0, by DPP moves: rows of 16 lanes, then
+// lane 15 of each row to the next row, then lane 31 to the upper half.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_0(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+template <typename F>
+__device__ __forceinline__ int wave_scan(int v, F f) {
+    v = f(v, dpp_or_0<0x111, 0xF>(v));   // row_shr 1, 2, 4, 8
+    v = f(v, dpp_or_0<0x112, 0xF>(v));
+    v = f(v, dpp_or_0<0x114, 0xF>(v));
+    v = f(v, dpp_or_0<0x118, 0xF>(v));
+    v = f(v, dpp_or_0<0x142, 0xA>(v));   // row_bcast 15
+    return f(v, dpp_or_0<0x143, 0xC>(v));   // row_bcast 31
+}
+
+// Row tiles of BM rows, each expert's rows starting a tile of their own, and the rows
+// past the last end after them.  Every lane of the wave takes part, 64 experts at a
+// time; the ends are clamped here, so any contents give rows in [0, rows).
 template <int BM>
-__device__ bool row_tile(const LinearArgs &a, int t, RowTile &r) {
-    if (!a.ends) {
-        r = {0, t * BM, a.rows};
-        return r.row0 < a.rows;
-    }
-    const int lane = threadIdx.x & 63;
-    int last = 0, tiles = 0;
-    for (int base = 0; base < a.experts; base += 64) {
+struct RowTiles {
+    const LinearArgs &a;
+    const int lane;
+    int end, begin, n, first;   // this lane's expert of the 64 looked at last
+    int last = 0, tiles = 0;    // rows and tiles up to the end of those
+
+    __device__ RowTiles(const LinearArgs &args) : a(args), lane(threadIdx.x & 63) {}
+
+    __device__ void look(int base) {
         const int i = base + lane;
-        int end = i < a.experts ? a.ends[i] : 0;
-        end = max(min(end, a.rows), last);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(end, o, 64);
-            if (lane >= o) end = max(end, u);
-        }
-        int begin = __shfl_up(end, 1, 64);
+        end = i < a.experts ? a.ends[i] : 0;
+        end = wave_scan(max(min(end, a.rows), last), [](int x, int y) { return max(x, y); });
+        begin = __builtin_amdgcn_update_dpp(0, end, 0x138, 0xF, 0xF, false);   // wave_shr 1
         if (lane == 0) begin = last;
-        const int n = (end - begin + BM - 1) / BM;
-        int c = n;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(c, o, 64);
-            if (lane >= o) c += u;
-        }
-        const int first = tiles + c - n;
-        const uint64_t hit = __ballot(t >= first && t < first + n);
-        if (hit) {
-            const int l = __builtin_ctzll(hit);
-            r.expert = base + l;
-            r.row0 = __builtin_amdgcn_readlane(begin, l) + (t - __builtin_amdgcn_readlane(first, l)) * BM;
-            r.end = __builtin_amdgcn_readlane(end, l);
-            return true;
-        }
+        n = (end - begin + BM - 1) / BM;
+        const int c = wave_scan(n, [](int x, int y) { return x + y; });
+        first = tiles + c - n;
         last = __builtin_amdgcn_readlane(end, 63);
         tiles += __builtin_amdgcn_readlane(c, 63);
     }
-    r = {-1, last + (t - tiles) * BM, a.rows};
-    return r.row0 < a.rows;
-}
+
+    // All the row tiles.
+    __device__ int total() {
+        if (!a.ends) return (a.rows + BM - 1) / BM;
+        for (int base = 0; base < a.experts; base += 64) look(base);
+        return tiles + (a.rows - last + BM - 1) / BM;
+    }
+
+    // Tile t < total(), after total().
+    __device__ RowTile find(int t) {
+        if (!a.ends) return {0, t * BM, a.rows};
+        if (t >= tiles) return {-1, last + (t - tiles) * BM, a.rows};
+        const bool again = a.experts > 64;
+        if (again) last = tiles = 0;
+        for (int base = 0;; base += 64) {
+            if (again) look(base);
+            const uint64_t hit = __ballot(t >= first && t < first + n);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                return {base + l, __builtin_amdgcn_readlane(begin, l) + (t - __builtin_amdgcn_readlane(first, l)) * BM,
+                        __builtin_amdgcn_readlane(end, l)};
+            }
+        }
+    }
+};
 
 // Upper bound of the row tiles over any ends (host).
-int64_t row_tiles(const LinearArgs &a, int bm) {
+int64_t most_row_tiles(const LinearArgs &a, int bm) {
     const int64_t full = (a.rows + bm - 1) / bm;
     if (!a.ends) return full;
     // each group adds at most one part tile, and there are at most `rows` groups
@@ -158,8 +179,9 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
     const int per = WAVES / wk, groups = (a.cout + 16 * per - 1) / (16 * per);
     const int bid = blockIdx.y * gridDim.x + blockIdx.x;
     const int t = bid / groups, g0 = (bid - t * groups) * per;
-    RowTile r;
-    if (!row_tile<16 * MT>(a, t, r)) return;
+    RowTiles<16 * MT> tiles(a);
+    if (t >= tiles.total()) return;
+    const RowTile r = tiles.find(t);
     const int rows = min(r.end - r.row0, 16 * MT);
     if (r.expert < 0) return zero_tile(a, r.row0, rows, g0 * 16, 16 * per);
 
@@ -363,26 +385,31 @@ __device__ __forceinline__ TileIndex tile_index(int bid, int tiles_m, int tiles_
     return {band * 8 + in - tn * high, tn};
 }
 
-// Stores 32 rows of COLS outputs, fp32 in a wave's LDS rows of COLS + 4, to y: lanes take
-// 16-byte pieces, so a store instruction writes whole runs of rows.
-template <typename T, int COLS>
-__device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0, int rows, int c0, int lane) {
+// Stores 32 rows of COLS outputs, fp32 in LDS rows of COLS + 4, to y: lanes take 16-byte
+// pieces, so a store instruction writes whole runs of rows.  PARTS waves share the rows.
+template <typename T, int COLS, int PARTS>
+__device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0, int rows, int c0, int lane, int part) {
     constexpr int E = 16 / sizeof(T), PER = COLS / E;   // elements of a piece, pieces of a row
+    if (c0 >= a.cout) return;
     T *y = static_cast<T *>(a.y);
     const bool vec = (reinterpret_cast<uintptr_t>(y) & 15) == 0 && (a.y_stride & (E - 1)) == 0;
-    if (vec && c0 + COLS <= a.cout) {
 #pragma unroll
-        for (int u = 0; u < 32 * PER / 64; ++u) {
-            const int r = (u * 64 + lane) / PER, c = lane % PER * E;
-            float z[E];
+    for (int k = 0; k < (32 * PER / 64 + PARTS - 1) / PARTS; ++k) {
+        const int u = k * PARTS + part;
+        if (u >= 32 * PER / 64) break;
+        const int r = (u * 64 + lane) / PER, c = lane % PER * E;
+        float z[E];
 #pragma unroll
-            for (int k = 0; k < E; k += 4) *reinterpret_cast<float4 *>(z + k) = *reinterpret_cast<const float4 *>(from + r * (COLS + 4) + c + k);
-            if (r < rows) store16(y + (row0 + r) * a.y_stride + c0 + c, z);
-        }
-    } else {
-        for (int u = lane; u < 32 * COLS; u += 64) {
-            const int r = u / COLS, c = u % COLS;
-            if (r < rows && c0 + c < a.cout) y[(row0 + r) * a.y_stride + c0 + c] = from_float<T>(from[r * (COLS + 4) + c]);
+        for (int e = 0; e < E; e += 4)
+            *reinterpret_cast<float4 *>(z + e) = *reinterpret_cast<const float4 *>(from + r * (COLS + 4) + c + e);
+        if (r >= rows) continue;
+        T *to = y + (row0 + r) * a.y_stride + c0 + c;
+        if (vec && c0 + c + E <= a.cout) {
+            store16(to, z);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (c0 + c + e < a.cout) to[e] = from_float<T>(z[e]);
         }
     }
 }
@@ -397,29 +424,37 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
 // cores, and the one barrier of a step stands between its halves: the reads of a
 // buffer end before it, the loads that refill that buffer and the reads of the next
 // one begin after it.
-template <int WM, int WN, int FM, int FN, int STAGES, int G>
-__global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearArgs a) {
+//
+// Few tiles: KG such groups of waves share a tile, each a run of the contraction with a
+// ring of its own, and add up in LDS.  A step costs a group about 0.17 us of LDS and
+// barrier latency however few MFMAs it has; the groups of a CU overlap it.
+template <int WM, int WN, int FM, int FN, int STAGES, int KG, int G>
+__global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const LinearArgs a) {
     constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
     constexpr int A_INSTR = BM / 16 / NW, B_INSTR = BN / 16 / NW, PER_STAGE = A_INSTR + B_INSTR;
     constexpr int STAGE_BYTES = (BM + BN) * 64;
     constexpr int COLS = FN / G * 32;   // outputs of a wave's row
     static_assert(A_INSTR * NW * 16 == BM && B_INSTR * NW * 16 == BN && FN % G == 0, "tile");
-    static_assert(NW * 32 * (COLS + 4) * 4 <= STAGES * STAGE_BYTES, "output staging");
+    constexpr int RING = STAGES * STAGE_BYTES;
+    static_assert(NW * 32 * (COLS + 4) * 4 <= KG * RING, "output staging");
+    static_assert(KG == 1 || (4 % KG == 0 && KG * NW * FM * FN * 4096 <= KG * RING), "partial sums");
     static_assert(BN / 4 <= 64 * NW, "column factors");
     // the ring, then the columns' scales and biases, [2][BN] floats.  (One array: with a
     // second LDS object the compiler waits for every load under way before each read.)
-    __shared__ __attribute__((aligned(1024))) int8_t lds[STAGES * STAGE_BYTES + 8 * BN];
-    float4 *factor = reinterpret_cast<float4 *>(lds + STAGES * STAGE_BYTES);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / WN, wn = wave % WN;
+    __shared__ __attribute__((aligned(1024))) int8_t lds[KG * RING + 8 * BN];
+    float4 *factor = reinterpret_cast<float4 *>(lds + KG * RING);
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kg = all / NW, wave = all % NW, wm = wave / WN, wn = wave % WN;
+    int8_t *ring = lds + kg * RING;
 
     const int tiles_n = (a.cout_pad + BN - 1) / BN;
     const int bid = blockIdx.y * gridDim.x + blockIdx.x;
-    if (bid >= a.tiles_m * tiles_n) return;
-    const TileIndex ti = tile_index(bid, a.tiles_m, tiles_n);
+    RowTiles<BM> row_tiles(a);
+    const int tiles_m = row_tiles.total();
+    if (bid >= tiles_m * tiles_n) return;
+    const TileIndex ti = tile_index(bid, tiles_m, tiles_n);
     const int tn = ti.tn;
-    RowTile r;
-    if (!row_tile<BM>(a, ti.t, r)) return;
+    const RowTile r = row_tiles.find(ti.t);
     const int rows = min(r.end - r.row0, BM);
     if (r.expert < 0) return zero_tile(a, r.row0, rows, tn * BN / G, BN / G);
 
@@ -434,18 +469,20 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
         const int tok = token_of(a, r.row0 + min((wm * FM + i) * 32 + (lane & 31), rows - 1));
         scale[i] = tok < 0 ? 0.0f : a.sx[tok];
     }
-    const int nks = a.k_stride >> 6;
+    // this group's steps: `nks` of them from k0, in a loop of `turns` for every group
+    const int steps = a.k_stride >> 6, turns = (steps + KG - 1) / KG;
+    const int k0 = min(kg * turns, steps - 1), nks = max(min(steps - kg * turns, turns), 0);
     const int8_t *pa[A_INSTR], *pb[B_INSTR];
 #pragma unroll
     for (int j = 0; j < A_INSTR; ++j) {
         const int m = 16 * (wave + NW * j) + (lane >> 2);
         const int tok = token_of(a, r.row0 + min(m, rows - 1));
-        pa[j] = a.xq + (int64_t)max(tok, 0) * a.k_stride + 16 * ((lane & 3) ^ ((m >> 2) & 3));
+        pa[j] = a.xq + (int64_t)max(tok, 0) * a.k_stride + k0 * 64 + 16 * ((lane & 3) ^ ((m >> 2) & 3));
     }
 #pragma unroll
     for (int j = 0; j < B_INSTR; ++j) {
         const int block = min(tn * (BN / 16) + wave + NW * j, a.cout_pad / 16 - 1);
-        pb[j] = a.wp + ((int64_t)r.expert * a.cout_pad + block * 16) * a.k_stride + lane * 16;
+        pb[j] = a.wp + ((int64_t)r.expert * a.cout_pad + block * 16) * a.k_stride + k0 * 1024 + lane * 16;
     }
     // Loads the step that the pointers are at into a buffer; `more`: go on to the next.
     // (Past the last step the last one is loaded again, so that every step has the same
@@ -497,44 +534,72 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
     };
 
 #pragma unroll
-    for (int k = 0; k < STAGES; ++k) issue(lds + k * STAGE_BYTES, k + 1 < nks);
+    for (int k = 0; k < STAGES; ++k) issue(ring + k * STAGE_BYTES, k + 1 < nks);
     wait_vmcnt_lds<(STAGES - 1) * PER_STAGE>();
     __builtin_amdgcn_s_barrier();
 #pragma unroll
-    for (int k = 0; k < FM + FN; ++k) read(lds, 0, k);
+    for (int k = 0; k < FM + FN; ++k) read(ring, 0, k);
     int at = 0;   // this step's buffer
-    for (int ks = 0; ks < nks; ++ks) {
-        int8_t *now = lds + at;
-        at = at + STAGE_BYTES == STAGES * STAGE_BYTES ? 0 : at + STAGE_BYTES;
-        half(0, now);
+    for (int ks = 0; ks < turns; ++ks) {
+        int8_t *now = ring + at;
+        at = at + STAGE_BYTES == RING ? 0 : at + STAGE_BYTES;
+        if (KG == 1 || ks < nks) half(0, now);
         // the next step's loads have landed (STAGES - 2 later ones under way), this buffer
         // has been read: by every wave, past the barrier
         wait_vmcnt_lds<(STAGES - 2) * PER_STAGE>();
         __builtin_amdgcn_s_barrier();
         issue(now, ks + STAGES + 1 < nks);
-        half(1, lds + at);
+        if (KG == 1 || ks < nks) half(1, ring + at);
     }
     wait_vmcnt_lds<0>();
     __builtin_amdgcn_s_barrier();   // no load is under way into the buffers that stage the outputs
+
+    if constexpr (KG > 1) {
+        // partial sums [KG][NW][FN][FM][4][64]; group kg adds up the quads q = kg mod KG
+        v4i *part = reinterpret_cast<v4i *>(lds);
+        auto quad = [&](int k, int j, int i, int q) { return part + ((((k * NW + wave) * FN + j) * FM + i) * 4 + q) * 64 + lane; };
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *quad(kg, j, i, q) = v4i{acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]};
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int u = 0; u < 4 / KG; ++u) {
+                    // (the sum of quad u KG + kg goes to the registers of quad u)
+                    v4i sum = *quad(0, j, i, u * KG + kg);
+#pragma unroll
+                    for (int k = 1; k < KG; ++k) sum += *quad(k, j, i, u * KG + kg);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[j][i][4 * u + e] = sum[e];
+                }
+        __syncthreads();
+    }
 
     float *mine = reinterpret_cast<float *>(lds) + wave * 32 * (COLS + 4);
     const int c0 = (tn * BN + wn * FN * 32) / G;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-        const int first = (wm * FM + i) * 32;
-        if (first >= rows) break;
+        const int first = (wm * FM + i) * 32, n = min(rows - first, 32);
+        if (KG == 1 && n <= 0) break;
 #pragma unroll
         for (int j = 0; j < FN; j += G)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int u = 0; u < 4 / KG; ++u) {
                 // element 0's column: rows 8 q + 4 (lane / 32) of the 32 x 32 tile
-                const int in = 8 * q + 4 * (lane >> 5);
+                const int in = 8 * (u * KG + kg) + 4 * (lane >> 5);
                 const float4 *f = factor + ((wn * FN + j) * 32 + in) / 4;
                 float z[2][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    const int v[4] = {acc[j + g][i][4 * q], acc[j + g][i][4 * q + 1], acc[j + g][i][4 * q + 2],
-                                      acc[j + g][i][4 * q + 3]};
+                    const int v[4] = {acc[j + g][i][4 * u], acc[j + g][i][4 * u + 1], acc[j + g][i][4 * u + 2],
+                                      acc[j + g][i][4 * u + 3]};
                     dequant4(a, reinterpret_cast<const float *>(f + 8 * g), reinterpret_cast<const float *>(f + BN / 4 + 8 * g), v,
                              scale[i], z[g]);
                 }
@@ -545,18 +610,19 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(const LinearA
                 *reinterpret_cast<float4 *>(mine + (lane & 31) * (COLS + 4) + j / G * 32 + in) =
                     make_float4(z[0][0], z[0][1], z[0][2], z[0][3]);
             }
-        // (a wave's LDS accesses are in order: its rows are whole when it reads them)
-        const int n = min(rows - first, 32);
-        if (a.y_type == kBf16) store_rows<bf16_t, COLS>(a, mine, r.row0 + first, n, c0, lane);
-        else if (a.y_type == kF16) store_rows<_Float16, COLS>(a, mine, r.row0 + first, n, c0, lane);
-        else store_rows<float, COLS>(a, mine, r.row0 + first, n, c0, lane);
+        // (one group: a wave's LDS accesses are in order, so its rows are whole when it reads them)
+        if (KG > 1) __syncthreads();
+        if (a.y_type == kBf16) store_rows<bf16_t, COLS, KG>(a, mine, r.row0 + first, n, c0, lane, kg);
+        else if (a.y_type == kF16) store_rows<_Float16, COLS, KG>(a, mine, r.row0 + first, n, c0, lane, kg);
+        else store_rows<float, COLS, KG>(a, mine, r.row0 + first, n, c0, lane, kg);
+        if (KG > 1 && i + 1 < FM) __syncthreads();
     }
 }
 
 template <int MT, int U>
 void stream(const LinearArgs &a, hipStream_t st, int wk) {
     const int cols = 16 * 8 / wk;
-    const dim3 grid = grid_of(row_tiles(a, 16 * MT) * ((a.cout + cols - 1) / cols));
+    const dim3 grid = grid_of(most_row_tiles(a, 16 * MT) * ((a.cout + cols - 1) / cols));
     if (a.gated) linear_stream_kernel<MT, 2, U><<<grid, 512, 0, st>>>(a, wk);
     else linear_stream_kernel<MT, 1, U><<<grid, 512, 0, st>>>(a, wk);
 }
@@ -578,14 +644,12 @@ void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     else token<T, 4, 8>(a, x, st);
 }
 
-template <int WM, int WN, int FM, int FN, int STAGES>
-void tile(const LinearArgs &b, hipStream_t st) {
+template <int WM, int WN, int FM, int FN, int STAGES, int KG = 1>
+void tile(const LinearArgs &a, hipStream_t st) {
     constexpr int BM = WM * FM * 32, BN = WN * FN * 32;
-    LinearArgs a = b;
-    a.tiles_m = (int32_t)row_tiles(a, BM);
-    const dim3 grid = grid_of((int64_t)a.tiles_m * ((a.cout_pad + BN - 1) / BN));
-    if (a.gated) linear_tile_kernel<WM, WN, FM, FN, STAGES, 2><<<grid, 64 * WM * WN, 0, st>>>(a);
-    else linear_tile_kernel<WM, WN, FM, FN, STAGES, 1><<<grid, 64 * WM * WN, 0, st>>>(a);
+    const dim3 grid = grid_of(most_row_tiles(a, BM) * ((a.cout_pad + BN - 1) / BN));
+    if (a.gated) linear_tile_kernel<WM, WN, FM, FN, STAGES, KG, 2><<<grid, 64 * WM * WN * KG, 0, st>>>(a);
+    else linear_tile_kernel<WM, WN, FM, FN, STAGES, KG, 1><<<grid, 64 * WM * WN * KG, 0, st>>>(a);
 }
 
 }  // namespace
@@ -601,16 +665,85 @@ hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStre
     return hipGetLastError();
 }
 
+// ---- which kernel ------------------------------------------------------------------------
+// Estimates in microseconds, fitted to measurements of all the kernels over 320 to 16384
+// contractions and outputs, 16 to 6144 rows, 1 to 64 experts (MI355X).  `tiles` stands for
+// the row tiles that are met: groups fill half of their last tile on average.
+struct TileCost {
+    int bm, bn;
+    double fixed, step;   // of a launch; a step of 64 bytes of the contraction, latency
+    int slots;            // tiles that the card holds at once
+    double rate;          // TOP/s with the card full
+};
+constexpr TileCost kTiles[] = {
+    {64, 64, 4.5, 0.085, 256, 1000.0},   // four groups of waves over the contraction
+    {64, 128, 4.0, 0.15, 1024, 1450.0},
+    {128, 128, 4.0, 0.19, 768, 1850.0},
+    {128, 256, 6.0, 0.30, 512, 2050.0},
+    {256, 256, 6.0, 0.56, 256, 2120.0},
+};
+constexpr double kWeightRate = 6.5e6, kRowRate = 7.3e6;   // bytes a microsecond: memory, codes from the L2s
+constexpr double kTileRate = 4.0e4;                       // and what one tile's CU takes of the weights
+
+double met_tiles(const LinearArgs &a, int bm) {
+    if (!a.ends) return (a.rows + bm - 1) / bm;
+    const double groups = a.experts < a.rows ? a.experts : a.rows, t = (double)a.rows / bm + 0.5 * groups;
+    return t > groups ? t : groups;
+}
+
+double weight_time(const LinearArgs &a, double tiles) {
+    const double groups = a.ends && a.experts < a.rows ? a.experts : a.ends ? a.rows : 1;
+    return groups * a.cout_pad * a.k_stride / (tiles * kTileRate < kWeightRate ? tiles * kTileRate : kWeightRate);
+}
+
+// The stream kernel reads the rows' codes again for every 16 channels.
+double stream_cost(const LinearArgs &a, int bm) {
+    const double rows = met_tiles(a, bm) * bm * (double)a.k_stride * (a.cout_pad / 16) / kRowRate, w = weight_time(a, 1e9);
+    return 3.0 + (rows > w ? rows : w);
+}
+
+double tile_cost(const LinearArgs &a, const TileCost &c) {
+    const double tiles = met_tiles(a, c.bm) * ((a.cout_pad + c.bn - 1) / c.bn), steps = a.k_stride / 64;
+    // one layer's tiles are alike: the last ones of a full card run by themselves
+    const double whole = a.ends || tiles <= 256.0 ? tiles : 256.0 * (double)((int64_t)(tiles + 255.0) / 256);
+    double t = whole * c.bm * c.bn * a.k_stride * 2e-6 / c.rate;
+    // (where a CU holds one tile, the start and the end of one are not hidden by another)
+    const double rounds = 1 + (int64_t)((tiles - 1.0) / c.slots), w = weight_time(a, tiles);
+    const double latency = rounds * steps * c.step + (c.slots == 256 ? (rounds - 1) * c.fixed : 0.0);
+    if (latency > t) t = latency;
+    if (w > t) t = w;
+    return c.fixed + t;
+}
+
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st) {
-    // rows a group has on average
-    const int64_t per = a.ends ? (a.rows + a.experts - 1) / a.experts : a.rows;
-    if (per <= 16) stream<1, 8>(a, st, 8);
-    else if (per <= 32) stream<2, 4>(a, st, 8);
-    else if (per <= 64) stream<4, 4>(a, st, 8);
-    else {
-        const int64_t big = row_tiles(a, 256) * ((a.cout_pad + 255) / 256);
-        if (big >= 256) tile<2, 4, 4, 2, 4>(a, st);
-        else tile<2, 2, 2, 2, 4>(a, st);
+    int best = -1;
+    double cost = stream_cost(a, 16);
+    // (a long call never streams; the products of large sizes stay far inside a double)
+    if (met_tiles(a, 16) * 16 > 4096 + 16.0 * a.experts) cost = 1e300;
+    for (int i = 0; i < 5; ++i) {
+        const double c = tile_cost(a, kTiles[i]);
+        if (c < cost) {
+            cost = c;
+            best = i;
+        }
+    }
+    switch (best) {
+        case 0: tile<2, 1, 1, 2, 3, 4>(a, st); break;
+        case 1: tile<2, 2, 1, 2, 3>(a, st); break;
+        case 2: tile<2, 2, 2, 2, 3>(a, st); break;
+        case 3: tile<2, 4, 2, 2, 3>(a, st); break;
+        case 4: tile<2, 4, 4, 2, 4>(a, st); break;
+        default: {
+            // Waves on a group of channels.  One layer: all eight (4096 x 4096, 16 rows: 6.3 us,
+            // two 12.1).  Experts: runs of eight steps a wave or a little less (64 experts of 2048
+            // -> 1024, 384 rows: 4 waves 24.7 us, 8 28.5, 2 25.2; 32 of 512 -> 1024, 96 rows: 2
+            // waves 5.5, 4 6.5, 8 9.7).
+            const int steps = a.k_stride >> 6, wk = !a.ends ? 8 : steps >= 16 ? 4 : 2;
+            // Tiles of 32 rows where they fill the card (64 rows, 4096 x 4096: 11.9 us, 12.9 in
+            // tiles of 16; 8192 -> 1024: 11.4 and 8.0)
+            if (!a.ends && a.rows > 32 && (a.cout + 15) / 16 * ((a.rows + 31) / 32) >= 256) stream<2, 4>(a, st, wk);
+            else stream<1, 8>(a, st, wk);
+        }
     }
     return hipGetLastError();
 }
