@@ -520,9 +520,12 @@ int32_t hatq_linear_int8(const hatq_linear_weights *W, const int8_t *xq, const f
                          void *y, int32_t y_type, int64_t y_stride, void *stream);
 
 /* The whole layer, floats in: hatq_token_quant into the workspace, then
- * hatq_linear_int8 (for a few tokens one kernel that does both, with the same
- * result).  ws: device memory, 256-byte aligned, of at least
- * hatq_linear_ws_bytes(W, rows) bytes. */
+ * hatq_linear_int8, or for a few tokens (rows <= HATQ_TOKEN_ROWS and rows
+ * k_stride <= HATQ_TOKEN_CODES) one kernel that does both, with the same result.
+ * ws: device memory, 256-byte aligned, of at least hatq_linear_ws_bytes(W, rows)
+ * bytes; for a few tokens it is not used and may be NULL. */
+#define HATQ_TOKEN_ROWS 16
+#define HATQ_TOKEN_CODES 16384
 size_t hatq_linear_ws_bytes(const hatq_linear_weights *W, int32_t rows);
 int32_t hatq_linear_forward(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t rows,
                             int64_t x_stride, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,

@@ -58,9 +58,8 @@ struct LinearArgs {
 };
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
 
-// The product of tokens that its own blocks quantize (xq and sx unused; x.rows = x_rows),
-// for calls that have few elements to quantize a row tile.
-bool linear_takes_tokens(const LinearArgs &a);
+// One layer's product of at most 16 rows and 16384 codes that its own blocks quantize (xq
+// and sx unused, no ends).
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st);
 
 struct OrderArgs {

@@ -32,22 +32,6 @@ struct RowTile {
     int row0, end;  // rows [row0, min(row0 + BM, end))
 };
 
-// Inclusive scans over the wave, of values >= 0, by DPP moves: rows of 16 lanes, then
-// lane 15 of each row to the next row, then lane 31 to the upper half.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_or_0(int v) {
-    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
-}
-template <typename F>
-__device__ __forceinline__ int wave_scan(int v, F f) {
-    v = f(v, dpp_or_0<0x111, 0xF>(v));   // row_shr 1, 2, 4, 8
-    v = f(v, dpp_or_0<0x112, 0xF>(v));
-    v = f(v, dpp_or_0<0x114, 0xF>(v));
-    v = f(v, dpp_or_0<0x118, 0xF>(v));
-    v = f(v, dpp_or_0<0x142, 0xA>(v));   // row_bcast 15
-    return f(v, dpp_or_0<0x143, 0xC>(v));   // row_bcast 31
-}
-
 // Row tiles of BM rows, each expert's rows starting a tile of their own, and the rows
 // past the last end after them.  Every lane of the wave takes part, 64 experts at a
 // time; the ends are clamped here, so any contents give rows in [0, rows).
@@ -653,10 +637,6 @@ void tile(const LinearArgs &a, hipStream_t st) {
 }
 
 }  // namespace
-
-bool linear_takes_tokens(const LinearArgs &a) {
-    return !a.ends && a.rows <= 16 && (int64_t)a.rows * a.k_stride <= 16384;
-}
 
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     if (x.x_type == kF32) token<float>(a, x, st);

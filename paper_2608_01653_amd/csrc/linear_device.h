@@ -82,6 +82,22 @@ __device__ __forceinline__ void store16(_Float16 *p, const float *v) {
     *reinterpret_cast<v8h *>(p) = h;
 }
 
+// Inclusive scans over the wave, of values >= 0, by DPP moves: rows of 16 lanes, then
+// lane 15 of each row to the next row, then lane 31 to the upper half.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_0(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+template <typename F>
+__device__ __forceinline__ int wave_scan(int v, F f) {
+    v = f(v, dpp_or_0<0x111, 0xF>(v));   // row_shr 1, 2, 4, 8
+    v = f(v, dpp_or_0<0x112, 0xF>(v));
+    v = f(v, dpp_or_0<0x114, 0xF>(v));
+    v = f(v, dpp_or_0<0x118, 0xF>(v));
+    v = f(v, dpp_or_0<0x142, 0xA>(v));   // row_bcast 15
+    return f(v, dpp_or_0<0x143, 0xC>(v));   // row_bcast 31
+}
+
 // ---- token codes --------------------------------------------------------------------
 // A lane holds chunks of 8 adjacent elements, neighbouring lanes neighbouring chunks:
 // index bits 0-2 are registers, bits 3-6 lanes of one 16-lane row, so the butterflies of

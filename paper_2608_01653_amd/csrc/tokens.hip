@@ -98,28 +98,22 @@ __global__ void __launch_bounds__(kThreads) linear_prepare_kernel(const LinearPr
     const int held = a.gated ? 2 * a.cout : a.cout;
     const int ch = held_channel(a, p);
     const int64_t row = (int64_t)e * held + ch;
-    const T *w = ch >= 0 && !a.codes ? static_cast<const T *>(a.w) + row * a.cin : nullptr;
+    const T *w = static_cast<const T *>(a.w) + row * a.cin;
     float s = 0.0f;
     if (ch >= 0) {
-        if (a.codes) {
-            s = a.scale_in[row];
-        } else {
-            float m = 0.0f;
-            for (int d = threadIdx.x; d < a.cin; d += kThreads)
-                m = fmaxf(m, fabsf((float)transformed(w, d, a.hblock)));
-            m = wave_max(m);
-            __shared__ float red[kThreads / 64];
-            if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-            __syncthreads();
-            s = act_scale_from_absmax(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-        }
+        float m = 0.0f;
+        for (int d = threadIdx.x; d < a.cin; d += kThreads)
+            m = fmaxf(m, fabsf((float)transformed(w, d, a.hblock)));
+        m = wave_max(m);
+        __shared__ float red[kThreads / 64];
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+        __syncthreads();
+        s = act_scale_from_absmax(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
     }
     int8_t *out = a.wpack + ((int64_t)e * a.cout_pad + (p & ~15)) * a.k_stride + (p & 15) * 16;
     for (int d = threadIdx.x; d < a.k_stride; d += kThreads) {
         int8_t q = 0;
-        if (ch >= 0 && d < a.cin)
-            q = a.codes ? a.codes[row * a.cin + d]
-                        : (int8_t)(int)rintf(clamp127((float)transformed(w, d, a.hblock) / s));
+        if (ch >= 0 && d < a.cin) q = (int8_t)(int)rintf(clamp127((float)transformed(w, d, a.hblock) / s));
         out[(int64_t)(d >> 6) * 1024 + ((d >> 4) & 3) * 256 + (d & 15)] = q;
     }
     if (threadIdx.x == 0) {
@@ -128,133 +122,189 @@ __global__ void __launch_bounds__(kThreads) linear_prepare_kernel(const LinearPr
     }
 }
 
+// Codes that are there already, 16 of a column at a time.
+__global__ void __launch_bounds__(kThreads) linear_pack_kernel(const LinearPrepArgs a) {
+    const int p = blockIdx.x, e = blockIdx.y, ch = held_channel(a, p);
+    const int64_t row = (int64_t)e * (a.gated ? 2 * a.cout : a.cout) + ch;
+    const int8_t *from = a.codes + row * a.cin;
+    const bool whole = (reinterpret_cast<uintptr_t>(a.codes) & 15) == 0 && a.cin % 16 == 0;
+    int8_t *out = a.wpack + ((int64_t)e * a.cout_pad + (p & ~15)) * a.k_stride + (p & 15) * 16;
+    for (int c = threadIdx.x; c < a.k_stride >> 4; c += kThreads) {
+        v4i q = {0, 0, 0, 0};
+        if (ch >= 0) {
+            if (whole) {
+                if (c * 16 < a.cin) q = *reinterpret_cast<const v4i *>(from + c * 16);
+            } else {
+                int8_t *b = reinterpret_cast<int8_t *>(&q);
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (c * 16 + j < a.cin) b[j] = from[c * 16 + j];
+            }
+        }
+        *reinterpret_cast<v4i *>(out + (int64_t)(c >> 2) * 1024 + (c & 3) * 256) = q;
+    }
+    if (threadIdx.x == 0) {
+        a.w_scale[(int64_t)e * a.cout_pad + p] = ch >= 0 ? a.scale_in[row] : 0.0f;
+        a.bias[(int64_t)e * a.cout_pad + p] = ch >= 0 && a.bias_in ? a.bias_in[row] : 0.0f;
+    }
+}
+
 // ---- the order of expert rows -----------------------------------------------------
-// A stable counting sort of `pairs` ids.  Block b owns a contiguous segment, wave w
-// of it a contiguous part: counts per wave in LDS, a block's first row of expert e =
-// rows of the experts before + rows of e in the blocks before, then each wave ranks
-// its pairs 64 at a time in order.  Ranks come from ballots, not from atomics, so
-// equal ids keep their order.
-constexpr int kOrderWaves = 4;
+// A stable counting sort of `pairs` ids.  Block b owns a contiguous segment, wave w of it
+// a contiguous part.  The first row of expert e in block b is the rows of the experts
+// before e plus the rows of e in the blocks before b; each wave then ranks its pairs 64
+// at a time in order.  Ranks come from ballots, not from atomics, so equal ids keep
+// their order.  Up to kOrderOne pairs every block counts all of them itself (one launch;
+// 16384 pairs of 32 experts: 18.1 us with a launch for the counts before); beyond, a
+// first launch leaves the blocks' counts in a table.
+constexpr int kOrderWaves = 8;
+constexpr int kOrderThreads = 64 * kOrderWaves;
 constexpr int kOrderBlocks = 256;
 constexpr int kOrderSegment = 1024;   // pairs of a block, more when that would take over kOrderBlocks
+constexpr int kOrderOne = 32768;
 
 __host__ __device__ __forceinline__ int64_t order_segment(int64_t pairs) {
     const int64_t per = (pairs + kOrderBlocks - 1) / kOrderBlocks;
     const int64_t seg = per > kOrderSegment ? per : kOrderSegment;
-    return (seg + 255) / 256 * 256;
+    return (seg + kOrderThreads - 1) / kOrderThreads * kOrderThreads;
 }
 
-struct WaveSpan {
+// f(first index, ids) over [begin, end) by `step` threads, this one the t-th, N ids of a
+// thread loaded at once; -1 past the end.
+template <int N, typename F>
+__device__ __forceinline__ void order_ids(const int32_t *ids, int64_t begin, int64_t end, int t, int step, F f) {
+    for (int64_t b = begin; b < end; b += step * N) {
+        int id[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int64_t i = b + k * step + t;
+            id[k] = i < end ? ids[i] : -1;
+        }
+        f(b + t, id);
+    }
+}
+
+struct Span {
     int64_t begin, end;
 };
-__device__ __forceinline__ WaveSpan order_span(int64_t pairs, int block, int wave) {
+__device__ __forceinline__ Span order_span(int64_t pairs, int block, int wave) {
     const int64_t seg = order_segment(pairs), part = seg / kOrderWaves;
-    const int64_t b = block * seg + wave * part;
-    const int64_t e = b + part;
+    const int64_t b = block * seg + wave * part, e = b + part;
     return {b < pairs ? b : pairs, e < pairs ? e : pairs};
 }
 
-// counts[w][e] of this block's waves.
-__device__ void order_counts(const OrderArgs &a, int64_t pairs, int *counts) {
-    for (int i = threadIdx.x; i < kOrderWaves * a.experts; i += kThreads) counts[i] = 0;
-    __syncthreads();
+// counts[w][e] of this block's waves (zeroed, and a barrier on both sides).
+__device__ __forceinline__ void order_counts(const OrderArgs &a, int64_t pairs, int *counts) {
     const int w = threadIdx.x >> 6;
-    const WaveSpan s = order_span(pairs, blockIdx.x, w);
-    for (int64_t i = s.begin + (threadIdx.x & 63); i < s.end; i += 64) {
-        const int id = a.ids[i];
-        if ((unsigned)id < (unsigned)a.experts) atomicAdd(&counts[w * a.experts + id], 1);
-    }
-    __syncthreads();
+    const Span s = order_span(pairs, blockIdx.x, w);
+    order_ids<2>(a.ids, s.begin, s.end, threadIdx.x & 63, 64, [&](int64_t, const int *id) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if ((unsigned)id[k] < (unsigned)a.experts) atomicAdd(&counts[w * a.experts + id[k]], 1);
+    });
 }
 
-__global__ void __launch_bounds__(kThreads) order_count_kernel(const OrderArgs a) {
+__global__ void __launch_bounds__(kOrderThreads) order_count_kernel(const OrderArgs a) {
     extern __shared__ int lds[];
+    for (int i = threadIdx.x; i < kOrderWaves * a.experts; i += kOrderThreads) lds[i] = 0;
+    __syncthreads();
     order_counts(a, (int64_t)a.tokens * a.topk, lds);
-    for (int e = threadIdx.x; e < a.experts; e += kThreads) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.experts; e += kOrderThreads) {
         int n = 0;
         for (int w = 0; w < kOrderWaves; ++w) n += lds[w * a.experts + e];
         a.ws[(int64_t)blockIdx.x * a.experts + e] = n;
     }
 }
 
-// Several blocks read the table of order_count_kernel; one block (ws unused) has
-// every pair itself.
-__global__ void __launch_bounds__(kThreads) order_place_kernel(const OrderArgs a) {
-    extern __shared__ int lds[];   // counts [waves][experts], then ends [experts]
+template <bool TABLE>
+__global__ void __launch_bounds__(kOrderThreads) order_place_kernel(const OrderArgs a) {
+    extern __shared__ int lds[];   // [experts] rows in all blocks, in the blocks before; counts [waves][experts]
+    const int E = a.experts;
+    int *total = lds, *before = lds + E, *counts = lds + 2 * E;
     const int64_t pairs = (int64_t)a.tokens * a.topk;
-    int *counts = lds, *ends = lds + kOrderWaves * a.experts;
+    for (int i = threadIdx.x; i < (2 + kOrderWaves) * E; i += kOrderThreads) lds[i] = 0;
+    __syncthreads();
     order_counts(a, pairs, counts);
-    // rows of each expert in all blocks, and in those before this one
-    constexpr int PER = kMaxExperts / kThreads;
-    int total[PER], before[PER];
+    if (TABLE) {
+        for (int i = threadIdx.x; i < (int)gridDim.x * E; i += kOrderThreads) {
+            const int b = i / E, e = i - b * E, n = a.ws[i];
+            atomicAdd(&total[e], n);
+            if (b < (int)blockIdx.x) atomicAdd(&before[e], n);
+        }
+    } else {
+        const int64_t mine = blockIdx.x * order_segment(pairs);
+        order_ids<16>(a.ids, 0, mine, threadIdx.x, kOrderThreads, [&](int64_t, const int *id) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if ((unsigned)id[k] < (unsigned)E) atomicAdd(&before[id[k]], 1);
+        });
+        order_ids<16>(a.ids, mine, pairs, threadIdx.x, kOrderThreads, [&](int64_t, const int *id) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                if ((unsigned)id[k] < (unsigned)E) atomicAdd(&total[id[k]], 1);
+        });
+    }
+    __syncthreads();
+    // exclusive scan over the block's threads, each with PER experts in a row
+    constexpr int PER = kMaxExperts / kOrderThreads;
+    int n[PER], sum = 0;
+#pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int e = threadIdx.x * PER + k;
-        total[k] = before[k] = 0;
-        if (e >= a.experts) continue;
-        if (gridDim.x == 1) {
-            for (int w = 0; w < kOrderWaves; ++w) total[k] += counts[w * a.experts + e];
-        } else {
-            for (int b = 0; b < (int)gridDim.x; ++b) {
-                const int n = a.ws[(int64_t)b * a.experts + e];
-                total[k] += n;
-                before[k] += b < (int)blockIdx.x ? n : 0;
-            }
-        }
+        n[k] = e < E ? total[e] + (TABLE ? 0 : before[e]) : 0;
+        sum += n[k];
     }
-    // exclusive scan over the block's threads, each with PER experts in a row
-    int sum = 0;
-    for (int k = 0; k < PER; ++k) sum += total[k];
-    int scan = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int u = __shfl_up(scan, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) scan += u;
-    }
+    const int scan = wave_scan(sum, [](int x, int y) { return x + y; });
     __shared__ int wave_sum[kOrderWaves];
     if ((threadIdx.x & 63) == 63) wave_sum[threadIdx.x >> 6] = scan;
     __syncthreads();
-    int first = scan - sum;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) first += wave_sum[w];
-    int all = 0;
-    for (int w = 0; w < kOrderWaves; ++w) all += wave_sum[w];
+    int first = scan - sum, all = 0;
+    for (int w = 0; w < kOrderWaves; ++w) {
+        if (w < (int)(threadIdx.x >> 6)) first += wave_sum[w];
+        all += wave_sum[w];
+    }
+#pragma unroll
     for (int k = 0; k < PER; ++k) {
         const int e = threadIdx.x * PER + k;
-        if (e >= a.experts) break;
+        if (e >= E) break;
         // the waves' first rows of this expert
-        int at = first + before[k];
+        int at = first + before[e];
         for (int w = 0; w < kOrderWaves; ++w) {
-            const int n = counts[w * a.experts + e];
-            counts[w * a.experts + e] = at;
-            at += n;
+            const int c = counts[w * E + e];
+            counts[w * E + e] = at;
+            at += c;
         }
-        first += total[k];
-        ends[e] = first;
+        first += n[k];
         if (blockIdx.x == 0) a.ends[e] = first;
     }
     __syncthreads();
     const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    volatile int *next = counts + w * a.experts;   // read and written by turns within the wave
-    const WaveSpan s = order_span(pairs, blockIdx.x, w);
-    for (int64_t b = s.begin; b < s.end; b += 64) {
-        const int64_t i = b + lane;
-        const int id = i < s.end ? a.ids[i] : -1;
-        const bool in = (unsigned)id < (unsigned)a.experts;
-        uint64_t same = __ballot(in);
+    volatile int *next = counts + w * E;   // read and written by turns within the wave
+    const Span s = order_span(pairs, blockIdx.x, w);
+    order_ids<2>(a.ids, s.begin, s.end, lane, 64, [&](int64_t i0, const int *ids) {
 #pragma unroll
-        for (int bit = 0; bit < 10; ++bit) {
-            const uint64_t set = __ballot((id >> bit) & 1);
-            same &= (id >> bit) & 1 ? set : ~set;
+        for (int k = 0; k < 2; ++k) {
+            const int id = ids[k];
+            const int64_t i = i0 + k * 64;
+            const bool in = (unsigned)id < (unsigned)E;
+            uint64_t same = __ballot(in);
+#pragma unroll
+            for (int bit = 0; bit < 10; ++bit) {
+                const uint64_t set = __ballot((id >> bit) & 1);
+                same &= (id >> bit) & 1 ? set : ~set;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            int row = -1;
+            if (in) row = next[id] + rank;
+            __builtin_amdgcn_wave_barrier();   // every lane has read before the last of each id writes
+            if (in && rank + 1 == __popcll(same)) next[id] = row + 1;
+            __builtin_amdgcn_wave_barrier();
+            if (in) a.src[row] = (int)((unsigned)i / (unsigned)a.topk);
+            if (i < s.end) a.pos[i] = row;
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        int row = -1;
-        if (in) row = next[id] + rank;
-        __builtin_amdgcn_wave_barrier();   // every lane has read before the last of each id writes
-        if (in && rank + 1 == __popcll(same)) next[id] = row + 1;
-        __builtin_amdgcn_wave_barrier();
-        if (in) a.src[row] = (int)(i / a.topk);
-        if (i < s.end) a.pos[i] = row;
-    }
-    for (int64_t i = all + (int64_t)blockIdx.x * kThreads + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * kThreads)
+    });
+    for (int64_t i = all + (int64_t)blockIdx.x * kOrderThreads + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * kOrderThreads)
         a.src[i] = -1;
 }
 
@@ -316,7 +366,8 @@ hipError_t launch_token_quant(const TokenArgs &a, hipStream_t st) {
 
 hipError_t launch_linear_prepare(const LinearPrepArgs &a, hipStream_t st) {
     const dim3 grid(a.cout_pad, a.experts);
-    if (a.w_type == kBf16) linear_prepare_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a);
+    if (a.codes) linear_pack_kernel<<<grid, kThreads, 0, st>>>(a);
+    else if (a.w_type == kBf16) linear_prepare_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a);
     else if (a.w_type == kF16) linear_prepare_kernel<_Float16><<<grid, kThreads, 0, st>>>(a);
     else linear_prepare_kernel<float><<<grid, kThreads, 0, st>>>(a);
     return hipGetLastError();
@@ -325,9 +376,13 @@ hipError_t launch_linear_prepare(const LinearPrepArgs &a, hipStream_t st) {
 hipError_t launch_expert_order(const OrderArgs &a, hipStream_t st) {
     const int64_t pairs = (int64_t)a.tokens * a.topk, seg = order_segment(pairs);
     const int blocks = pairs > seg ? (int)((pairs + seg - 1) / seg) : 1;
-    const size_t counts = sizeof(int) * kOrderWaves * a.experts;
-    if (blocks > 1) order_count_kernel<<<blocks, kThreads, counts, st>>>(a);
-    order_place_kernel<<<blocks, kThreads, counts + sizeof(int) * a.experts, st>>>(a);
+    const size_t counts = sizeof(int) * kOrderWaves * a.experts, all = counts + 2 * sizeof(int) * a.experts;
+    if (pairs <= kOrderOne) {
+        order_place_kernel<false><<<blocks, kOrderThreads, all, st>>>(a);
+    } else {
+        order_count_kernel<<<blocks, kOrderThreads, counts, st>>>(a);
+        order_place_kernel<true><<<blocks, kOrderThreads, all, st>>>(a);
+    }
     return hipGetLastError();
 }
 
@@ -346,7 +401,7 @@ hipError_t launch_expert_combine(const CombineArgs &a, hipStream_t st) {
 
 size_t expert_order_ws_ints(int64_t pairs, int32_t experts) {
     const int64_t seg = order_segment(pairs);
-    return pairs > seg ? (size_t)((pairs + seg - 1) / seg) * experts : 0;
+    return pairs > kOrderOne ? (size_t)((pairs + seg - 1) / seg) * experts : 0;
 }
 
 }  // namespace hatq

@@ -645,6 +645,7 @@ def _on_stream(f):
     return g
 
 
+HATQ_TOKEN_ROWS, HATQ_TOKEN_CODES = 16, 16384
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -810,9 +811,13 @@ def hatq_linear_forward(lin: PreparedLinear, x: torch.Tensor, out_dtype: Optiona
     """Tokens x [rows, cin] through one layer: y [rows, cout] of out_dtype (default: x's)."""
     n, _, xs, xt = _rows(x, "x", lin.cin)
     y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x.device)
-    ws = _linear_ws(lin, n, ws, x.device)
-    _check(load().hatq_linear_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, ws.data_ptr(),
-                                      ws.numel(), _stream()), "hatq_linear_forward")
+    if n <= HATQ_TOKEN_ROWS and n * lin.k_stride <= HATQ_TOKEN_CODES:
+        wp, wn = None, 0                # a few tokens need no workspace
+    else:
+        ws = _linear_ws(lin, n, ws, x.device)
+        wp, wn = ws.data_ptr(), ws.numel()
+    _check(load().hatq_linear_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, wp, wn, _stream()),
+           "hatq_linear_forward")
     return y
 
 

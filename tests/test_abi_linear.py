@@ -109,9 +109,12 @@ def test_refusals(L):
 
     def forward(w=None, x=P, t=1, rows=4, xs=192, y=P, yt=0, ys=100, ws=P, size=n):
         return L.hatq_linear_forward(ctypes.byref(w or weights()), x, t, rows, xs, y, yt, ys, ws, size, None)
-    for bad in [dict(x=None), dict(xs=10), dict(t=9), dict(ws=None), dict(ws=P + 64), dict(ys=0)]:
+    for bad in [dict(x=None), dict(xs=10), dict(t=9), dict(rows=17, ws=None), dict(rows=17, ws=P + 64), dict(ys=0)]:
         assert forward(**bad) == EINVAL, bad
-    assert forward(size=1023) == EWS
+    assert forward(rows=17, size=3583) == EWS
+    wide = weights(cin=8192, k_stride=8192)
+    assert forward(w=wide, rows=3, xs=8192, ws=None) == EINVAL
+    assert forward(w=wide, rows=3, xs=8192, size=3 * 8192) == EWS
 
     def grouped(w=None, x_rows=3, ends=P, src=P, rows=8, y=P, ys=100, xq=P):
         return L.hatq_experts_int8(ctypes.byref(w or weights(experts=5)), xq, P, x_rows, ends, src, rows, y, 2, ys, None)
@@ -165,7 +168,6 @@ namespace hatq {   // no launch may be reached
 hipError_t launch_token_quant(const TokenArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_linear_prepare(const LinearPrepArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_linear(const LinearArgs &, hipStream_t) { std::abort(); }
-bool linear_takes_tokens(const LinearArgs &) { std::abort(); }
 hipError_t launch_linear_tokens(const LinearArgs &, const TokenArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_expert_order(const OrderArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_expert_combine(const CombineArgs &, hipStream_t) { std::abort(); }

@@ -594,7 +594,9 @@ def test_refusals():
         (lambda: hatq.hatq_token_quant(x, 3), hatq.HATQ_EINVAL),
         (lambda: hatq.hatq_token_quant(x, 192), hatq.HATQ_EUNSUPPORTED),
         (lambda: hatq.hatq_token_quant(x, 128), hatq.HATQ_EUNSUPPORTED),        # 64 % 128
-        (lambda: hatq.hatq_linear_forward(lin, x, ws=torch.empty(256, dtype=torch.int8, device=DEV)), hatq.HATQ_EWORKSPACE),
+        (lambda: hatq.hatq_linear_forward(lin, torch.zeros((17, 64), device=DEV), ws=torch.empty(256, dtype=torch.int8, device=DEV)),
+         hatq.HATQ_EWORKSPACE),
+        (lambda: hatq.hatq_experts_forward(lin, x, ends, ws=torch.empty(256, dtype=torch.int8, device=DEV)), hatq.HATQ_EWORKSPACE),
         (lambda: hatq.hatq_expert_order(torch.zeros((2, 2), dtype=torch.int32, device=DEV), 1025), hatq.HATQ_EUNSUPPORTED),
         (lambda: hatq.hatq_pack_linear(torch.zeros((4, 8), dtype=torch.int8, device=DEV), torch.ones(4, device=DEV), hblock=16),
          hatq.HATQ_EUNSUPPORTED),
