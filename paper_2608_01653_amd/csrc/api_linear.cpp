@@ -211,10 +211,10 @@ int32_t check_mlp(const hatq_linear_weights *W_in, const hatq_linear_weights *W_
     return fit ? HATQ_OK : HATQ_EINVAL;
 }
 
-// hatq_expert_mlp's workspace: ends (at 0), src, pos, hidden and output rows, and what
-// one call at a time needs.  bytes = 0 for sizes that are not supported.
+// hatq_expert_mlp's workspace: ends (at 0), src, pos, the order's own, hidden and output
+// rows, and the codes of one layer at a time.  bytes = 0 for sizes that are not supported.
 struct MlpPlaces {
-    size_t src, pos, hidden, rows, scratch, bytes;
+    size_t src, pos, order, hidden, rows, scratch, bytes;
 };
 MlpPlaces mlp_places(const hatq_linear_weights *W_in, const hatq_linear_weights *W_out, int32_t tokens, int32_t topk) {
     MlpPlaces p{};
@@ -223,13 +223,12 @@ MlpPlaces mlp_places(const hatq_linear_weights *W_in, const hatq_linear_weights 
     const size_t pairs = (size_t)tokens * topk;
     p.src = align256((size_t)W_in->experts * 4);
     p.pos = p.src + align256(pairs * 4);
-    p.hidden = p.pos + align256(pairs * 4);
+    p.order = p.pos + align256(pairs * 4);
+    p.hidden = p.order + order;
     p.rows = p.hidden + align256(pairs * W_in->cout * 4);
     p.scratch = p.rows + align256(pairs * W_out->cout * 4);
-    size_t most = order;
-    for (size_t n : {hatq_linear_ws_bytes(W_in, tokens), hatq_linear_ws_bytes(W_out, (int32_t)pairs)})
-        if (n > most) most = n;
-    p.bytes = p.scratch + most;
+    const size_t in = hatq_linear_ws_bytes(W_in, tokens), out = hatq_linear_ws_bytes(W_out, (int32_t)pairs);
+    p.bytes = p.scratch + (in > out ? in : out);
     return p;
 }
 
@@ -383,12 +382,13 @@ int32_t hatq_expert_mlp(const hatq_linear_weights *W_in, const hatq_linear_weigh
     float *hidden = reinterpret_cast<float *>(base + p.hidden), *rows = reinterpret_cast<float *>(base + p.rows);
     const int32_t pairs = tokens * topk;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const hatq::OrderArgs o{ids, ends, src, pos, reinterpret_cast<int32_t *>(base + p.scratch), tokens, topk,
+    const hatq::OrderArgs o{ids, ends, src, pos, reinterpret_cast<int32_t *>(base + p.order), tokens, topk,
                             W_in->experts};
-    if (hatq::launch_expert_order(o, st) != hipSuccess) return HATQ_EHIP;
-    if ((s = enqueue(W_in, x, x_type, tokens, x_stride, ends, src, pairs, hidden, HATQ_F32, W_in->cout,
-                     base + p.scratch, st)) != HATQ_OK)
-        return s;
+    int8_t *xq = base + p.scratch;
+    float *sx = reinterpret_cast<float *>(xq + align256((size_t)tokens * W_in->k_stride));
+    const hatq::TokenArgs t = token_args(W_in, x, x_type, tokens, x_stride, xq, sx);
+    if (hatq::launch_order_quant(o, t, st) != hipSuccess) return HATQ_EHIP;
+    if ((s = product(W_in, xq, sx, tokens, ends, src, pairs, hidden, HATQ_F32, W_in->cout, st)) != HATQ_OK) return s;
     if ((s = enqueue(W_out, hidden, HATQ_F32, pairs, W_in->cout, ends, nullptr, pairs, rows, HATQ_F32, W_out->cout,
                      base + p.scratch, st)) != HATQ_OK)
         return s;

@@ -70,6 +70,9 @@ struct OrderArgs {
 size_t expert_order_ws_ints(int64_t pairs, int32_t experts);
 hipError_t launch_expert_order(const OrderArgs &a, hipStream_t st);
 
+// Both of an expert block's first steps, in one launch where they are small enough.
+hipError_t launch_order_quant(const OrderArgs &o, const TokenArgs &a, hipStream_t st);
+
 struct CombineArgs {
     const float *h;
     const int32_t *pos;

@@ -658,9 +658,9 @@ struct TileCost {
 constexpr TileCost kTiles[] = {
     {64, 64, 4.5, 0.085, 256, 1000.0},   // four groups of waves over the contraction
     {64, 128, 4.0, 0.15, 1024, 1450.0},
-    {128, 128, 4.0, 0.19, 768, 1850.0},
-    {128, 256, 6.0, 0.30, 512, 2050.0},
-    {256, 256, 6.0, 0.56, 256, 2120.0},
+    {128, 128, 5.5, 0.19, 768, 1850.0},
+    {128, 256, 7.0, 0.30, 512, 2050.0},
+    {256, 256, 10.0, 0.56, 256, 2120.0},
 };
 constexpr double kWeightRate = 6.5e6, kRowRate = 7.3e6;   // bytes a microsecond: memory, codes from the L2s
 constexpr double kTileRate = 4.0e4;                       // and what one tile's CU takes of the weights

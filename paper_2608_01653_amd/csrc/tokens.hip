@@ -15,14 +15,13 @@ constexpr int kThreads = 256;
 // A token's row stays in registers between its maximum and its codes, so x is read
 // once.  Chunk i of row thread t is number i * 64 * WAVES + t.  The maximum keeps NaN:
 // a token with a value that is not finite gets the scale NaN and codes 0.
+// Row `row` by its thread t; red: WAVES floats of LDS for each row of the block.
 template <int WAVES, int CH, typename T>
-__global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quant_kernel(const TokenArgs a, int vec) {
+__device__ __forceinline__ void token_quant_row(const TokenArgs &a, int vec, int64_t row, int t, float *red) {
     constexpr int RT = 64 * WAVES;   // threads of a row
-    const int t = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const int block = blockIdx.y * gridDim.x + blockIdx.x;
-    const int row = WAVES == 1 ? block * (kThreads / 64) + (threadIdx.x >> 6) : block;
-    if (row >= a.rows) return;   // whole waves; all of a block where a row has several
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+    const bool in = row < a.rows;    // (a block of several waves a row has a barrier for all)
+    if (WAVES == 1 && !in) return;
+    const T *x = static_cast<const T *>(a.x) + (in ? row : 0) * a.x_stride;
     const int chunks = a.k_stride >> 3;
 
     float v[CH * 8];
@@ -39,18 +38,18 @@ __global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quan
     const float sigma = token_butterfly(v, t, a.log_b);
     float m = token_max(v);
     if constexpr (WAVES > 1) {
-        __shared__ float red[WAVES];
         if ((t & 63) == 0) red[t >> 6] = m;
         __syncthreads();
         m = red[0];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m = __builtin_elementwise_maximum(m, red[w]);
+        if (!in) return;
     }
     const float s = token_scale(m);
     if (t == 0) a.sx[row] = s;
     const float r = sigma * (1.0f / s);
     const bool plain = token_plain(s);
-    int8_t *q = a.xq + (int64_t)row * a.k_stride;
+    int8_t *q = a.xq + row * a.k_stride;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * RT + t;
@@ -59,12 +58,24 @@ __global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quan
     }
 }
 
+// One row a block of WAVES waves, or four of one wave.
+template <int WAVES, int CH, typename T>
+__global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quant_kernel(const TokenArgs a, int vec) {
+    __shared__ float red[WAVES];
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t row = WAVES == 1 ? block * (kThreads / 64) + (threadIdx.x >> 6) : block;
+    token_quant_row<WAVES, CH, T>(a, vec, row, WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, red);
+}
+
+int vector_rows(const TokenArgs &a) {
+    return (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride * (a.x_type == kF32 ? 4 : 2) % 16 == 0;
+}
+
 template <int WAVES, int CH>
 hipError_t token_launch(const TokenArgs &a, hipStream_t st) {
     const dim3 grid = grid_of(WAVES == 1 ? (a.rows + 3) / 4 : a.rows);
     const int threads = WAVES == 1 ? kThreads : 64 * WAVES;
-    const int size = a.x_type == kF32 ? 4 : 2;
-    const int vec = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride * size % 16 == 0;
+    const int vec = vector_rows(a);
     if (a.x_type == kF32) token_quant_kernel<WAVES, CH, float><<<grid, threads, 0, st>>>(a, vec);
     else if (a.x_type == kBf16) token_quant_kernel<WAVES, CH, bf16_t><<<grid, threads, 0, st>>>(a, vec);
     else token_quant_kernel<WAVES, CH, _Float16><<<grid, threads, 0, st>>>(a, vec);
@@ -217,9 +228,10 @@ __global__ void __launch_bounds__(kOrderThreads) order_count_kernel(const OrderA
     }
 }
 
+// Block blockIdx.x of `blocks`.  lds: [experts] rows in all blocks, in the blocks before;
+// counts [waves][experts].
 template <bool TABLE>
-__global__ void __launch_bounds__(kOrderThreads) order_place_kernel(const OrderArgs a) {
-    extern __shared__ int lds[];   // [experts] rows in all blocks, in the blocks before; counts [waves][experts]
+__device__ void order_place(const OrderArgs &a, int blocks, int *lds) {
     const int E = a.experts;
     int *total = lds, *before = lds + E, *counts = lds + 2 * E;
     const int64_t pairs = (int64_t)a.tokens * a.topk;
@@ -227,7 +239,7 @@ __global__ void __launch_bounds__(kOrderThreads) order_place_kernel(const OrderA
     __syncthreads();
     order_counts(a, pairs, counts);
     if (TABLE) {
-        for (int i = threadIdx.x; i < (int)gridDim.x * E; i += kOrderThreads) {
+        for (int i = threadIdx.x; i < blocks * E; i += kOrderThreads) {
             const int b = i / E, e = i - b * E, n = a.ws[i];
             atomicAdd(&total[e], n);
             if (b < (int)blockIdx.x) atomicAdd(&before[e], n);
@@ -304,8 +316,26 @@ __global__ void __launch_bounds__(kOrderThreads) order_place_kernel(const OrderA
             if (i < s.end) a.pos[i] = row;
         }
     });
-    for (int64_t i = all + (int64_t)blockIdx.x * kOrderThreads + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * kOrderThreads)
+    for (int64_t i = all + (int64_t)blockIdx.x * kOrderThreads + threadIdx.x; i < pairs; i += (int64_t)blocks * kOrderThreads)
         a.src[i] = -1;
+}
+
+template <bool TABLE>
+__global__ void __launch_bounds__(kOrderThreads) order_place_kernel(const OrderArgs a) {
+    extern __shared__ int lds[];
+    order_place<TABLE>(a, gridDim.x, lds);
+}
+
+// The order of the rows in the first blocks, the codes of the tokens in the rest: neither
+// needs the other.
+template <int WAVES, int CH, typename T>
+__global__ void __launch_bounds__(kOrderThreads) order_quant_kernel(const OrderArgs o, int blocks, const TokenArgs a,
+                                                                    int vec) {
+    extern __shared__ int lds[];
+    if ((int)blockIdx.x < blocks) return order_place<false>(o, blocks, lds);
+    constexpr int ROWS = kOrderThreads / (64 * WAVES);   // of a block
+    token_quant_row<WAVES, CH, T>(a, vec, (blockIdx.x - blocks) * ROWS + threadIdx.x / (64 * WAVES),
+                                  threadIdx.x % (64 * WAVES), reinterpret_cast<float *>(lds) + threadIdx.x / (64 * WAVES) * WAVES);
 }
 
 // ---- the weighted sum of expert rows ------------------------------------------------
@@ -384,6 +414,32 @@ hipError_t launch_expert_order(const OrderArgs &a, hipStream_t st) {
         order_place_kernel<true><<<blocks, kOrderThreads, all, st>>>(a);
     }
     return hipGetLastError();
+}
+
+template <int WAVES, int CH>
+static hipError_t order_quant(const OrderArgs &o, int blocks, const TokenArgs &a, hipStream_t st) {
+    constexpr int ROWS = kOrderThreads / (64 * WAVES);
+    const int grid = blocks + (a.rows + ROWS - 1) / ROWS, vec = vector_rows(a);
+    size_t bytes = sizeof(int) * (2 + kOrderWaves) * o.experts;
+    if (bytes < sizeof(float) * kOrderWaves) bytes = sizeof(float) * kOrderWaves;
+    if (a.x_type == kF32) order_quant_kernel<WAVES, CH, float><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a, vec);
+    else if (a.x_type == kBf16) order_quant_kernel<WAVES, CH, bf16_t><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a, vec);
+    else order_quant_kernel<WAVES, CH, _Float16><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a, vec);
+    return hipGetLastError();
+}
+
+hipError_t launch_order_quant(const OrderArgs &o, const TokenArgs &a, hipStream_t st) {
+    const int64_t pairs = (int64_t)o.tokens * o.topk, seg = order_segment(pairs);
+    const int blocks = pairs > seg ? (int)((pairs + seg - 1) / seg) : 1, chunks = a.k_stride >> 3;
+    if (pairs > kOrderOne || chunks > 1024) {
+        const hipError_t e = launch_expert_order(o, st);
+        return e == hipSuccess ? launch_token_quant(a, st) : e;
+    }
+    if (chunks <= 64) return order_quant<1, 1>(o, blocks, a, st);
+    if (chunks <= 128) return order_quant<1, 2>(o, blocks, a, st);
+    if (chunks <= 256) return order_quant<2, 2>(o, blocks, a, st);
+    if (chunks <= 512) return order_quant<4, 2>(o, blocks, a, st);
+    return order_quant<8, 2>(o, blocks, a, st);
 }
 
 hipError_t launch_expert_combine(const CombineArgs &a, hipStream_t st) {

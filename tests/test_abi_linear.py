@@ -171,6 +171,7 @@ hipError_t launch_linear(const LinearArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_linear_tokens(const LinearArgs &, const TokenArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_expert_order(const OrderArgs &, hipStream_t) { std::abort(); }
 hipError_t launch_expert_combine(const CombineArgs &, hipStream_t) { std::abort(); }
+hipError_t launch_order_quant(const OrderArgs &, const TokenArgs &, hipStream_t) { std::abort(); }
 size_t expert_order_ws_ints(int64_t pairs, int32_t experts) { return (size_t)pairs * experts; }
 }
 int main() {
