@@ -169,8 +169,7 @@ hatq::TokenArgs token_args(const hatq_linear_weights *W, const void *x, int32_t 
     return a;
 }
 
-// One layer's tokens that the product's own blocks quantize.  (bf16, 4096 -> 4096, one
-// row: 5.7 us, 8.9 by two kernels; four rows of 4096 and sixteen of 1024 are level.)
+// One layer's calls that need no workspace: the product's own blocks quantize.
 bool few_tokens(const hatq_linear_weights *W, int32_t rows) {
     return rows <= HATQ_TOKEN_ROWS && (int64_t)rows * W->k_stride <= HATQ_TOKEN_CODES;
 }
@@ -184,7 +183,7 @@ int32_t enqueue(const hatq_linear_weights *W, const void *x, int32_t x_type, int
     float *sx = reinterpret_cast<float *>(xq + align256((size_t)x_rows * W->k_stride));
     const hatq::TokenArgs t = token_args(W, x, x_type, x_rows, x_stride, xq, sx);
     const hatq::LinearArgs a = product_args(W, xq, sx, x_rows, ends, src, rows, y, y_type, y_stride);
-    if (!ends && few_tokens(W, rows)) return hip_status(hatq::launch_linear_tokens(a, t, st));
+    if (hatq::linear_takes_tokens(a)) return hip_status(hatq::launch_linear_tokens(a, t, st));
     if (hatq::launch_token_quant(t, st) != hipSuccess) return HATQ_EHIP;
     return hip_status(hatq::launch_linear(a, st));
 }

@@ -58,8 +58,9 @@ struct LinearArgs {
 };
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
 
-// One layer's product of at most 16 rows and 16384 codes that its own blocks quantize (xq
-// and sx unused, no ends).
+// One layer's product of tokens that its own blocks quantize (xq and sx unused, no ends):
+// for a few tokens (HATQ_TOKEN_ROWS, HATQ_TOKEN_CODES) and for small layers.
+bool linear_takes_tokens(const LinearArgs &a);
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st);
 
 struct OrderArgs {

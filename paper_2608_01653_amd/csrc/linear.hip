@@ -6,6 +6,7 @@
 // an accumulator lane holds one token and runs of four adjacent channels, which it
 // stores as one piece.  The contraction index inside a 64-byte step is the same
 // permutation on both sides, which an integer sum does not see.
+#include "../../include/hatq.h"
 #include "hatq_device.h"
 #include "linear.h"
 #include "linear_device.h"
@@ -149,6 +150,53 @@ __device__ void zero_tile(const LinearArgs &a, int row0, int rows, int c0, int c
     }
 }
 
+// The outputs of one 16 x 16 accumulator of the layer with factors at w_scale and bias:
+// this lane's row (written if below end), channels 16 c16 + 4 (lane / 16) and on.
+template <int G>
+__device__ __forceinline__ void finish16(const LinearArgs &a, const float *w_scale, const float *bias, const v4i (&sum)[G],
+                                         float scale, int row, int end, int c16, int block0, int lane) {
+    float z[2][4];
+    const int p = block0 * 16 + (lane >> 4) * 4, c = c16 * 16 + (lane >> 4) * 4;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const int q[4] = {sum[g][0], sum[g][1], sum[g][2], sum[g][3]};
+        dequant4(a, w_scale + p + 32 * g, bias + p + 32 * g, q, scale, z[g]);
+    }
+    if (G == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
+    }
+    if (row < end && c < a.cout) put4(a, row, c, z[0], vector_rows(a));
+}
+
+// A token's chunks of 8 elements, number i * THREADS + t, and their codes in LDS.
+template <typename T, int CH, int THREADS>
+__device__ __forceinline__ void load_chunks(const TokenArgs &x, int row, int t, int vec, float (&v)[8 * CH]) {
+    const T *p = static_cast<const T *>(x.x) + max(row, 0) * x.x_stride;
+    const int n = row < 0 ? 0 : x.cin;   // (an empty token is all zeros)
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int e = (i * THREADS + t) * 8;
+        if (vec && e + 8 <= n) {
+            load8(p + e, &v[8 * i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < n ? to_float(p[e + j]) : 0.0f;
+        }
+    }
+}
+template <int CH, int THREADS>
+__device__ __forceinline__ void store_chunks(int8_t *to, int k_stride, int t, const float (&v)[8 * CH], float sigma, float s) {
+    const float r = sigma * (1.0f / s);
+    const bool plain = token_plain(s);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = i * THREADS + t;
+        const uint2 q = token_codes8(&v[8 * i], sigma, s, r, plain);
+        if (c < k_stride >> 3) *reinterpret_cast<uint2 *>(to + c * 8) = q;
+    }
+}
+
 // ---- few rows -------------------------------------------------------------------------
 // Eight waves, WK of them on one group of 16 output channels (gated: of their gates and
 // their values) by 16 MT rows: they take the contraction 64 bytes in turn and add up in
@@ -241,13 +289,14 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
 }
 
 // ---- few tokens, floats in ------------------------------------------------------------
-// At most 16 rows, one layer, with the tokens' quantization in front: every block makes the codes of its
-// rows itself, in LDS, while its first weights are on their way.  WR waves share a row
-// (and 8 / WR rows are taken at once), a lane CH chunks of 8 elements.  It pays where a
-// block has few elements to quantize: one launch instead of two, and no codes in memory.
-template <typename T, int G, int CH, int WR>
+// At most 16 rows, one layer, with the tokens' quantization in front: every block makes
+// the codes of its rows itself, in LDS, while its first weights are on their way.  All
+// eight waves share a row (a lane CH chunks of 8 elements, one row after the other) and
+// then the contraction of 16 output channels.  One launch instead of two, and no codes
+// in memory.
+template <typename T, int G, int CH>
 __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, const TokenArgs x, int vec) {
-    constexpr int WAVES = 8, U = 8, RT = 64 * WR;
+    constexpr int WAVES = 8, U = 8;
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     v4i(*part)[G][64] = reinterpret_cast<v4i(*)[G][64]>(lds);                // [WAVES][G][64]
     float *scale = reinterpret_cast<float *>(lds + WAVES * G * 1024);          // [16]
@@ -257,22 +306,8 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     const int c16 = blockIdx.x, rows = a.rows;
     const int pitch = a.k_stride + 16;   // 16 rows' pieces then lie in different banks
 
-    const int rt = (wave % WR) * 64 + lane;
     float v[8 * CH];
-    auto load = [&](int row) {
-        const T *p = static_cast<const T *>(x.x) + min(row, rows - 1) * x.x_stride;
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const int e = (i * RT + rt) * 8;
-            if (vec && e + 8 <= x.cin) {
-                load8(p + e, &v[8 * i]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < x.cin ? to_float(p[e + j]) : 0.0f;
-            }
-        }
-    };
-    load(wave / WR);
+    load_chunks<T, CH, 512>(x, 0, threadIdx.x, vec, v);
 
     const int nks = a.k_stride >> 6;
     const int block0 = G == 1 ? c16 : (c16 >> 1) * 4 + (c16 & 1);   // of 16 packed columns
@@ -289,30 +324,19 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     weights(wave);
     __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
 
-    for (int first = 0; first < rows; first += WAVES / WR) {
-        const int row = first + wave / WR;
-        if (first) load(row);
+    for (int row = 0; row < rows; ++row) {
+        if (row) load_chunks<T, CH, 512>(x, row, threadIdx.x, vec, v);
         const float sigma = token_butterfly(v, lane, x.log_b);
         float m = token_max(v);
-        if constexpr (WR > 1) {
-            if (first) __syncthreads();   // the row before has been read
-            if (lane == 0) most[wave] = m;
-            __syncthreads();
-            m = most[0];
+        if (row) __syncthreads();   // the row before has been read
+        if (lane == 0) most[wave] = m;
+        __syncthreads();
+        m = most[0];
 #pragma unroll
-            for (int k = 1; k < WR; ++k) m = __builtin_elementwise_maximum(m, most[k]);
-        }
-        const float s = token_scale(m), rs = sigma * (1.0f / s);
-        const bool plain = token_plain(s);
-        if (row < rows) {
-            if (rt == 0) scale[row] = s;
-#pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const int c = i * RT + rt;
-                const uint2 q = token_codes8(&v[8 * i], sigma, s, rs, plain);
-                if (c < a.k_stride >> 3) *reinterpret_cast<uint2 *>(codes + row * pitch + c * 8) = q;
-            }
-        }
+        for (int k = 1; k < WAVES; ++k) m = __builtin_elementwise_maximum(m, most[k]);
+        const float s = token_scale(m);
+        if (threadIdx.x == 0) scale[row] = s;
+        store_chunks<CH, 512>(codes + row * pitch, a.k_stride, threadIdx.x, v, sigma, s);
     }
     __syncthreads();
 
@@ -335,22 +359,102 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     for (int g = 0; g < G; ++g) part[wave][g][lane] = acc[g];
     __syncthreads();
     if (wave != 0) return;
-    float z[2][4];
-    const int p = block0 * 16 + (lane >> 4) * 4;
+    v4i sum[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        v4i sum = part[0][g][lane];
+        sum[g] = part[0][g][lane];
 #pragma unroll
-        for (int k = 1; k < WAVES; ++k) sum += part[k][g][lane];
-        const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
-        dequant4(a, a.w_scale + p + 32 * g, a.bias + p + 32 * g, q, scale[mine], z[g]);
+        for (int k = 1; k < WAVES; ++k) sum[g] += part[k][g][lane];
     }
-    if (G == 2) {
+    finish16<G>(a, a.w_scale, a.bias, sum, scale[mine], lane & 15, rows, c16, block0, lane);
+}
+
+// ---- small layers, floats in ------------------------------------------------------------
+// A contraction of at most 1024: a block quantizes 16 MT rows (of one expert), a wave a
+// row at a time (all of a wave's rows loaded at once), into LDS, and then each wave takes
+// groups of 16 output channels over the whole contraction, the weights straight from the
+// L2s.  blockIdx.y: `per` of the groups, a multiple of the waves.
+template <typename T, int G, int CH, int MT>
+__global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, const TokenArgs x, int vec, int per) {
+    constexpr int WAVES = 8, U = 8, ROWS = 16 * MT, TURNS = ROWS / WAVES;
+    __shared__ __attribute__((aligned(16))) int8_t codes[ROWS * (512 * CH + 16)];
+    __shared__ float scale[ROWS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    RowTiles<ROWS> tiles(a);
+    if ((int)blockIdx.x >= tiles.total()) return;
+    const RowTile r = tiles.find(blockIdx.x);
+    const int row0 = r.row0, rows = min(r.end - row0, ROWS);
+    if (r.expert < 0) return zero_tile(a, row0, rows, blockIdx.y * per * 16, per * 16);
+    const int64_t first = (int64_t)r.expert * a.cout_pad;   // of this expert's columns
+    const int nks = a.k_stride >> 6, pitch = a.k_stride + 16;
+    const int end = min(((int)blockIdx.y + 1) * per, (a.cout + 15) / 16);
+    int c16 = blockIdx.y * per + wave;
+
+    float v[TURNS][8 * CH];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
+    for (int i = 0; i < TURNS; ++i)
+        if (wave + WAVES * i < rows) load_chunks<T, CH, 64>(x, token_of(a, row0 + wave + WAVES * i), lane, vec, v[i]);
+
+    const int64_t value = (int64_t)32 * a.k_stride;   // from the gates' columns to the values'
+    v4i fw[U][G];
+    auto weights = [&](int c, int k0) {
+        const int block0 = G == 1 ? c : (c >> 1) * 4 + (c & 1);
+        const int8_t *w = a.wp + (first + block0 * 16) * a.k_stride + lane * 16;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+                fw[u][g] = *reinterpret_cast<const v4i *>(w + g * value + min(k0 + u, nks - 1) * 1024);
+    };
+    if (c16 < end) weights(c16, 0);
+    __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
+
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int row = wave + WAVES * i;
+        if (row >= rows) break;
+        const float sigma = token_butterfly(v[i], lane, x.log_b);
+        const float s = token_scale(token_max(v[i]));
+        if (lane == 0) scale[row] = s;
+        store_chunks<CH, 64>(codes + row * pitch, a.k_stride, lane, v[i], sigma, s);
     }
-    const int c = c16 * 16 + (lane >> 4) * 4;
-    if ((lane & 15) < rows && c < a.cout) put4(a, lane & 15, c, z[0], vector_rows(a));
+    __syncthreads();
+
+    int mine[MT];
+    const int8_t *from[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        mine[m] = min(16 * m + (lane & 15), rows - 1);
+        from[m] = codes + mine[m] * pitch + (lane >> 4) * 16;
+    }
+    while (c16 < end) {
+        v4i acc[MT][G];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int g = 0; g < G; ++g) acc[m][g] = v4i{0, 0, 0, 0};
+        for (int k0 = 0; k0 < nks; k0 += U) {
+            if (k0) weights(c16, k0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (k0 + u >= nks) break;
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const v4i fx = *reinterpret_cast<const v4i *>(from[m] + (k0 + u) * 64);
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+                        acc[m][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][g], fx, acc[m][g], 0, 0, 0);
+                }
+            }
+        }
+        const int c = c16;
+        c16 += WAVES;
+        if (c16 < end) weights(c16, 0);   // the next group's, under way over the stores
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+            finish16<G>(a, a.w_scale + first, a.bias + first, acc[m], scale[mine[m]], row0 + 16 * m + (lane & 15),
+                        row0 + rows, c, G == 1 ? c : (c >> 1) * 4 + (c & 1), lane);
+    }
 }
 
 // ---- many rows --------------------------------------------------------------------------
@@ -611,21 +715,37 @@ void stream(const LinearArgs &a, hipStream_t st, int wk) {
     else linear_stream_kernel<MT, 1, U><<<grid, 512, 0, st>>>(a, wk);
 }
 
-template <typename T, int CH, int WR>
-void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
+template <typename T, int CH>
+void token(const LinearArgs &a, const TokenArgs &x, int vec, hipStream_t st) {
     const int grid = (a.cout + 15) / 16;
     const size_t bytes = 8 * (a.gated ? 2 : 1) * 1024 + 128 + (size_t)a.rows * (a.k_stride + 16);
-    const int vec = (reinterpret_cast<uintptr_t>(x.x) & 15) == 0 && x.x_stride * (int)sizeof(T) % 16 == 0;
-    if (a.gated) linear_token_kernel<T, 2, CH, WR><<<grid, 512, bytes, st>>>(a, x, vec);
-    else linear_token_kernel<T, 1, CH, WR><<<grid, 512, bytes, st>>>(a, x, vec);
+    if (a.gated) linear_token_kernel<T, 2, CH><<<grid, 512, bytes, st>>>(a, x, vec);
+    else linear_token_kernel<T, 1, CH><<<grid, 512, bytes, st>>>(a, x, vec);
 }
+
+template <typename T, int CH, int MT>
+void small(const LinearArgs &a, const TokenArgs &x, int vec, hipStream_t st) {
+    // as few column ranges as fill the card twice: each range quantizes the rows again
+    const int groups = (a.cout + 15) / 16, blocks = (int)most_row_tiles(a, 16 * MT);
+    int ranges = (groups + 7) / 8;
+    if (ranges > (512 + blocks - 1) / blocks) ranges = (512 + blocks - 1) / blocks;
+    const int per = ((groups + ranges - 1) / ranges + 7) / 8 * 8;
+    const dim3 grid(blocks, (groups + per - 1) / per);
+    if (a.gated) linear_small_kernel<T, 2, CH, MT><<<grid, 512, 0, st>>>(a, x, vec, per);
+    else linear_small_kernel<T, 1, CH, MT><<<grid, 512, 0, st>>>(a, x, vec, per);
+}
+
 template <typename T>
 void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
-    if (a.k_stride <= 512) token<T, 1, 1>(a, x, st);
-    else if (a.k_stride <= 1024 && a.rows > 1) token<T, 2, 1>(a, x, st);
-    else if (a.k_stride <= 4096) token<T, 1, 8>(a, x, st);
-    else if (a.k_stride <= 8192) token<T, 2, 8>(a, x, st);
-    else token<T, 4, 8>(a, x, st);
+    const int vec = (reinterpret_cast<uintptr_t>(x.x) & 15) == 0 && x.x_stride * (int)sizeof(T) % 16 == 0;
+    // (1024 -> 256, bf16: 16384 rows 20.4 us in tiles of 32 rows, 25.1 of 16; 4096 rows 10.5
+    // and 9.8; 320 -> 320, 6144 rows: 16.2 and 8.9)
+    const bool two = !a.ends && a.rows > 8192;
+    if (a.k_stride <= 512) two ? small<T, 1, 2>(a, x, vec, st) : small<T, 1, 1>(a, x, vec, st);
+    else if (a.k_stride <= 1024) two ? small<T, 2, 2>(a, x, vec, st) : small<T, 2, 1>(a, x, vec, st);
+    else if (a.k_stride <= 4096) token<T, 1>(a, x, vec, st);
+    else if (a.k_stride <= 8192) token<T, 2>(a, x, vec, st);
+    else token<T, 4>(a, x, vec, st);
 }
 
 template <int WM, int WN, int FM, int FN, int STAGES, int KG = 1>
@@ -638,6 +758,26 @@ void tile(const LinearArgs &a, hipStream_t st) {
 
 }  // namespace
 
+// Row tiles that are met: groups fill half of their last tile on average.
+double met_tiles(const LinearArgs &a, int bm) {
+    if (!a.ends) return (a.rows + bm - 1) / bm;
+    const double groups = a.experts < a.rows ? a.experts : a.rows, t = (double)a.rows / bm + 0.5 * groups;
+    return t > groups ? t : groups;
+}
+
+// The small kernel reads the weights again for every 16 rows: it wins while these are
+// few, or cheap against the codes' way through memory.  (us, two kernels and one.  bf16:
+// 320 -> 320, 6144 rows 12.0 and 8.9; 512 -> 2048, 1024 rows 9.7 and 8.9, 2048 rows 11.9
+// and 13.0; 1024 -> 256, 6144 rows 15.6 and 13.2; 1024 -> 4096, 128 rows 9.2 and 8.5, 512
+// rows 11.7 and 13.4.  Float32, 32 experts of 512 -> 1024, 96 rows 8.1 and 6.0, 384 rows
+// 10.0 and 7.3, 768 rows 10.4 and 11.5; 16 of 1024 -> 2048, 192 rows 13.4 and 12.1, 384
+// rows 13.4 and 17.0; 8 of 320 -> 320, 8192 rows 15.8 and 12.3.)
+bool linear_takes_tokens(const LinearArgs &a) {
+    if (!a.ends && a.rows <= HATQ_TOKEN_ROWS && (int64_t)a.rows * a.k_stride <= HATQ_TOKEN_CODES) return true;
+    const double most = a.ends ? 8e8 : a.cout_pad <= 512 ? 5e9 : 1.2e9;
+    return a.k_stride <= 1024 && met_tiles(a, 16) * 16.0 * a.k_stride * a.cout_pad <= most;
+}
+
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     if (x.x_type == kF32) token<float>(a, x, st);
     else if (x.x_type == kBf16) token<bf16_t>(a, x, st);
@@ -647,8 +787,7 @@ hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStre
 
 // ---- which kernel ------------------------------------------------------------------------
 // Estimates in microseconds, fitted to measurements of all the kernels over 320 to 16384
-// contractions and outputs, 16 to 6144 rows, 1 to 64 experts (MI355X).  `tiles` stands for
-// the row tiles that are met: groups fill half of their last tile on average.
+// contractions and outputs, 16 to 6144 rows, 1 to 64 experts (MI355X). 
 struct TileCost {
     int bm, bn;
     double fixed, step;   // of a launch; a step of 64 bytes of the contraction, latency
@@ -664,12 +803,6 @@ constexpr TileCost kTiles[] = {
 };
 constexpr double kWeightRate = 6.5e6, kRowRate = 7.3e6;   // bytes a microsecond: memory, codes from the L2s
 constexpr double kTileRate = 4.0e4;                       // and what one tile's CU takes of the weights
-
-double met_tiles(const LinearArgs &a, int bm) {
-    if (!a.ends) return (a.rows + bm - 1) / bm;
-    const double groups = a.experts < a.rows ? a.experts : a.rows, t = (double)a.rows / bm + 0.5 * groups;
-    return t > groups ? t : groups;
-}
 
 double weight_time(const LinearArgs &a, double tiles) {
     const double groups = a.ends && a.experts < a.rows ? a.experts : a.ends ? a.rows : 1;
