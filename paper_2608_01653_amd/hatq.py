@@ -10,7 +10,6 @@ The function names mirror the C ABI in ``include/hatq.h``.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
 from dataclasses import dataclass
 from typing import Optional, Tuple
@@ -633,18 +632,9 @@ def hatq_layer_forward(layer: PreparedLayer, form, x: torch.Tensor, x_absmax: Op
 
 # ---- linear layers over tokens ------------------------------------------------
 
-# Every function here takes stream=, a torch.cuda.Stream: the call, what it allocates and
-# the copies it makes of its arguments are then that stream's, not the current one's.
-def _on_stream(f):
-    @functools.wraps(f)
-    def g(*args, stream=None, **named):
-        if stream is None:
-            return f(*args, **named)
-        with torch.cuda.stream(stream):
-            return f(*args, **named)
-    return g
-
-
+# With stream=, a torch.cuda.Stream, a call, what it allocates and the copies it makes of
+# its arguments are that stream's, not the current one's: each function calls itself again
+# under it.
 HATQ_TOKEN_ROWS, HATQ_TOKEN_CODES = 16, 16384
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
@@ -715,10 +705,13 @@ def _linear(call: str, e: int, held: int, cin: int, gated: bool, hblock: int, de
     return PreparedLinear(buf, out, e, cin, cout, out.k_stride)
 
 
-@_on_stream
-def hatq_prepare_linear(w: torch.Tensor, bias: Optional[torch.Tensor] = None, hblock: int = 1, gated: bool = False) -> PreparedLinear:
+def hatq_prepare_linear(w: torch.Tensor, bias: Optional[torch.Tensor] = None, hblock: int = 1, gated: bool = False,
+                        stream=None) -> PreparedLinear:
     """A layer from float weights [held, cin], or experts from [experts, held, cin]
     (bias accordingly).  gated: held = 2 cout, gates first."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_prepare_linear(w, bias, hblock, gated)
     w, e, held, cin = _held(w, gated, "w")
     t = _dtype(w.dtype, "w")
     _need(w, "w", w.dtype, 0)
@@ -729,11 +722,13 @@ def hatq_prepare_linear(w: torch.Tensor, bias: Optional[torch.Tensor] = None, hb
                                                                          _stream()))
 
 
-@_on_stream
 def hatq_pack_linear(codes: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
-                     hblock: int = 1, gated: bool = False) -> PreparedLinear:
+                     hblock: int = 1, gated: bool = False, stream=None) -> PreparedLinear:
     """The same from int8 codes of the transformed weights and their fp32 scales, one
     for each channel (quantized elsewhere)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_pack_linear(codes, w_scale, bias, hblock, gated)
     codes, e, held, cin = _held(codes, gated, "codes")
     _need(codes, "codes", torch.int8, 0)
     s = w_scale.contiguous()
@@ -745,11 +740,13 @@ def hatq_pack_linear(codes: torch.Tensor, w_scale: torch.Tensor, bias: Optional[
                                                                       out, _stream()))
 
 
-@_on_stream
 def hatq_token_quant(x: torch.Tensor, hblock: int = 1, xq: Optional[torch.Tensor] = None,
-                     scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+                     scale: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Tokens x [rows, cin] -> (int8 codes [rows, cin rounded up to 64], a scale for
     each token, fp32 [rows])."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_token_quant(x, hblock, xq, scale)
     n, c, stride, t = _rows(x, "x")
     ks = (c + 63) // 64 * 64
     if xq is None:
@@ -763,10 +760,10 @@ def hatq_token_quant(x: torch.Tensor, hblock: int = 1, xq: Optional[torch.Tensor
     return xq, scale
 
 
-def _out_rows(y: Optional[torch.Tensor], rows: int, cout: int, dtype: torch.dtype, device):
-    """(y, stride, dtype code) of the output rows, allocated if y is None."""
+def _out_rows(y: Optional[torch.Tensor], rows: int, cout: int, dtype: torch.dtype, x: torch.Tensor):
+    """(y, stride, dtype code) of the output rows, allocated beside x if y is None."""
     if y is None:
-        return torch.empty((rows, cout), dtype=dtype, device=device), cout, _dtype(dtype, "out_dtype")
+        return x.new_empty((rows, cout), dtype=dtype), cout, _dtype(dtype, "out_dtype")
     n, _, stride, t = _rows(y, "y", cout)
     if n != rows:
         raise ValueError(f"y: {rows} rows expected, got {n}")
@@ -781,12 +778,14 @@ def _codes(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor) -> int:
     return xq.shape[0]
 
 
-@_on_stream
 def hatq_linear_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor,
-                     out_dtype: torch.dtype = torch.float32, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+                     out_dtype: torch.dtype = torch.float32, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Token codes through one layer: y [rows, cout] of out_dtype (or of the given y)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_linear_int8(lin, xq, scale, out_dtype, y)
     n = _codes(lin, xq, scale)
-    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype, xq.device)
+    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype, xq)
     _check(load().hatq_linear_int8(lin.ref, xq.data_ptr(), scale.data_ptr(), n, y.data_ptr(), yt, ys,
                                    _stream()), "hatq_linear_int8")
     return y
@@ -796,25 +795,26 @@ def hatq_linear_ws_bytes(lin: PreparedLinear, rows: int) -> int:
     return int(load().hatq_linear_ws_bytes(lin.ref, rows))
 
 
-def _linear_ws(lin: PreparedLinear, rows: int, ws: Optional[torch.Tensor], device) -> torch.Tensor:
+def _linear_ws(lin: PreparedLinear, rows: int, ws: Optional[torch.Tensor], x: torch.Tensor) -> torch.Tensor:
     if ws is None:
         # hatq_linear_ws_bytes, without the call
-        return torch.empty(((rows * lin.k_stride + 255) & -256) + ((4 * rows + 255) & -256) or 256,
-                           dtype=torch.int8, device=device)
+        return x.new_empty(((rows * lin.k_stride + 255) & -256) + ((4 * rows + 255) & -256) or 256, dtype=torch.int8)
     _need(ws, "ws", torch.int8, 0)
     return ws
 
 
-@_on_stream
 def hatq_linear_forward(lin: PreparedLinear, x: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
-                        y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+                        y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Tokens x [rows, cin] through one layer: y [rows, cout] of out_dtype (default: x's)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_linear_forward(lin, x, out_dtype, y, ws)
     n, _, xs, xt = _rows(x, "x", lin.cin)
-    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x.device)
+    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
     if n <= HATQ_TOKEN_ROWS and n * lin.k_stride <= HATQ_TOKEN_CODES:
         wp, wn = None, 0                # a few tokens need no workspace
     else:
-        ws = _linear_ws(lin, n, ws, x.device)
+        ws = _linear_ws(lin, n, ws, x)
         wp, wn = ws.data_ptr(), ws.numel()
     _check(load().hatq_linear_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, wp, wn, _stream()),
            "hatq_linear_forward")
@@ -832,42 +832,48 @@ def _grouping(lin: PreparedLinear, ends: torch.Tensor, src: Optional[torch.Tenso
     return src.shape[0]
 
 
-@_on_stream
 def hatq_experts_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor, ends: torch.Tensor,
                       src: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
-                      y: Optional[torch.Tensor] = None) -> torch.Tensor:
+                      y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Token codes grouped by expert: row i of y is token src[i] (or i) through the first
     expert e with i < ends[e] (int32 [experts], on the device)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_experts_int8(lin, xq, scale, ends, src, out_dtype, y)
     n = _codes(lin, xq, scale)
     rows = _grouping(lin, ends, src, n)
-    y, ys, yt = _out_rows(y, rows, lin.cout, out_dtype, xq.device)
+    y, ys, yt = _out_rows(y, rows, lin.cout, out_dtype, xq)
     _check(load().hatq_experts_int8(lin.ref, xq.data_ptr(), scale.data_ptr(), n, ends.data_ptr(), _ptr(src), rows,
                                     y.data_ptr(), yt, ys, _stream()), "hatq_experts_int8")
     return y
 
 
-@_on_stream
 def hatq_experts_forward(lin: PreparedLinear, x: torch.Tensor, ends: torch.Tensor,
                          src: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
-                         y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+                         y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """hatq_experts_int8 of tokens x [x_rows, cin], each quantized once."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_experts_forward(lin, x, ends, src, out_dtype, y, ws)
     n, _, xs, xt = _rows(x, "x", lin.cin)
     rows = _grouping(lin, ends, src, n)
-    y, ys, yt = _out_rows(y, rows, lin.cout, out_dtype or x.dtype, x.device)
-    ws = _linear_ws(lin, n, ws, x.device)
+    y, ys, yt = _out_rows(y, rows, lin.cout, out_dtype or x.dtype, x)
+    ws = _linear_ws(lin, n, ws, x)
     _check(load().hatq_experts_forward(lin.ref, x.data_ptr(), xt, n, xs, ends.data_ptr(), _ptr(src), rows,
                                        y.data_ptr(), yt, ys, ws.data_ptr(), ws.numel(), _stream()),
            "hatq_experts_forward")
     return y
 
 
-@_on_stream
 def hatq_expert_order(ids: torch.Tensor, experts: int, ends: Optional[torch.Tensor] = None,
                       src: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
-                      ws: Optional[torch.Tensor] = None):
+                      ws: Optional[torch.Tensor] = None, stream=None):
     """Chosen experts ids (int32 [tokens, topk]) -> (ends [experts], src [tokens * topk],
     pos [tokens, topk]): the rows of the grouped calls, sorted by expert.  An id outside
     [0, experts) masks its pair (pos -1)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_expert_order(ids, experts, ends, src, pos, ws)
     if ids.dim() != 2:
         raise ValueError(f"ids: [tokens, topk] expected, got shape {tuple(ids.shape)}")
     _need(ids, "ids", torch.int32, 0)
@@ -890,11 +896,14 @@ def hatq_expert_order(ids: torch.Tensor, experts: int, ends: Optional[torch.Tens
     return ends, src, pos
 
 
-@_on_stream
 def hatq_expert_combine(h: torch.Tensor, pos: torch.Tensor, weights: torch.Tensor,
-                        out_dtype: torch.dtype = torch.float32, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+                        out_dtype: torch.dtype = torch.float32, y: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
     """y[t] = sum over j of weights[t, j] h[pos[t, j]]: h fp32 [rows, cols], pos int32 and
     weights fp32 [tokens, topk]; a pos outside the rows adds nothing."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_expert_combine(h, pos, weights, out_dtype, y)
     n, c, hs, ht = _rows(h, "h")
     if ht != 0:
         raise ValueError(f"h: float32 expected, got {h.dtype}")
@@ -903,7 +912,7 @@ def hatq_expert_combine(h: torch.Tensor, pos: torch.Tensor, weights: torch.Tenso
     _need(pos, "pos", torch.int32, 0)
     _need(weights, "weights", torch.float32, 0)
     t, k = pos.shape
-    y, ys, yt = _out_rows(y, t, c, out_dtype, h.device)
+    y, ys, yt = _out_rows(y, t, c, out_dtype, h)
     _check(load().hatq_expert_combine(h.data_ptr(), n, c, hs, pos.data_ptr(), weights.data_ptr(), t, k, y.data_ptr(),
                                       yt, ys, _stream()), "hatq_expert_combine")
     return y
@@ -913,18 +922,20 @@ def hatq_expert_mlp_ws_bytes(w_in: PreparedLinear, w_out: PreparedLinear, tokens
     return int(load().hatq_expert_mlp_ws_bytes(w_in.ref, w_out.ref, tokens, topk))
 
 
-@_on_stream
 def hatq_expert_mlp(w_in: PreparedLinear, w_out: PreparedLinear, x: torch.Tensor, ids: torch.Tensor,
                     weights: torch.Tensor, out_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None,
-                    ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Tokens x [tokens, cin] through their chosen gated experts, ids int32 and weights
     fp32 [tokens, topk]: y [tokens, cout] of out_dtype (default: x's)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_expert_mlp(w_in, w_out, x, ids, weights, out_dtype, y, ws)
     n, _, xs, xt = _rows(x, "x", w_in.cin)
     if ids.dim() != 2 or ids.shape[0] != n or weights.shape != ids.shape:
         raise ValueError(f"ids, weights: [{n}, topk] expected, got {tuple(ids.shape)}, {tuple(weights.shape)}")
     _need(ids, "ids", torch.int32, 0)
     _need(weights, "weights", torch.float32, 0)
-    y, ys, yt = _out_rows(y, n, w_out.cout, out_dtype or x.dtype, x.device)
+    y, ys, yt = _out_rows(y, n, w_out.cout, out_dtype or x.dtype, x)
     topk = ids.shape[1]
     if ws is None:
         ws = torch.empty(max(hatq_expert_mlp_ws_bytes(w_in, w_out, n, topk), 256), dtype=torch.int8, device=x.device)
