@@ -107,14 +107,14 @@ __device__ __forceinline__ float gated_unit(float g, float u) {
     return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
 }
 
-// z of four adjacent packed columns with factors at w_scale and bias (memory or LDS).
-__device__ __forceinline__ void dequant4(const LinearArgs &a, const float *w_scale, const float *bias, const int *acc,
-                                         float s, float *z) {
+// z of four adjacent packed columns with factors at w_scale and bias (memory or LDS); s =
+// the token's scale times 1/b, a power of two, so s w is fl(s_token w) / b.
+__device__ __forceinline__ void dequant4(const float *w_scale, const float *bias, const int *acc, float s, float *z) {
     const float4 w = *reinterpret_cast<const float4 *>(w_scale), b = *reinterpret_cast<const float4 *>(bias);
-    z[0] = __builtin_fmaf((float)acc[0], s * w.x * a.inv_b, b.x);
-    z[1] = __builtin_fmaf((float)acc[1], s * w.y * a.inv_b, b.y);
-    z[2] = __builtin_fmaf((float)acc[2], s * w.z * a.inv_b, b.z);
-    z[3] = __builtin_fmaf((float)acc[3], s * w.w * a.inv_b, b.w);
+    z[0] = __builtin_fmaf((float)acc[0], s * w.x, b.x);
+    z[1] = __builtin_fmaf((float)acc[1], s * w.y, b.y);
+    z[2] = __builtin_fmaf((float)acc[2], s * w.z, b.z);
+    z[3] = __builtin_fmaf((float)acc[3], s * w.w, b.w);
 }
 
 template <typename T>
@@ -160,7 +160,7 @@ __device__ __forceinline__ void finish16(const LinearArgs &a, const float *w_sca
 #pragma unroll
     for (int g = 0; g < G; ++g) {
         const int q[4] = {sum[g][0], sum[g][1], sum[g][2], sum[g][3]};
-        dequant4(a, w_scale + p + 32 * g, bias + p + 32 * g, q, scale, z[g]);
+        dequant4(w_scale + p + 32 * g, bias + p + 32 * g, q, scale, z[g]);
     }
     if (G == 2) {
 #pragma unroll
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
     for (int m = 0; m < MT; ++m) {
         const int tok = token_of(a, r.row0 + min(16 * m + (lane & 15), rows - 1));
         x[m] = a.xq + (int64_t)max(tok, 0) * a.k_stride + (lane >> 4) * 16;
-        s[m] = tok < 0 ? 0.0f : a.sx[tok];
+        s[m] = tok < 0 ? 0.0f : a.sx[tok] * a.inv_b;
     }
     v4i acc[MT][G];
 #pragma unroll
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
                 for (int k = 1; k < wk; ++k) sum += part[wave - first + k][m][g][lane];
             }
             const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
-            dequant4(a, w_scale + p + 32 * g, bias + p + 32 * g, q, s[m], z[g]);
+            dequant4(w_scale + p + 32 * g, bias + p + 32 * g, q, s[m], z[g]);
         }
         if (G == 2) {
 #pragma unroll
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) m = __builtin_elementwise_maximum(m, most[k]);
         const float s = token_scale(m);
-        if (threadIdx.x == 0) scale[row] = s;
+        if (threadIdx.x == 0) scale[row] = s * a.inv_b;
         store_chunks<CH, 512>(codes + row * pitch, a.k_stride, threadIdx.x, v, sigma, s);
     }
     __syncthreads();
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, c
         if (row >= rows) break;
         const float sigma = token_butterfly(v[i], lane, x.log_b);
         const float s = token_scale(token_max(v[i]));
-        if (lane == 0) scale[row] = s;
+        if (lane == 0) scale[row] = s * a.inv_b;
         store_chunks<CH, 64>(codes + row * pitch, a.k_stride, lane, v[i], sigma, s);
     }
     __syncthreads();
@@ -477,27 +477,41 @@ __device__ __forceinline__ TileIndex tile_index(int bid, int tiles_m, int tiles_
 // pieces, so a store instruction writes whole runs of rows.  PARTS waves share the rows.
 template <typename T, int COLS, int PARTS>
 __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0, int rows, int c0, int lane, int part) {
-    constexpr int E = 16 / sizeof(T), PER = COLS / E;   // elements of a piece, pieces of a row
+    constexpr int E = 16 / sizeof(T), PER = COLS / E;     // elements of a piece, pieces of a row
+    constexpr int STEP = 64 / PER, PIECES = 32 / STEP;    // rows that a wave's piece covers, such pieces
     if (c0 >= a.cout) return;
-    T *y = static_cast<T *>(a.y);
-    const bool vec = (reinterpret_cast<uintptr_t>(y) & 15) == 0 && (a.y_stride & (E - 1)) == 0;
-#pragma unroll
-    for (int k = 0; k < (32 * PER / 64 + PARTS - 1) / PARTS; ++k) {
-        const int u = k * PARTS + part;
-        if (u >= 32 * PER / 64) break;
-        const int r = (u * 64 + lane) / PER, c = lane % PER * E;
-        float z[E];
+    const int r0 = lane / PER, c = lane % PER * E;
+    T *to = static_cast<T *>(a.y) + (row0 + r0) * a.y_stride + c0 + c;
+    from += r0 * (COLS + 4) + c;
+    const int64_t step = STEP * a.y_stride;
+    auto piece = [&](int u, float *z) {
 #pragma unroll
         for (int e = 0; e < E; e += 4)
-            *reinterpret_cast<float4 *>(z + e) = *reinterpret_cast<const float4 *>(from + r * (COLS + 4) + c + e);
-        if (r >= rows) continue;
-        T *to = y + (row0 + r) * a.y_stride + c0 + c;
-        if (vec && c0 + c + E <= a.cout) {
+            *reinterpret_cast<float4 *>(z + e) = *reinterpret_cast<const float4 *>(from + u * STEP * (COLS + 4) + e);
+    };
+    const bool vec = (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && (a.y_stride & (E - 1)) == 0;
+    if (vec && c0 + COLS <= a.cout && rows >= 32 && PIECES % PARTS == 0) {
+        to += part * step;
+#pragma unroll
+        for (int k = 0; k < PIECES / PARTS; ++k) {
+            float z[E];
+            piece(k * PARTS + part, z);
             store16(to, z);
+            to += PARTS * step;
+        }
+        return;
+    }
+    for (int u = part; u < PIECES; u += PARTS) {
+        if (u * STEP + r0 >= rows) continue;
+        float z[E];
+        piece(u, z);
+        T *at = to + u * step;
+        if (vec && c0 + c + E <= a.cout) {
+            store16(at, z);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (c0 + c + e < a.cout) to[e] = from_float<T>(z[e]);
+                if (c0 + c + e < a.cout) at[e] = from_float<T>(z[e]);
         }
     }
 }
@@ -555,7 +569,7 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int tok = token_of(a, r.row0 + min((wm * FM + i) * 32 + (lane & 31), rows - 1));
-        scale[i] = tok < 0 ? 0.0f : a.sx[tok];
+        scale[i] = tok < 0 ? 0.0f : a.sx[tok] * a.inv_b;
     }
     // this group's steps: `nks` of them from k0, in a loop of `turns` for every group
     const int steps = a.k_stride >> 6, turns = (steps + KG - 1) / KG;
@@ -688,7 +702,7 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
                 for (int g = 0; g < G; ++g) {
                     const int v[4] = {acc[j + g][i][4 * u], acc[j + g][i][4 * u + 1], acc[j + g][i][4 * u + 2],
                                       acc[j + g][i][4 * u + 3]};
-                    dequant4(a, reinterpret_cast<const float *>(f + 8 * g), reinterpret_cast<const float *>(f + BN / 4 + 8 * g), v,
+                    dequant4(reinterpret_cast<const float *>(f + 8 * g), reinterpret_cast<const float *>(f + BN / 4 + 8 * g), v,
                              scale[i], z[g]);
                 }
                 if (G == 2) {
