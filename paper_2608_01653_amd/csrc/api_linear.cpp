@@ -211,7 +211,9 @@ int32_t check_mlp(const hatq_linear_weights *W_in, const hatq_linear_weights *W_
 }
 
 // hatq_expert_mlp's workspace: ends (at 0), src, pos, the order's own, hidden and output
-// rows, and the codes of one layer at a time.  bytes = 0 for sizes that are not supported.
+// rows, and the codes of one layer at a time.  Where the hidden rows become codes before
+// the second product starts, the output rows take their place (less memory, and lines
+// that the memory-side cache still holds).  bytes = 0 for sizes that are not supported.
 struct MlpPlaces {
     size_t src, pos, order, hidden, rows, scratch, bytes;
 };
@@ -219,14 +221,18 @@ MlpPlaces mlp_places(const hatq_linear_weights *W_in, const hatq_linear_weights 
     MlpPlaces p{};
     const size_t order = hatq_expert_order_ws_bytes(tokens, topk, W_in->experts);
     if (order == 0 || tokens <= 0) return p;
-    const size_t pairs = (size_t)tokens * topk;
+    const int32_t pairs = tokens * topk;
+    const size_t hidden = align256((size_t)pairs * W_in->cout * 4), rows = align256((size_t)pairs * W_out->cout * 4);
+    static const int32_t grouped = 0;   // (any ends: the choice of kernels does not read them)
+    const bool reads_hidden = hatq::linear_takes_tokens(
+        product_args(W_out, nullptr, nullptr, pairs, &grouped, nullptr, pairs, nullptr, HATQ_F32, W_out->cout));
     p.src = align256((size_t)W_in->experts * 4);
-    p.pos = p.src + align256(pairs * 4);
-    p.order = p.pos + align256(pairs * 4);
+    p.pos = p.src + align256((size_t)pairs * 4);
+    p.order = p.pos + align256((size_t)pairs * 4);
     p.hidden = p.order + order;
-    p.rows = p.hidden + align256(pairs * W_in->cout * 4);
-    p.scratch = p.rows + align256(pairs * W_out->cout * 4);
-    const size_t in = hatq_linear_ws_bytes(W_in, tokens), out = hatq_linear_ws_bytes(W_out, (int32_t)pairs);
+    p.rows = reads_hidden ? p.hidden + hidden : p.hidden;
+    p.scratch = p.rows + (reads_hidden || rows > hidden ? rows : hidden);
+    const size_t in = hatq_linear_ws_bytes(W_in, tokens), out = hatq_linear_ws_bytes(W_out, pairs);
     p.bytes = p.scratch + (in > out ? in : out);
     return p;
 }
