@@ -459,8 +459,9 @@ int32_t hatq_layer_forward(const hatq_weights *W, int32_t form, const float *x, 
  * call with no rows is HATQ_OK and launches nothing, one of more than 2^24 rows
  * HATQ_EUNSUPPORTED.  x and y may have any
  * alignment of their type (rows at multiples of 16 bytes are read and written
- * faster); codes and prepared weights are 16-byte aligned.  No kernel's result
- * depends on the order in which blocks run. */
+ * faster); codes and prepared weights are 16-byte aligned.  Outputs and the
+ * workspace do not overlap the inputs.  No kernel's result depends on the order in
+ * which blocks run. */
 typedef enum { HATQ_F32 = 0, HATQ_BF16 = 1, HATQ_F16 = 2 } hatq_dtype;
 
 /* Prepared linear weights: a plain view into the caller's device buffer.

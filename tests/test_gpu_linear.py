@@ -246,6 +246,77 @@ def test_product(rows, cin, cout, gated):
     assert_close(y.view, ref, err, torch.float32)
 
 
+# Shapes that take each of the kernels, at their edges: the sums stay below 2^24, so that
+# with scales of 1 and no bias float32 outputs are the integers themselves.
+LARGE = [(20, 8192, 100), (45, 2048, 4100), (65, 4096, 1030), (129, 16384, 200), (190, 4096, 4097), (385, 4032, 2050), (515, 4096, 4096),
+         (1025, 4096, 2100), (1000, 1000, 6000), (2050, 4096, 4100), (4097, 1088, 4100), (9000, 320, 700), (6145, 2048, 1300),
+         (70001, 64, 40)]
+
+
+def exact_sums(q, codes):
+    """q codes^T on the device, exact: integers below 2^53 in float64."""
+    return q.double() @ codes.double().t().contiguous()
+
+
+@pytest.mark.parametrize("rows,cin,cout", LARGE)
+def test_product_large(rows, cin, cout):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    lim = max(1, int((2 ** 24 / cin) ** 0.5) - 1)
+    codes = torch.randint(-lim, lim + 1, (cout, cin), generator=gen, device=DEV).to(torch.int8)
+    lin = hatq.hatq_pack_linear(codes, torch.ones(cout, device=DEV))
+    q = torch.zeros((rows, lin.k_stride), dtype=torch.int8, device=DEV)
+    q[:, :cin] = torch.randint(-lim, lim + 1, (rows, cin), generator=gen, device=DEV)
+    y = Guarded((rows, cout), torch.float32)
+    hatq.hatq_linear_int8(lin, q, torch.ones(rows, device=DEV), y=y.view)
+    y.check()
+    ref = exact_sums(q[:, :cin], codes)
+    assert torch.equal(y.view.double(), ref)
+    # one scale, halves and bfloat16 the same values rounded once; a gated layer its unit
+    for dtype in (torch.float16, torch.bfloat16):
+        got = hatq.hatq_linear_int8(lin, q, torch.full((rows,), 2.0 ** -12, device=DEV), out_dtype=dtype)
+        assert torch.equal(got, (ref * 2.0 ** -12).float().to(dtype))
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(45, 2048, 2050), (190, 4096, 2049), (385, 4032, 1030), (1025, 4096, 1050), (2050, 4096, 2050),
+                                           (4097, 1088, 2050)])
+def test_product_large_gated(rows, cin, cout):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    lim = max(1, int((2 ** 24 / cin) ** 0.5) - 1)
+    codes = torch.randint(-lim, lim + 1, (2 * cout, cin), generator=gen, device=DEV).to(torch.int8)
+    lin = hatq.hatq_pack_linear(codes, torch.full((2 * cout,), 2.0 ** -10, device=DEV), gated=True)
+    q = torch.zeros((rows, lin.k_stride), dtype=torch.int8, device=DEV)
+    q[:, :cin] = torch.randint(-lim, lim + 1, (rows, cin), generator=gen, device=DEV)
+    y = hatq.hatq_linear_int8(lin, q, torch.full((rows,), 2.0 ** -8, device=DEV))
+    z = exact_sums(q[:, :cin], codes) * 2.0 ** -18          # exact in float32 too
+    g, u = z[:, :cout], z[:, cout:]
+    ref = g * torch.sigmoid(g) * u
+    assert bool(((y.double() - ref).abs() <= 2 * (g.abs() + 8) * U * ref.abs() + 2.0 ** -120).all())
+
+
+@pytest.mark.parametrize("e,rows,cin,cout", [(3, 900, 2048, 1030), (40, 3000, 1088, 600), (8, 9001, 2048, 1100), (100, 20000, 576, 520),
+                                             (2, 5000, 4096, 2050), (64, 64, 4096, 130), (16, 700, 2048, 2050), (300, 40000, 128, 100)])
+def test_grouped_large(e, rows, cin, cout):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    rng = np.random.default_rng(rows)
+    lim = max(1, int((2 ** 24 / cin) ** 0.5) - 1)
+    codes = torch.randint(-lim, lim + 1, (e, cout, cin), generator=gen, device=DEV).to(torch.int8)
+    lin = hatq.hatq_pack_linear(codes, torch.ones((e, cout), device=DEV))
+    x_rows = rows // 2 + 1
+    q = torch.zeros((x_rows, lin.k_stride), dtype=torch.int8, device=DEV)
+    q[:, :cin] = torch.randint(-lim, lim + 1, (x_rows, cin), generator=gen, device=DEV)
+    ends = np.cumsum(rng.multinomial(rows - 7, rng.dirichlet(np.full(e, 0.5))))      # seven rows left over
+    src = torch.randint(0, x_rows, (rows,), generator=gen, device=DEV).to(torch.int32)
+    y = Guarded((rows, cout), torch.float32)
+    hatq.hatq_experts_int8(lin, q, torch.ones(x_rows, device=DEV), dev(ends.astype(np.int32)), src, y=y.view)
+    y.check()
+    begin = 0
+    for k, end in enumerate(ends.tolist()):
+        if end > begin:
+            assert torch.equal(y.view[begin:end].double(), exact_sums(q[src[begin:end].long(), :cin], codes[k])), k
+        begin = end
+    assert not bool(y.view[begin:].any())
+
+
 @pytest.mark.parametrize("rows,cout", [(3, 50), (40, 66), (150, 130), (300, 512)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("pad,shift", [(0, 0), (1, 0), (8, 8), (5, 3)])
@@ -321,7 +392,8 @@ def test_forward(rows, cin, cout, b, gated, dtype):
 @pytest.mark.parametrize("rows,cin,cout,b,pad", [
     (1, 1, 1, 1, 0), (1, 64, 16, 64, 0), (2, 500, 40, 4, 1), (16, 512, 33, 128, 0), (9, 640, 20, 128, 8), (16, 1024, 50, 64, 0),
     (1, 1024, 70, 64, 0), (3, 1100, 17, 2, 3), (4, 4096, 64, 128, 0), (3, 4097, 24, 1, 0), (2, 8192, 16, 128, 0), (1, 16384, 40, 128, 0),
-    (1, 16000, 16, 64, 8), (1, 20000, 16, 32, 0), (17, 256, 30, 64, 0)])
+    (1, 16000, 16, 64, 8), (1, 20000, 16, 32, 0), (17, 256, 30, 64, 0), (300, 320, 200, 64, 0), (9001, 192, 70, 64, 0),
+    (8300, 1000, 24, 8, 1), (33, 1024, 1500, 128, 0)])
 def test_forward_is_its_two_steps(dtype, gated, rows, cin, cout, b, pad):
     """Floats in and codes in give the same bits, whichever kernels a call takes."""
     rng = np.random.default_rng(cin + rows)
