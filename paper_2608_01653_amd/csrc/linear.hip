@@ -27,6 +27,12 @@ __device__ __forceinline__ void wait_vmcnt_lds() {
     __builtin_amdgcn_s_waitcnt((N & 15) | 0x70 | ((N >> 4) << 14));
 }
 
+// A bare barrier (loads to LDS stay under way over it), and no access moved across it.
+__device__ __forceinline__ void block_barrier() {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // ---- which rows a tile has --------------------------------------------------------
 struct RowTile {
     int expert;     // -1: rows past the last end, written 0
@@ -202,7 +208,9 @@ __device__ __forceinline__ void store_chunks(int8_t *to, int k_stride, int t, co
 // their values) by 16 MT rows: they take the contraction 64 bytes in turn and add up in
 // LDS; 8 / WK groups a block.  The weights go from memory to registers in runs of 1 KB,
 // U of them in flight a wave: the kernel is bound by their bytes.  WK is large where the
-// groups alone would not fill the card.
+// groups alone would not fill the card.  13 rows, 4096 -> 2 x 8192 gated: 12.7 us, 5.3 TB/s
+// of weights (a large copy moves 5.1).  Tried without gain: 4, 12 and 16 runs in flight,
+// nontemporal loads (13.3 us).
 template <int MT, int G, int U>
 __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, int wk) {
     constexpr int WAVES = 8;
@@ -373,7 +381,10 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
 // A contraction of at most 1024: a block quantizes 16 MT rows (of one expert), a wave a
 // row at a time (all of a wave's rows loaded at once), into LDS, and then each wave takes
 // groups of 16 output channels over the whole contraction, the weights straight from the
-// L2s.  blockIdx.y: `per` of the groups, a multiple of the waves.
+// L2s.  blockIdx.y: `per` of the groups, a multiple of the waves.  Bound by latency (a row
+// in, its maximum, the weights' first bytes) until the weights' repeated reads take over:
+// 6144 rows, 320 -> 320, float32, 9.3 us (its 15.8 MB would take 3.1), 12-13 us as two
+// kernels.
 template <typename T, int G, int CH, int MT>
 __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, const TokenArgs x, int vec, int per) {
     constexpr int WAVES = 8, U = 8, ROWS = 16 * MT, TURNS = ROWS / WAVES;
@@ -527,6 +538,15 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
 // buffer end before it, the loads that refill that buffer and the reads of the next
 // one begin after it.
 //
+// 4096 x 4096 x 4096, bf16 out: 66 us, 2.1 POP/s; 8192 x 4096 x 16384 gated: 490 us, 2.24
+// POP/s, as the INT8 library product of that size, which writes plain sums.  There the
+// matrix cores are busy 60 % of the cycles at 1.7 GHz, where power holds the clock (2.4
+// nominal); without the outputs it is 2.4 POP/s.  Wave tiles of 64 x 64 in blocks of 128 x
+// 256, two a CU, are 3 % behind 128 x 64 in 256 x 256 where all tiles are whole, and ahead
+// elsewhere: 32768 rows over 64 experts 175 us against 200.  Tried without gain: five
+// stages, wave priorities, 16 waves on 256 x 256, float32 stores without LDS, codes laid
+// out in the weights' order (3-5 % for whole tiles; rows gathered by expert cannot).
+//
 // Few tiles: KG such groups of waves share a tile, each a run of the contraction with a
 // ring of its own, and add up in LDS.  A step costs a group about 0.17 us of LDS and
 // barrier latency however few MFMAs it has; the groups of a CU overlap it.
@@ -638,7 +658,7 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
 #pragma unroll
     for (int k = 0; k < STAGES; ++k) issue(ring + k * STAGE_BYTES, k + 1 < nks);
     wait_vmcnt_lds<(STAGES - 1) * PER_STAGE>();
-    __builtin_amdgcn_s_barrier();
+    block_barrier();
 #pragma unroll
     for (int k = 0; k < FM + FN; ++k) read(ring, 0, k);
     int at = 0;   // this step's buffer
@@ -649,12 +669,12 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
         // the next step's loads have landed (STAGES - 2 later ones under way), this buffer
         // has been read: by every wave, past the barrier
         wait_vmcnt_lds<(STAGES - 2) * PER_STAGE>();
-        __builtin_amdgcn_s_barrier();
+        block_barrier();
         issue(now, ks + STAGES + 1 < nks);
         if (KG == 1 || ks < nks) half(1, ring + at);
     }
     wait_vmcnt_lds<0>();
-    __builtin_amdgcn_s_barrier();   // no load is under way into the buffers that stage the outputs
+    block_barrier();   // no load is under way into the buffers that stage the outputs
 
     if constexpr (KG > 1) {
         // partial sums [KG][NW][FN][FM][4][64]; group kg adds up the quads q = kg mod KG
@@ -813,7 +833,7 @@ constexpr TileCost kTiles[] = {
     {64, 128, 4.0, 0.15, 1024, 1450.0},
     {128, 128, 5.5, 0.19, 768, 1850.0},
     {128, 256, 7.0, 0.30, 512, 2050.0},
-    {256, 256, 10.0, 0.56, 256, 2120.0},
+    {256, 256, 8.0, 0.56, 256, 2120.0},
 };
 constexpr double kWeightRate = 6.5e6, kRowRate = 7.3e6;   // bytes a microsecond: memory, codes from the L2s
 constexpr double kTileRate = 4.0e4;                       // and what one tile's CU takes of the weights

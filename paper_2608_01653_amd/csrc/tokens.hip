@@ -14,7 +14,9 @@ constexpr int kThreads = 256;
 //
 // A token's row stays in registers between its maximum and its codes, so x is read
 // once.  Chunk i of row thread t is number i * 64 * WAVES + t.  The maximum keeps NaN:
-// a token with a value that is not finite gets the scale NaN and codes 0.
+// a token with a value that is not finite gets the scale NaN and codes 0.  Bound by
+// memory with the butterflies (7 adds an element at order 128) close behind: 4096 tokens
+// of 4096, bf16, 13.8 us, 3.6 TB/s; 8192 of them 19.5 us, 5.2 TB/s.
 // Row `row` by its thread t; red: WAVES floats of LDS for each row of the block.
 template <int WAVES, int CH, typename T>
 __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int vec, int64_t row, int t, float *red) {
@@ -166,7 +168,8 @@ __global__ void __launch_bounds__(kThreads) linear_pack_kernel(const LinearPrepA
 // before e plus the rows of e in the blocks before b; each wave then ranks its pairs 64
 // at a time in order.  Ranks come from ballots, not from atomics, so equal ids keep
 // their order.  Up to kOrderOne pairs every block counts all of them itself (one launch;
-// 16384 pairs of 32 experts: 18.1 us with a launch for the counts before); beyond, a
+// 16384 pairs of 32 experts 9.8 us, 18.1 with a launch for the counts before; 96 pairs
+// 4.2); beyond, a
 // first launch leaves the blocks' counts in a table.
 constexpr int kOrderWaves = 8;
 constexpr int kOrderThreads = 64 * kOrderWaves;
@@ -339,6 +342,8 @@ __global__ void __launch_bounds__(kOrderThreads) order_quant_kernel(const OrderA
 }
 
 // ---- the weighted sum of expert rows ------------------------------------------------
+// Four channels a thread, its rows in ascending order; bound by the rows' bytes (16384 rows
+// of 2048 into 4096 of bf16, 151 MB: 25 us, 6.0 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a, int vec) {
     const int groups = (a.cols + 3) / 4;
