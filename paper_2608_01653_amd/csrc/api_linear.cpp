@@ -169,7 +169,7 @@ hatq::TokenArgs token_args(const hatq_linear_weights *W, const void *x, int32_t 
     return a;
 }
 
-// One layer's calls that need no workspace: the product's own blocks quantize.
+// One layer's calls that need no workspace: linear_takes_tokens takes all of them.
 bool few_tokens(const hatq_linear_weights *W, int32_t rows) {
     return rows <= HATQ_TOKEN_ROWS && (int64_t)rows * W->k_stride <= HATQ_TOKEN_CODES;
 }
@@ -184,6 +184,7 @@ int32_t enqueue(const hatq_linear_weights *W, const void *x, int32_t x_type, int
     const hatq::TokenArgs t = token_args(W, x, x_type, x_rows, x_stride, xq, sx);
     const hatq::LinearArgs a = product_args(W, xq, sx, x_rows, ends, src, rows, y, y_type, y_stride);
     if (hatq::linear_takes_tokens(a)) return hip_status(hatq::launch_linear_tokens(a, t, st));
+    if (!ws) return HATQ_EINVAL;
     if (hatq::launch_token_quant(t, st) != hipSuccess) return HATQ_EHIP;
     return hip_status(hatq::launch_linear(a, st));
 }

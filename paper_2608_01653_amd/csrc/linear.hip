@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
 }
 
 // ---- small layers, floats in ------------------------------------------------------------
-// A contraction of at most 1024: a block quantizes 16 MT rows (of one expert), a wave a
+// A contraction of at most 2048: a block quantizes 16 MT rows (of one expert), a wave a
 // row at a time (all of a wave's rows loaded at once), into LDS, and then each wave takes
 // groups of 16 output channels over the whole contraction, the weights straight from the
 // L2s.  blockIdx.y: `per` of the groups, a multiple of the waves.  Bound by latency (a row
@@ -777,6 +777,8 @@ void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     const bool two = !a.ends && a.rows > 8192;
     if (a.k_stride <= 512) two ? small<T, 1, 2>(a, x, vec, st) : small<T, 1, 1>(a, x, vec, st);
     else if (a.k_stride <= 1024) two ? small<T, 2, 2>(a, x, vec, st) : small<T, 2, 1>(a, x, vec, st);
+    else if (a.k_stride <= 2048 && (a.ends || (int64_t)a.rows * a.k_stride > HATQ_TOKEN_CODES || a.rows > HATQ_TOKEN_ROWS))
+        small<T, 4, 1>(a, x, vec, st);
     else if (a.k_stride <= 4096) token<T, 1>(a, x, vec, st);
     else if (a.k_stride <= 8192) token<T, 2>(a, x, vec, st);
     else token<T, 4>(a, x, vec, st);
@@ -803,13 +805,16 @@ double met_tiles(const LinearArgs &a, int bm) {
 // few, or cheap against the codes' way through memory.  (us, two kernels and one.  bf16:
 // 320 -> 320, 6144 rows 12.0 and 8.9; 512 -> 2048, 1024 rows 9.7 and 8.9, 2048 rows 11.9
 // and 13.0; 1024 -> 256, 6144 rows 15.6 and 13.2; 1024 -> 4096, 128 rows 9.2 and 8.5, 512
-// rows 11.7 and 13.4.  Float32, 32 experts of 512 -> 1024, 96 rows 8.1 and 6.0, 384 rows
-// 10.0 and 7.3, 768 rows 10.4 and 11.5; 16 of 1024 -> 2048, 192 rows 13.4 and 12.1, 384
-// rows 13.4 and 17.0; 8 of 320 -> 320, 8192 rows 15.8 and 12.3.)
+// rows 11.7 and 13.4.)  By expert, while a tile of 16 rows is mostly all that an expert
+// has.  (Float32: 32 experts of 512 -> 1024, 96 rows 8.1 and 6.0, 384 rows 10.0 and 7.3, 768
+// rows 10.4 and 11.5; 64 of 2048 -> 1024, 48 rows 16.2 and 14.2, 768 rows 30.8 and 29.5,
+// 1536 rows 32.1 and 48.9; 8 of 320 -> 320, 1536 rows 8.7 and 7.4.)
 bool linear_takes_tokens(const LinearArgs &a) {
     if (!a.ends && a.rows <= HATQ_TOKEN_ROWS && (int64_t)a.rows * a.k_stride <= HATQ_TOKEN_CODES) return true;
-    const double most = a.ends ? 8e8 : a.cout_pad <= 512 ? 5e9 : 1.2e9;
-    return a.k_stride <= 1024 && met_tiles(a, 16) * 16.0 * a.k_stride * a.cout_pad <= most;
+    const double work = met_tiles(a, 16) * 16.0 * a.k_stride * a.cout_pad;
+    if (a.ends) return a.k_stride <= 2048 && (work <= 4e8 || a.rows <= 12 * (int64_t)a.experts);
+    // (1024 to 2048: level in time, with a launch less: 2048 -> 1024, 96 rows 9.1 and 8.8)
+    return a.k_stride <= 2048 && work <= (a.k_stride > 1024 ? 4e8 : a.cout_pad <= 512 ? 5e9 : 1.2e9);
 }
 
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {

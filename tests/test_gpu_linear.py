@@ -393,7 +393,7 @@ def test_forward(rows, cin, cout, b, gated, dtype):
     (1, 1, 1, 1, 0), (1, 64, 16, 64, 0), (2, 500, 40, 4, 1), (16, 512, 33, 128, 0), (9, 640, 20, 128, 8), (16, 1024, 50, 64, 0),
     (1, 1024, 70, 64, 0), (3, 1100, 17, 2, 3), (4, 4096, 64, 128, 0), (3, 4097, 24, 1, 0), (2, 8192, 16, 128, 0), (1, 16384, 40, 128, 0),
     (1, 16000, 16, 64, 8), (1, 20000, 16, 32, 0), (17, 256, 30, 64, 0), (300, 320, 200, 64, 0), (9001, 192, 70, 64, 0),
-    (8300, 1000, 24, 8, 1), (33, 1024, 1500, 128, 0)])
+    (8300, 1000, 24, 8, 1), (33, 1024, 1500, 128, 0), (20, 2048, 200, 128, 0), (100, 1900, 70, 4, 3), (9, 2048, 40, 64, 0)])
 def test_forward_is_its_two_steps(dtype, gated, rows, cin, cout, b, pad):
     """Floats in and codes in give the same bits, whichever kernels a call takes."""
     rng = np.random.default_rng(cin + rows)
