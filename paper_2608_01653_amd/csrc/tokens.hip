@@ -135,28 +135,32 @@ __global__ void __launch_bounds__(kThreads) linear_prepare_kernel(const LinearPr
     }
 }
 
-// Codes that are there already, 16 of a column at a time.
+// Codes that are there already: a block takes 256 of 16 columns, reads runs of columns and
+// writes runs of the packed order, by way of LDS.
 __global__ void __launch_bounds__(kThreads) linear_pack_kernel(const LinearPrepArgs a) {
-    const int p = blockIdx.x, e = blockIdx.y, ch = held_channel(a, p);
+    __shared__ v4i tile[16][17];
+    const int e = blockIdx.z, column = threadIdx.x >> 4, chunk = threadIdx.x & 15;
+    const int p = blockIdx.y * 16 + column, c = blockIdx.x * 16 + chunk, ch = held_channel(a, p);
     const int64_t row = (int64_t)e * (a.gated ? 2 * a.cout : a.cout) + ch;
-    const int8_t *from = a.codes + row * a.cin;
+    const int8_t *from = a.codes + row * a.cin + c * 16;
     const bool whole = (reinterpret_cast<uintptr_t>(a.codes) & 15) == 0 && a.cin % 16 == 0;
-    int8_t *out = a.wpack + ((int64_t)e * a.cout_pad + (p & ~15)) * a.k_stride + (p & 15) * 16;
-    for (int c = threadIdx.x; c < a.k_stride >> 4; c += kThreads) {
-        v4i q = {0, 0, 0, 0};
-        if (ch >= 0) {
-            if (whole) {
-                if (c * 16 < a.cin) q = *reinterpret_cast<const v4i *>(from + c * 16);
-            } else {
-                int8_t *b = reinterpret_cast<int8_t *>(&q);
+    v4i q = {0, 0, 0, 0};
+    if (ch >= 0 && c * 16 < a.cin) {
+        if (whole) {
+            q = *reinterpret_cast<const v4i *>(from);
+        } else {
+            int8_t *b = reinterpret_cast<int8_t *>(&q);
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c * 16 + j < a.cin) b[j] = from[c * 16 + j];
-            }
+            for (int j = 0; j < 16; ++j)
+                if (c * 16 + j < a.cin) b[j] = from[j];
         }
-        *reinterpret_cast<v4i *>(out + (int64_t)(c >> 2) * 1024 + (c & 3) * 256) = q;
     }
-    if (threadIdx.x == 0) {
+    tile[chunk][column] = q;
+    __syncthreads();
+    const int to = blockIdx.x * 16 + column;   // the chunk that this thread writes, of column `chunk`
+    int8_t *out = a.wpack + ((int64_t)e * a.cout_pad + blockIdx.y * 16) * a.k_stride;
+    if (to < a.k_stride >> 4) *reinterpret_cast<v4i *>(out + (int64_t)to * 256 + chunk * 16) = tile[column][chunk];
+    if (blockIdx.x == 0 && chunk == 0) {
         a.w_scale[(int64_t)e * a.cout_pad + p] = ch >= 0 ? a.scale_in[row] : 0.0f;
         a.bias[(int64_t)e * a.cout_pad + p] = ch >= 0 && a.bias_in ? a.bias_in[row] : 0.0f;
     }
@@ -401,7 +405,8 @@ hipError_t launch_token_quant(const TokenArgs &a, hipStream_t st) {
 
 hipError_t launch_linear_prepare(const LinearPrepArgs &a, hipStream_t st) {
     const dim3 grid(a.cout_pad, a.experts);
-    if (a.codes) linear_pack_kernel<<<grid, kThreads, 0, st>>>(a);
+    if (a.codes)
+        linear_pack_kernel<<<dim3((a.k_stride + 255) / 256, a.cout_pad / 16, a.experts), kThreads, 0, st>>>(a);
     else if (a.w_type == kBf16) linear_prepare_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a);
     else if (a.w_type == kF16) linear_prepare_kernel<_Float16><<<grid, kThreads, 0, st>>>(a);
     else linear_prepare_kernel<float><<<grid, kThreads, 0, st>>>(a);
