@@ -124,9 +124,9 @@ __device__ __forceinline__ void dequant4(const float *w_scale, const float *bias
 }
 
 template <typename T>
-__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z, bool vec) {
+__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z) {
     T *y = static_cast<T *>(a.y) + row * a.y_stride + c;
-    if (vec && c + 4 <= a.cout) {
+    if (c + 4 <= a.cout) {
         store4(y, z);
     } else {
 #pragma unroll
@@ -134,25 +134,19 @@ __device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, co
             if (c + j < a.cout) y[j] = from_float<T>(z[j]);
     }
 }
-__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z, bool vec) {
-    if (a.y_type == kBf16) put4<bf16_t>(a, row, c, z, vec);
-    else if (a.y_type == kF16) put4<_Float16>(a, row, c, z, vec);
-    else put4<float>(a, row, c, z, vec);
-}
-
-__device__ __forceinline__ bool vector_rows(const LinearArgs &a) {
-    const int size = a.y_type == kF32 ? 4 : 2;
-    return (reinterpret_cast<uintptr_t>(a.y) & (4 * size - 1)) == 0 && (a.y_stride & 3) == 0;
+__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z) {
+    if (a.y_type == kBf16) put4<bf16_t>(a, row, c, z);
+    else if (a.y_type == kF16) put4<_Float16>(a, row, c, z);
+    else put4<float>(a, row, c, z);
 }
 
 // Rows of a tile past the last end: BN outputs each of zeros.
 __device__ void zero_tile(const LinearArgs &a, int row0, int rows, int c0, int cols) {
     const float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const bool vec = vector_rows(a);
     const int groups = cols / 4;
     for (int u = threadIdx.x; u < rows * groups; u += blockDim.x) {
         const int r = u / groups, c = c0 + (u - r * groups) * 4;
-        if (c < a.cout) put4(a, row0 + r, c, z, vec);
+        if (c < a.cout) put4(a, row0 + r, c, z);
     }
 }
 
@@ -172,18 +166,18 @@ __device__ __forceinline__ void finish16(const LinearArgs &a, const float *w_sca
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
     }
-    if (row < end && c < a.cout) put4(a, row, c, z[0], vector_rows(a));
+    if (row < end && c < a.cout) put4(a, row, c, z[0]);
 }
 
 // A token's chunks of 8 elements, number i * THREADS + t, and their codes in LDS.
 template <typename T, int CH, int THREADS>
-__device__ __forceinline__ void load_chunks(const TokenArgs &x, int row, int t, int vec, float (&v)[8 * CH]) {
+__device__ __forceinline__ void load_chunks(const TokenArgs &x, int row, int t, float (&v)[8 * CH]) {
     const T *p = static_cast<const T *>(x.x) + max(row, 0) * x.x_stride;
     const int n = row < 0 ? 0 : x.cin;   // (an empty token is all zeros)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int e = (i * THREADS + t) * 8;
-        if (vec && e + 8 <= n) {
+        if (e + 8 <= n) {
             load8(p + e, &v[8 * i]);
         } else {
 #pragma unroll
@@ -270,7 +264,6 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
             for (int g = 0; g < G; ++g) part[wave][m][g][lane] = acc[m][g];
         __syncthreads();
     }
-    const bool vec = vector_rows(a);
     const float *w_scale = a.w_scale + (int64_t)r.expert * a.cout_pad, *bias = a.bias + (int64_t)r.expert * a.cout_pad;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -292,7 +285,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
             for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
         }
         const int row = 16 * m + (lane & 15), c = c16 * 16 + (lane >> 4) * 4;
-        if (row < rows && c < a.cout && c16 == g0 + wave / wk) put4(a, r.row0 + row, c, z[0], vec);
+        if (row < rows && c < a.cout && c16 == g0 + wave / wk) put4(a, r.row0 + row, c, z[0]);
     }
 }
 
@@ -303,7 +296,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
 // then the contraction of 16 output channels.  One launch instead of two, and no codes
 // in memory.
 template <typename T, int G, int CH>
-__global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, const TokenArgs x, int vec) {
+__global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, const TokenArgs x) {
     constexpr int WAVES = 8, U = 8;
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     v4i(*part)[G][64] = reinterpret_cast<v4i(*)[G][64]>(lds);                // [WAVES][G][64]
@@ -315,7 +308,7 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     const int pitch = a.k_stride + 16;   // 16 rows' pieces then lie in different banks
 
     float v[8 * CH];
-    load_chunks<T, CH, 512>(x, 0, threadIdx.x, vec, v);
+    load_chunks<T, CH, 512>(x, 0, threadIdx.x, v);
 
     const int nks = a.k_stride >> 6;
     const int block0 = G == 1 ? c16 : (c16 >> 1) * 4 + (c16 & 1);   // of 16 packed columns
@@ -333,7 +326,7 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
 
     for (int row = 0; row < rows; ++row) {
-        if (row) load_chunks<T, CH, 512>(x, row, threadIdx.x, vec, v);
+        if (row) load_chunks<T, CH, 512>(x, row, threadIdx.x, v);
         const float sigma = token_butterfly(v, lane, x.log_b);
         float m = token_max(v);
         if (row) __syncthreads();   // the row before has been read
@@ -386,7 +379,7 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
 // 6144 rows, 320 -> 320, float32, 9.3 us (its 15.8 MB would take 3.1), 12-13 us as two
 // kernels.
 template <typename T, int G, int CH, int MT>
-__global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, const TokenArgs x, int vec, int per) {
+__global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, const TokenArgs x, int per) {
     constexpr int WAVES = 8, U = 8, ROWS = 16 * MT, TURNS = ROWS / WAVES;
     __shared__ __attribute__((aligned(16))) int8_t codes[ROWS * (512 * CH + 16)];
     __shared__ float scale[ROWS];
@@ -404,7 +397,7 @@ __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, c
     float v[TURNS][8 * CH];
 #pragma unroll
     for (int i = 0; i < TURNS; ++i)
-        if (wave + WAVES * i < rows) load_chunks<T, CH, 64>(x, token_of(a, row0 + wave + WAVES * i), lane, vec, v[i]);
+        if (wave + WAVES * i < rows) load_chunks<T, CH, 64>(x, token_of(a, row0 + wave + WAVES * i), lane, v[i]);
 
     const int64_t value = (int64_t)32 * a.k_stride;   // from the gates' columns to the values'
     v4i fw[U][G];
@@ -500,8 +493,7 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
         for (int e = 0; e < E; e += 4)
             *reinterpret_cast<float4 *>(z + e) = *reinterpret_cast<const float4 *>(from + u * STEP * (COLS + 4) + e);
     };
-    const bool vec = (reinterpret_cast<uintptr_t>(a.y) & 15) == 0 && (a.y_stride & (E - 1)) == 0;
-    if (vec && c0 + COLS <= a.cout && rows >= 32 && PIECES % PARTS == 0) {
+    if (c0 + COLS <= a.cout && rows >= 32 && PIECES % PARTS == 0) {
         to += part * step;
 #pragma unroll
         for (int k = 0; k < PIECES / PARTS; ++k) {
@@ -517,7 +509,7 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
         float z[E];
         piece(u, z);
         T *at = to + u * step;
-        if (vec && c0 + c + E <= a.cout) {
+        if (c0 + c + E <= a.cout) {
             store16(at, z);
         } else {
 #pragma unroll
@@ -750,38 +742,37 @@ void stream(const LinearArgs &a, hipStream_t st, int wk) {
 }
 
 template <typename T, int CH>
-void token(const LinearArgs &a, const TokenArgs &x, int vec, hipStream_t st) {
+void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     const int grid = (a.cout + 15) / 16;
     const size_t bytes = 8 * (a.gated ? 2 : 1) * 1024 + 128 + (size_t)a.rows * (a.k_stride + 16);
-    if (a.gated) linear_token_kernel<T, 2, CH><<<grid, 512, bytes, st>>>(a, x, vec);
-    else linear_token_kernel<T, 1, CH><<<grid, 512, bytes, st>>>(a, x, vec);
+    if (a.gated) linear_token_kernel<T, 2, CH><<<grid, 512, bytes, st>>>(a, x);
+    else linear_token_kernel<T, 1, CH><<<grid, 512, bytes, st>>>(a, x);
 }
 
 template <typename T, int CH, int MT>
-void small(const LinearArgs &a, const TokenArgs &x, int vec, hipStream_t st) {
+void small(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     // as few column ranges as fill the card twice: each range quantizes the rows again
     const int groups = (a.cout + 15) / 16, blocks = (int)most_row_tiles(a, 16 * MT);
     int ranges = (groups + 7) / 8;
     if (ranges > (512 + blocks - 1) / blocks) ranges = (512 + blocks - 1) / blocks;
     const int per = ((groups + ranges - 1) / ranges + 7) / 8 * 8;
     const dim3 grid(blocks, (groups + per - 1) / per);
-    if (a.gated) linear_small_kernel<T, 2, CH, MT><<<grid, 512, 0, st>>>(a, x, vec, per);
-    else linear_small_kernel<T, 1, CH, MT><<<grid, 512, 0, st>>>(a, x, vec, per);
+    if (a.gated) linear_small_kernel<T, 2, CH, MT><<<grid, 512, 0, st>>>(a, x, per);
+    else linear_small_kernel<T, 1, CH, MT><<<grid, 512, 0, st>>>(a, x, per);
 }
 
 template <typename T>
 void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
-    const int vec = (reinterpret_cast<uintptr_t>(x.x) & 15) == 0 && x.x_stride * (int)sizeof(T) % 16 == 0;
     // (1024 -> 256, bf16: 16384 rows 20.4 us in tiles of 32 rows, 25.1 of 16; 4096 rows 10.5
     // and 9.8; 320 -> 320, 6144 rows: 16.2 and 8.9)
     const bool two = !a.ends && a.rows > 8192;
-    if (a.k_stride <= 512) two ? small<T, 1, 2>(a, x, vec, st) : small<T, 1, 1>(a, x, vec, st);
-    else if (a.k_stride <= 1024) two ? small<T, 2, 2>(a, x, vec, st) : small<T, 2, 1>(a, x, vec, st);
+    if (a.k_stride <= 512) two ? small<T, 1, 2>(a, x, st) : small<T, 1, 1>(a, x, st);
+    else if (a.k_stride <= 1024) two ? small<T, 2, 2>(a, x, st) : small<T, 2, 1>(a, x, st);
     else if (a.k_stride <= 2048 && (a.ends || (int64_t)a.rows * a.k_stride > HATQ_TOKEN_CODES || a.rows > HATQ_TOKEN_ROWS))
-        small<T, 4, 1>(a, x, vec, st);
-    else if (a.k_stride <= 4096) token<T, 1>(a, x, vec, st);
-    else if (a.k_stride <= 8192) token<T, 2>(a, x, vec, st);
-    else token<T, 4>(a, x, vec, st);
+        small<T, 4, 1>(a, x, st);
+    else if (a.k_stride <= 4096) token<T, 1>(a, x, st);
+    else if (a.k_stride <= 8192) token<T, 2>(a, x, st);
+    else token<T, 4>(a, x, st);
 }
 
 template <int WM, int WN, int FM, int FN, int STAGES, int KG = 1>

@@ -34,15 +34,27 @@ __device__ __forceinline__ _Float16 from_float<_Float16>(float v) { return (_Flo
 template <>
 __device__ __forceinline__ bf16_t from_float<bf16_t>(float v) { return {(uint16_t)bf16_pair(v, v)}; }
 
-// Eight adjacent elements, 16-byte aligned.
+// Vectors at any element's address: the hardware's loads and stores of 8 and 16 bytes need
+// no alignment, so odd row strides and offset views take the same path.  (7075 rows, 512 ->
+// 2198, bf16: the product MEAS.)
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef _Float16 f16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef _Float16 f16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+
+// Four and eight adjacent elements.
+__device__ __forceinline__ void load4(const float *p, float *v) {
+    const f32x4_any a = *reinterpret_cast<const f32x4_any *>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = a[j];
+}
 __device__ __forceinline__ void load8(const float *p, float *v) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    load4(p, v);
+    load4(p + 4, v + 4);
 }
 __device__ __forceinline__ void load8(const bf16_t *p, float *v) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    const u32x4_any w = *reinterpret_cast<const u32x4_any *>(p);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[2 * j] = __uint_as_float(w[j] << 16);
@@ -50,36 +62,32 @@ __device__ __forceinline__ void load8(const bf16_t *p, float *v) {
     }
 }
 __device__ __forceinline__ void load8(const _Float16 *p, float *v) {
-    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-    const v8h h = *reinterpret_cast<const v8h *>(p);
+    const f16x8_any h = *reinterpret_cast<const f16x8_any *>(p);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
 }
 
-// Four adjacent elements, aligned to their size.
 __device__ __forceinline__ void store4(float *p, const float *v) {
-    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<f32x4_any *>(p) = f32x4_any{v[0], v[1], v[2], v[3]};
 }
 __device__ __forceinline__ void store4(bf16_t *p, const float *v) {
-    *reinterpret_cast<uint2 *>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    *reinterpret_cast<u32x2_any *>(p) = u32x2_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
 }
 __device__ __forceinline__ void store4(_Float16 *p, const float *v) {
-    typedef _Float16 v4h __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<v4h *>(p) = v4h{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+    *reinterpret_cast<f16x4_any *>(p) = f16x4_any{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
 }
 
 // One 16-byte piece.
 __device__ __forceinline__ void store16(float *p, const float *v) { store4(p, v); }
 __device__ __forceinline__ void store16(bf16_t *p, const float *v) {
-    *reinterpret_cast<uint4 *>(p) =
-        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    *reinterpret_cast<u32x4_any *>(p) =
+        u32x4_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
 }
 __device__ __forceinline__ void store16(_Float16 *p, const float *v) {
-    typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-    v8h h;
+    f16x8_any h;
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[j] = (_Float16)v[j];
-    *reinterpret_cast<v8h *>(p) = h;
+    *reinterpret_cast<f16x8_any *>(p) = h;
 }
 
 // Inclusive scans over the wave, of values >= 0, by DPP moves: rows of 16 lanes, then

@@ -19,7 +19,7 @@ constexpr int kThreads = 256;
 // of 4096, bf16, 13.8 us, 3.6 TB/s; 8192 of them 19.5 us, 5.2 TB/s.
 // Row `row` by its thread t; red: WAVES floats of LDS for each row of the block.
 template <int WAVES, int CH, typename T>
-__device__ __forceinline__ void token_quant_row(const TokenArgs &a, int vec, int64_t row, int t, float *red) {
+__device__ __forceinline__ void token_quant_row(const TokenArgs &a, int64_t row, int t, float *red) {
     constexpr int RT = 64 * WAVES;   // threads of a row
     const bool in = row < a.rows;    // (a block of several waves a row has a barrier for all)
     if (WAVES == 1 && !in) return;
@@ -30,7 +30,7 @@ __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int vec, int
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int e = (i * RT + t) * 8;
-        if (vec && e + 8 <= a.cin) {
+        if (e + 8 <= a.cin) {
             load8(x + e, &v[8 * i]);
         } else {
 #pragma unroll
@@ -62,25 +62,20 @@ __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int vec, int
 
 // One row a block of WAVES waves, or four of one wave.
 template <int WAVES, int CH, typename T>
-__global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quant_kernel(const TokenArgs a, int vec) {
+__global__ void __launch_bounds__(WAVES == 1 ? kThreads : 64 * WAVES) token_quant_kernel(const TokenArgs a) {
     __shared__ float red[WAVES];
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int64_t row = WAVES == 1 ? block * (kThreads / 64) + (threadIdx.x >> 6) : block;
-    token_quant_row<WAVES, CH, T>(a, vec, row, WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, red);
-}
-
-int vector_rows(const TokenArgs &a) {
-    return (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride * (a.x_type == kF32 ? 4 : 2) % 16 == 0;
+    token_quant_row<WAVES, CH, T>(a, row, WAVES == 1 ? threadIdx.x & 63 : threadIdx.x, red);
 }
 
 template <int WAVES, int CH>
 hipError_t token_launch(const TokenArgs &a, hipStream_t st) {
     const dim3 grid = grid_of(WAVES == 1 ? (a.rows + 3) / 4 : a.rows);
     const int threads = WAVES == 1 ? kThreads : 64 * WAVES;
-    const int vec = vector_rows(a);
-    if (a.x_type == kF32) token_quant_kernel<WAVES, CH, float><<<grid, threads, 0, st>>>(a, vec);
-    else if (a.x_type == kBf16) token_quant_kernel<WAVES, CH, bf16_t><<<grid, threads, 0, st>>>(a, vec);
-    else token_quant_kernel<WAVES, CH, _Float16><<<grid, threads, 0, st>>>(a, vec);
+    if (a.x_type == kF32) token_quant_kernel<WAVES, CH, float><<<grid, threads, 0, st>>>(a);
+    else if (a.x_type == kBf16) token_quant_kernel<WAVES, CH, bf16_t><<<grid, threads, 0, st>>>(a);
+    else token_quant_kernel<WAVES, CH, _Float16><<<grid, threads, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -336,12 +331,11 @@ __global__ void __launch_bounds__(kOrderThreads) order_place_kernel(const OrderA
 // The order of the rows in the first blocks, the codes of the tokens in the rest: neither
 // needs the other.
 template <int WAVES, int CH, typename T>
-__global__ void __launch_bounds__(kOrderThreads) order_quant_kernel(const OrderArgs o, int blocks, const TokenArgs a,
-                                                                    int vec) {
+__global__ void __launch_bounds__(kOrderThreads) order_quant_kernel(const OrderArgs o, int blocks, const TokenArgs a) {
     extern __shared__ int lds[];
     if ((int)blockIdx.x < blocks) return order_place<false>(o, blocks, lds);
     constexpr int ROWS = kOrderThreads / (64 * WAVES);   // of a block
-    token_quant_row<WAVES, CH, T>(a, vec, (blockIdx.x - blocks) * ROWS + threadIdx.x / (64 * WAVES),
+    token_quant_row<WAVES, CH, T>(a, (blockIdx.x - blocks) * ROWS + threadIdx.x / (64 * WAVES),
                                   threadIdx.x % (64 * WAVES), reinterpret_cast<float *>(lds) + threadIdx.x / (64 * WAVES) * WAVES);
 }
 
@@ -349,11 +343,12 @@ __global__ void __launch_bounds__(kOrderThreads) order_quant_kernel(const OrderA
 // Four channels a thread, its rows in ascending order; bound by the rows' bytes (16384 rows
 // of 2048 into 4096 of bf16, 151 MB: 25 us, 6.0 TB/s).
 template <typename T>
-__global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a, int vec) {
+__global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a) {
     const int groups = (a.cols + 3) / 4;
     const int64_t n = (int64_t)a.tokens * groups;
     for (int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x; u < n; u += (int64_t)gridDim.x * kThreads) {
         const int tok = (int)(u / groups), c = (int)(u - (int64_t)tok * groups) * 4;
+        const bool whole = c + 4 <= a.cols;
         const int32_t *pos = a.pos + (int64_t)tok * a.topk;
         const float *wt = a.weights + (int64_t)tok * a.topk;
         float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -362,12 +357,11 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a, 
             if ((unsigned)p >= (unsigned)a.h_rows) continue;
             const float g = wt[j];
             const float *h = a.h + p * a.h_stride + c;
-            if (vec) {
-                const float4 f = *reinterpret_cast<const float4 *>(h);
-                s[0] = __builtin_fmaf(g, f.x, s[0]);
-                s[1] = __builtin_fmaf(g, f.y, s[1]);
-                s[2] = __builtin_fmaf(g, f.z, s[2]);
-                s[3] = __builtin_fmaf(g, f.w, s[3]);
+            if (whole) {
+                float f[4];
+                load4(h, f);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[k] = __builtin_fmaf(g, f[k], s[k]);
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -375,7 +369,7 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineArgs a, 
             }
         }
         T *y = static_cast<T *>(a.y) + tok * a.y_stride + c;
-        if (vec) {
+        if (whole) {
             store4(y, s);
         } else {
 #pragma unroll
@@ -429,12 +423,12 @@ hipError_t launch_expert_order(const OrderArgs &a, hipStream_t st) {
 template <int WAVES, int CH>
 static hipError_t order_quant(const OrderArgs &o, int blocks, const TokenArgs &a, hipStream_t st) {
     constexpr int ROWS = kOrderThreads / (64 * WAVES);
-    const int grid = blocks + (a.rows + ROWS - 1) / ROWS, vec = vector_rows(a);
+    const int grid = blocks + (a.rows + ROWS - 1) / ROWS;
     size_t bytes = sizeof(int) * (2 + kOrderWaves) * o.experts;
     if (bytes < sizeof(float) * kOrderWaves) bytes = sizeof(float) * kOrderWaves;
-    if (a.x_type == kF32) order_quant_kernel<WAVES, CH, float><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a, vec);
-    else if (a.x_type == kBf16) order_quant_kernel<WAVES, CH, bf16_t><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a, vec);
-    else order_quant_kernel<WAVES, CH, _Float16><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a, vec);
+    if (a.x_type == kF32) order_quant_kernel<WAVES, CH, float><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a);
+    else if (a.x_type == kBf16) order_quant_kernel<WAVES, CH, bf16_t><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a);
+    else order_quant_kernel<WAVES, CH, _Float16><<<grid, kOrderThreads, bytes, st>>>(o, blocks, a);
     return hipGetLastError();
 }
 
@@ -453,15 +447,12 @@ hipError_t launch_order_quant(const OrderArgs &o, const TokenArgs &a, hipStream_
 }
 
 hipError_t launch_expert_combine(const CombineArgs &a, hipStream_t st) {
-    const int size = a.y_type == kF32 ? 4 : 2;
-    const int vec = a.cols % 4 == 0 && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0 && a.h_stride % 4 == 0 &&
-                    (reinterpret_cast<uintptr_t>(a.y) & (4 * size - 1)) == 0 && a.y_stride % 4 == 0;
     const int64_t n = (int64_t)a.tokens * ((a.cols + 3) / 4);
     const int64_t blocks = (n + kThreads - 1) / kThreads;
     const int grid = (int)(blocks < 65536 ? blocks : 65536);
-    if (a.y_type == kF32) combine_kernel<float><<<grid, kThreads, 0, st>>>(a, vec);
-    else if (a.y_type == kBf16) combine_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a, vec);
-    else combine_kernel<_Float16><<<grid, kThreads, 0, st>>>(a, vec);
+    if (a.y_type == kF32) combine_kernel<float><<<grid, kThreads, 0, st>>>(a);
+    else if (a.y_type == kBf16) combine_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a);
+    else combine_kernel<_Float16><<<grid, kThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
