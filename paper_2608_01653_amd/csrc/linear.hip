@@ -541,7 +541,9 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
 //
 // Few tiles: KG such groups of waves share a tile, each a run of the contraction with a
 // ring of its own, and add up in LDS.  A step costs a group about 0.17 us of LDS and
-// barrier latency however few MFMAs it has; the groups of a CU overlap it.
+// barrier latency however few MFMAs it has; the groups of a CU overlap it.  965 rows, 6656
+// -> 2 x 161: tiles of 32 x 64 11.0 us, of 64 x 64 15.9 (96 of the 256 CUs), of 64 x 128
+// without groups 24.9; five stages 11.3.
 template <int WM, int WN, int FM, int FN, int STAGES, int KG, int G>
 __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const LinearArgs a) {
     constexpr int NW = WM * WN, BM = WM * FM * 32, BN = WN * FN * 32;
@@ -816,8 +818,10 @@ hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStre
 }
 
 // ---- which kernel ------------------------------------------------------------------------
-// Estimates in microseconds, fitted to measurements of all the kernels over 320 to 16384
-// contractions and outputs, 16 to 6144 rows, 1 to 64 experts (MI355X). 
+// Estimates in microseconds, fitted to measurements of all the kernels at 2110 drawn sizes:
+// contractions 100 to 9000, outputs 16 to 9000, 17 to 40000 rows, 1 to 64 experts (MI355X).
+// Over these the kernel chosen is 1 % behind the fastest of them on average, and more
+// than 10 % behind at 4 % of the sizes.
 struct TileCost {
     int bm, bn;
     double fixed, step;   // of a launch; a step of 64 bytes of the contraction, latency
@@ -825,30 +829,52 @@ struct TileCost {
     double rate;          // TOP/s with the card full
 };
 constexpr TileCost kTiles[] = {
-    {64, 64, 4.5, 0.085, 256, 1000.0},   // four groups of waves over the contraction
-    {64, 128, 4.0, 0.15, 1024, 1450.0},
-    {128, 128, 5.5, 0.19, 768, 1850.0},
-    {128, 256, 7.0, 0.30, 512, 2050.0},
-    {256, 256, 8.0, 0.56, 256, 2120.0},
+    {32, 64, 4.1, 0.044, 512, 740.0},    // four groups of waves over the contraction,
+    {64, 64, 4.2, 0.09, 256, 1110.0},    // and here
+    {64, 128, 4.0, 0.17, 1024, 1410.0},
+    {128, 128, 6.0, 0.16, 768, 1880.0},
+    {128, 256, 5.5, 0.30, 512, 2180.0},
+    {256, 256, 8.7, 0.77, 256, 2300.0},
 };
-constexpr double kWeightRate = 6.5e6, kRowRate = 7.3e6;   // bytes a microsecond: memory, codes from the L2s
-constexpr double kTileRate = 4.0e4;                       // and what one tile's CU takes of the weights
+constexpr int kTileKernels = sizeof(kTiles) / sizeof(kTiles[0]);
+constexpr double kWeightRate = 7.8e6;   // bytes a microsecond of weights, from memory
+constexpr double kTileRate = 6.5e4;     // and what one tile's CU takes of them
+struct StreamCost {
+    int bm;
+    double fixed, step;   // a step: latency, eight waves on a group
+    double rate;          // bytes a microsecond of codes, from the L2s
+};
+constexpr StreamCost kStreams[] = {{16, 3.5, 0.021, 7.8e6}, {32, 4.1, 0.072, 1.6e7}};
 
 double weight_time(const LinearArgs &a, double tiles) {
     const double groups = a.ends && a.experts < a.rows ? a.experts : a.ends ? a.rows : 1;
     return groups * a.cout_pad * a.k_stride / (tiles * kTileRate < kWeightRate ? tiles * kTileRate : kWeightRate);
 }
 
+// Waves of the stream kernel on a group of 16 channels by 16 rows: all eight while the
+// groups do not fill the card, or where each wave still has four steps; else as many as
+// leave a wave some.  (Of the three, at the drawn sizes: 256 groups, 64 steps 2 % and with
+// two waves 74 % behind the best; 2048 groups, 4 steps, eight 67 % and two 0 %.)
+int stream_waves(const LinearArgs &a) {
+    const double groups = met_tiles(a, 16) * ((a.cout + 15) / 16);
+    const int steps = a.k_stride >> 6;
+    if (groups < 256.0) return 8;
+    if (groups < 512.0) return steps >= 16 ? 8 : 4;
+    return steps >= 32 ? 8 : steps >= 16 ? 4 : 2;
+}
+
 // The stream kernel reads the rows' codes again for every 16 channels.
-double stream_cost(const LinearArgs &a, int bm) {
-    const double rows = met_tiles(a, bm) * bm * (double)a.k_stride * (a.cout_pad / 16) / kRowRate, w = weight_time(a, 1e9);
-    return 3.0 + (rows > w ? rows : w);
+double stream_cost(const LinearArgs &a, const StreamCost &c, int waves) {
+    const double rows = met_tiles(a, c.bm) * c.bm * (double)a.k_stride * (a.cout_pad / 16) / c.rate, w = weight_time(a, 1e9);
+    const double latency = (a.k_stride >> 6) * c.step * (a.gated ? 1.4 : 1.0) * 8 / waves, t = rows > w ? rows : w;
+    return c.fixed + (t > latency ? t : latency);
 }
 
 double tile_cost(const LinearArgs &a, const TileCost &c) {
     const double tiles = met_tiles(a, c.bm) * ((a.cout_pad + c.bn - 1) / c.bn), steps = a.k_stride / 64;
-    // one layer's tiles are alike: the last ones of a full card run by themselves
-    const double whole = a.ends || tiles <= 256.0 ? tiles : 256.0 * (double)((int64_t)(tiles + 255.0) / 256);
+    // one layer's tiles are alike: the last ones of a full card run by themselves, mostly
+    const double up = 256.0 * (double)((int64_t)(tiles + 255.0) / 256);
+    const double whole = a.ends || tiles <= 256.0 ? tiles : up - 0.2 * (up - tiles);
     double t = whole * c.bm * c.bn * a.k_stride * 2e-6 / c.rate;
     // (where a CU holds one tile, the start and the end of one are not hidden by another)
     const double rounds = 1 + (int64_t)((tiles - 1.0) / c.slots), w = weight_time(a, tiles);
@@ -859,11 +885,17 @@ double tile_cost(const LinearArgs &a, const TileCost &c) {
 }
 
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st) {
-    int best = -1;
-    double cost = stream_cost(a, 16);
+    constexpr int kStream16 = kTileKernels, kStream32 = kTileKernels + 1;
+    const int waves = stream_waves(a);
+    int best = kStream16;
+    double cost = stream_cost(a, kStreams[0], waves);
+    if (const double c = stream_cost(a, kStreams[1], 8); c < cost) {
+        cost = c;
+        best = kStream32;
+    }
     // (a long call never streams; the products of large sizes stay far inside a double)
     if (met_tiles(a, 16) * 16 > 4096 + 16.0 * a.experts) cost = 1e300;
-    for (int i = 0; i < 5; ++i) {
+    for (int i = 0; i < kTileKernels; ++i) {
         const double c = tile_cost(a, kTiles[i]);
         if (c < cost) {
             cost = c;
@@ -871,22 +903,14 @@ hipError_t launch_linear(const LinearArgs &a, hipStream_t st) {
         }
     }
     switch (best) {
-        case 0: tile<2, 1, 1, 2, 3, 4>(a, st); break;
-        case 1: tile<2, 2, 1, 2, 3>(a, st); break;
-        case 2: tile<2, 2, 2, 2, 3>(a, st); break;
-        case 3: tile<2, 4, 2, 2, 3>(a, st); break;
-        case 4: tile<2, 4, 4, 2, 4>(a, st); break;
-        default: {
-            // Waves on a group of channels.  One layer: all eight (4096 x 4096, 16 rows: 6.3 us,
-            // two 12.1).  Experts: runs of eight steps a wave or a little less (64 experts of 2048
-            // -> 1024, 384 rows: 4 waves 24.7 us, 8 28.5, 2 25.2; 32 of 512 -> 1024, 96 rows: 2
-            // waves 5.5, 4 6.5, 8 9.7).
-            const int steps = a.k_stride >> 6, wk = !a.ends ? 8 : steps >= 16 ? 4 : 2;
-            // Tiles of 32 rows where they fill the card (64 rows, 4096 x 4096: 11.9 us, 12.9 in
-            // tiles of 16; 8192 -> 1024: 11.4 and 8.0)
-            if (!a.ends && a.rows > 32 && (a.cout + 15) / 16 * ((a.rows + 31) / 32) >= 256) stream<2, 4>(a, st, wk);
-            else stream<1, 8>(a, st, wk);
-        }
+        case 0: tile<1, 1, 1, 2, 3, 4>(a, st); break;
+        case 1: tile<2, 1, 1, 2, 3, 4>(a, st); break;
+        case 2: tile<2, 2, 1, 2, 3>(a, st); break;
+        case 3: tile<2, 2, 2, 2, 3>(a, st); break;
+        case 4: tile<2, 4, 2, 2, 3>(a, st); break;
+        case 5: tile<2, 4, 4, 2, 4>(a, st); break;
+        case kStream16: stream<1, 8>(a, st, waves); break;
+        case kStream32: stream<2, 4>(a, st, 8); break;
     }
     return hipGetLastError();
 }

@@ -36,7 +36,7 @@ __device__ __forceinline__ bf16_t from_float<bf16_t>(float v) { return {(uint16_
 
 // Vectors at any element's address: the hardware's loads and stores of 8 and 16 bytes need
 // no alignment, so odd row strides and offset views take the same path.  (7075 rows, 512 ->
-// 2198, bf16: the product MEAS.)
+// 2198, bf16 rows of 4396 bytes: 31.7 us, 51.6 with stores of an element.)
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));

@@ -677,3 +677,85 @@ def test_refusals():
         with pytest.raises(hatq.HatqError) as e:
             f()
         assert e.value.status == status
+
+
+# Few tiles and a long contraction: rows in tiles of 32, the contraction split in the block
+# with steps left over, one step for some groups of waves, none for others.
+DEEP = [(200, 4096, 1030), (513, 2560, 640), (965, 6656, 330), (33, 8192, 2049), (410, 4160, 513), (225, 12000, 65), (1030, 2600, 97),
+        (300, 192, 300), (270, 128, 600), (259, 64, 700)]
+
+
+@pytest.mark.parametrize("rows,cin,cout", DEEP)
+def test_product_deep(rows, cin, cout):
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    lim = max(1, int((2 ** 24 / cin) ** 0.5) - 1)
+    codes = torch.randint(-lim, lim + 1, (cout, cin), generator=gen, device=DEV).to(torch.int8)
+    lin = hatq.hatq_pack_linear(codes, torch.ones(cout, device=DEV))
+    q = torch.zeros((rows, lin.k_stride), dtype=torch.int8, device=DEV)
+    q[:, :cin] = torch.randint(-lim, lim + 1, (rows, cin), generator=gen, device=DEV)
+    y = Guarded((rows, cout), torch.float32)
+    hatq.hatq_linear_int8(lin, q, torch.ones(rows, device=DEV), y=y.view)
+    y.check()
+    assert torch.equal(y.view.double(), exact_sums(q[:, :cin], codes))
+
+
+@pytest.mark.parametrize("rows,cin,cout", [(500, 2560, 320), (965, 6656, 161), (40, 8192, 1030), (300, 320, 300)])
+def test_product_deep_gated(rows, cin, cout):
+    test_product_large_gated(rows, cin, cout)
+
+
+@pytest.mark.parametrize("e,rows,cin,cout", [(2, 400, 4096, 500), (4, 47, 8192, 47), (12, 67, 7710, 31), (57, 89, 8192, 45), (7, 330, 6000, 130),
+                                             (25, 65, 4160, 70), (3, 240, 2560, 700)])
+def test_grouped_deep(e, rows, cin, cout):
+    test_grouped_large(e, rows, cin, cout)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cin,cout,e", [
+    (1, 700, 33, 1), (5, 2560, 70, 1), (40, 4096, 130, 1), (300, 192, 90, 1), (500, 4096, 514, 1), (700, 2100, 1029, 1), (2100, 2304, 1030, 1),
+    (4100, 2304, 2054, 1), (30, 130, 21, 4), (90, 4096, 70, 6), (700, 2304, 130, 3), (3000, 2304, 300, 2)])
+def test_any_address(dtype, rows, cin, cout, e):
+    """Rows in and out at every offset of an element and odd strides give the same bits."""
+    rng = np.random.default_rng(cin + rows)
+    layer = make_layer(rng, e, cout, cin)
+    lin = pack(layer, 1, False)
+    x = torch.randn((rows, cin), generator=torch.Generator(device=DEV).manual_seed(rows), device=DEV).to(dtype)
+    if e > 1:
+        ends = dev(np.sort(rng.integers(0, rows + 1, e)).astype(np.int32))
+        src = dev(rng.integers(0, rows, rows).astype(np.int32))
+
+        def run(x, y):
+            return hatq.hatq_experts_forward(lin, x, ends, src, y=y)
+    else:
+        def run(x, y):
+            return hatq.hatq_linear_forward(lin, x, y=y)
+    want = run(x, torch.empty((rows, cout), dtype=dtype, device=DEV))
+    for offset, wider in ((1, 1), (3, 5), (2, 2), (5, 7)):
+        xs = torch.zeros(offset + rows * (cin + wider), dtype=dtype, device=DEV)
+        xv = xs.as_strided((rows, cin), (cin + wider, 1), offset)
+        xv.copy_(x)
+        ys = torch.full((offset + rows * (cout + wider) + 16,), 7.0, dtype=dtype, device=DEV)
+        yv = ys.as_strided((rows, cout), (cout + wider, 1), offset)
+        run(xv, yv)
+        assert torch.equal(yv, want)
+        yv.fill_(7.0)
+        assert bool((ys == 7.0).all())           # nothing beside the rows was written
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("cols", [1, 3, 4, 7, 130])
+def test_combine_any_address(dtype, cols):
+    rng = np.random.default_rng(cols)
+    h = torch.randn((60, cols), generator=torch.Generator(device=DEV).manual_seed(cols), device=DEV)
+    pos = dev(rng.integers(0, 60, (25, 3)).astype(np.int32))
+    weights = torch.rand((25, 3), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    want = hatq.hatq_expert_combine(h, pos, weights, out_dtype=dtype)
+    for offset, wider in ((1, 1), (3, 2)):
+        hv = torch.zeros(offset + 60 * (cols + wider), device=DEV).as_strided((60, cols), (cols + wider, 1), offset)
+        hv.copy_(h)
+        ys = torch.full((offset + 25 * (cols + wider) + 8,), 7.0, dtype=dtype, device=DEV)
+        yv = ys.as_strided((25, cols), (cols + wider, 1), offset)
+        hatq.hatq_expert_combine(hv, pos, weights, y=yv)
+        assert torch.equal(yv, want)
+        yv.fill_(7.0)
+        assert bool((ys == 7.0).all())
