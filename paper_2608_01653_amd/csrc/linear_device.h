@@ -188,6 +188,7 @@ __device__ __forceinline__ uint2 token_codes8(const float *v, float sigma, float
         m = fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), m);
     }
     if (!(plain && m <= 0.5f - 0x1p-16f)) {
+        asm volatile("");   // a branch: else the compiler divides for every chunk and selects
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float q = clamp127(rintf((sigma * v[j]) / s));
