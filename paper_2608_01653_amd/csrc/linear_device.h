@@ -111,6 +111,43 @@ __device__ __forceinline__ int wave_scan(int v, F f) {
 // index bits 0-2 are registers, bits 3-6 lanes of one 16-lane row, so the butterflies of
 // a block of up to 128 stay inside a DPP row.
 
+// The butterfly with lane ^ MASK, v + c v' for c = 1 or -1, of eight registers: the lane move
+// is part of the fused multiply-add.  (Written out, since the compiler keeps a move, a wait
+// and an add for each.)  A lane move may read a register two instructions after its write,
+// so s_nop 1 comes first; the eight registers are independent.
+#define HATQ_EIGHT(LINE, ctrl) LINE(0, 8, ctrl) LINE(1, 9, ctrl) LINE(2, 10, ctrl) LINE(3, 11, ctrl) LINE(4, 12, ctrl) \
+    LINE(5, 13, ctrl) LINE(6, 14, ctrl) LINE(7, 15, ctrl)
+#define HATQ_SELF(i, t, ctrl) "v_fmac_f32_dpp %" #i ", %" #i ", %8 " ctrl " row_mask:0xf bank_mask:0xf\n\t"
+#define HATQ_MOVE(i, t, ctrl) "v_mov_b32_dpp %" #t ", %" #i " " ctrl " row_mask:0xf bank_mask:0xf\n\t"
+#define HATQ_FROM(i, t, ctrl) "v_fmac_f32_dpp %" #i ", %" #t ", %16 " ctrl " row_mask:0xf bank_mask:0xf\n\t"
+#define HATQ_INOUT(v) "+&v"(v[0]), "+&v"(v[1]), "+&v"(v[2]), "+&v"(v[3]), "+&v"(v[4]), "+&v"(v[5]), "+&v"(v[6]), "+&v"(v[7])
+#define HATQ_OUT(v) "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+template <int MASK>
+__device__ __forceinline__ void cross8(float *v, float c) {
+    static_assert(MASK == 1 || MASK == 2 || MASK == 4 || MASK == 8, "lane mask");
+    if constexpr (MASK == 1) asm("s_nop 1\n\t" HATQ_EIGHT(HATQ_SELF, "quad_perm:[1,0,3,2]") : HATQ_INOUT(v) : "v"(c));
+    if constexpr (MASK == 2) asm("s_nop 1\n\t" HATQ_EIGHT(HATQ_SELF, "quad_perm:[2,3,0,1]") : HATQ_INOUT(v) : "v"(c));
+    if constexpr (MASK == 8) asm("s_nop 1\n\t" HATQ_EIGHT(HATQ_SELF, "row_ror:8") : HATQ_INOUT(v) : "v"(c));
+    if constexpr (MASK == 4) {   // i -> 7 - i inside 8 lanes, then i -> i ^ 3
+        float t[8];
+        asm("s_nop 1\n\t" HATQ_EIGHT(HATQ_MOVE, "row_half_mirror") HATQ_EIGHT(HATQ_FROM, "quad_perm:[3,2,1,0]")
+            : HATQ_INOUT(v), HATQ_OUT(t) : "v"(c));
+    }
+}
+#undef HATQ_EIGHT
+#undef HATQ_SELF
+#undef HATQ_MOVE
+#undef HATQ_FROM
+#undef HATQ_INOUT
+#undef HATQ_OUT
+
+template <int MASK, int R>
+__device__ __forceinline__ void token_cross(float (&v)[R], float c) {
+    static_assert(R % 8 == 0, "chunks of 8");
+#pragma unroll
+    for (int r = 0; r < R; r += 8) cross8<MASK>(v + r, c);
+}
+
 // The order-2^lb butterfly of every chunk; returns the sign of the values held relative
 // to the transform's (hatq_device.h, cross_stage).
 template <int R>
@@ -121,22 +158,22 @@ __device__ __forceinline__ float token_butterfly(float (&v)[R], int lane, int lb
     if (lb >= 3) reg_stage<4>(v);
     if (lb >= 4) {
         const float c = (lane & 1) ? -1.0f : 1.0f;
-        cross_stage<1>(v, c);
+        token_cross<1>(v, c);
         sigma *= c;
     }
     if (lb >= 5) {
         const float c = (lane & 2) ? -1.0f : 1.0f;
-        cross_stage<2>(v, c);
+        token_cross<2>(v, c);
         sigma *= c;
     }
     if (lb >= 6) {
         const float c = (lane & 4) ? -1.0f : 1.0f;
-        cross_stage<4>(v, c);
+        token_cross<4>(v, c);
         sigma *= c;
     }
     if (lb >= 7) {
         const float c = (lane & 8) ? -1.0f : 1.0f;
-        cross_stage<8>(v, c);
+        token_cross<8>(v, c);
         sigma *= c;
     }
     return sigma;

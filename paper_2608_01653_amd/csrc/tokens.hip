@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 // once.  Chunk i of row thread t is number i * 64 * WAVES + t.  The maximum keeps NaN:
 // a token with a value that is not finite gets the scale NaN and codes 0.  Bound by
 // memory with the butterflies (7 adds an element at order 128) close behind: 4096 tokens
-// of 4096, bf16, 13.8 us, 3.6 TB/s; 8192 of them 19.5 us, 5.2 TB/s.
+// of 4096, bf16, 13.0 us, 3.9 TB/s; 8192 of them 19.8 us, 5.1 TB/s.
 // Row `row` by its thread t; red: WAVES floats of LDS for each row of the block.
 template <int WAVES, int CH, typename T>
 __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int64_t row, int t, float *red) {
