@@ -169,22 +169,18 @@ __device__ __forceinline__ void finish16(const LinearArgs &a, const float *w_sca
     if (row < end && c < a.cout) put4(a, row, c, z[0]);
 }
 
-// A token's chunks of 8 elements, number i * THREADS + t, and their codes in LDS.
-template <typename T, int CH, int THREADS>
-__device__ __forceinline__ void load_chunks(const TokenArgs &x, int row, int t, float (&v)[8 * CH]) {
-    const T *p = static_cast<const T *>(x.x) + max(row, 0) * x.x_stride;
-    const int n = row < 0 ? 0 : x.cin;   // (an empty token is all zeros)
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int e = (i * THREADS + t) * 8;
-        if (e + 8 <= n) {
-            load8(p + e, &v[8 * i]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < n ? to_float(p[e + j]) : 0.0f;
-        }
-    }
+// A token's row, and the elements that it has (none for an empty one).
+template <typename T>
+struct TokenRow {
+    const T *p;
+    int n;
+};
+template <typename T>
+__device__ __forceinline__ TokenRow<T> token_row(const TokenArgs &x, int row) {
+    return {static_cast<const T *>(x.x) + max(row, 0) * x.x_stride, row < 0 ? 0 : x.cin};
 }
+
+// The codes of a token's chunks (load_chunks), to LDS.
 template <int CH, int THREADS>
 __device__ __forceinline__ void store_chunks(int8_t *to, int k_stride, int t, const float (&v)[8 * CH], float sigma, float s) {
     const float r = sigma * (1.0f / s);
@@ -307,8 +303,9 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     const int c16 = blockIdx.x, rows = a.rows;
     const int pitch = a.k_stride + 16;   // 16 rows' pieces then lie in different banks
 
-    float v[8 * CH];
-    load_chunks<T, CH, 512>(x, 0, threadIdx.x, v);
+    TokenRow<T> token = token_row<T>(x, 0);
+    Raw8<T> raw[CH] = {};
+    load_chunks<T, CH, 512>(token.p, token.n, threadIdx.x, raw);
 
     const int nks = a.k_stride >> 6;
     const int block0 = G == 1 ? c16 : (c16 >> 1) * 4 + (c16 & 1);   // of 16 packed columns
@@ -326,7 +323,12 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
     __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
 
     for (int row = 0; row < rows; ++row) {
-        if (row) load_chunks<T, CH, 512>(x, row, threadIdx.x, v);
+        float v[8 * CH];
+        chunk_values<T, CH, 512>(token.p, token.n, threadIdx.x, raw, v);
+        if (row + 1 < rows) {   // the next row, under way over this one's codes
+            token = token_row<T>(x, row + 1);
+            load_chunks<T, CH, 512>(token.p, token.n, threadIdx.x, raw);
+        }
         const float sigma = token_butterfly(v, lane, x.log_b);
         float m = token_max(v);
         if (row) __syncthreads();   // the row before has been read
@@ -394,10 +396,12 @@ __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, c
     const int end = min(((int)blockIdx.y + 1) * per, (a.cout + 15) / 16);
     int c16 = blockIdx.y * per + wave;
 
-    float v[TURNS][8 * CH];
+    TokenRow<T> token[TURNS];
+    Raw8<T> raw[TURNS][CH] = {};
 #pragma unroll
-    for (int i = 0; i < TURNS; ++i)
-        if (wave + WAVES * i < rows) load_chunks<T, CH, 64>(x, token_of(a, row0 + wave + WAVES * i), lane, v[i]);
+    for (int i = 0; i < TURNS; ++i) token[i] = token_row<T>(x, token_of(a, row0 + min(wave + WAVES * i, rows - 1)));
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) load_chunks<T, CH, 64>(token[i].p, token[i].n, lane, raw[i]);
 
     const int64_t value = (int64_t)32 * a.k_stride;   // from the gates' columns to the values'
     v4i fw[U][G];
@@ -417,10 +421,12 @@ __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, c
     for (int i = 0; i < TURNS; ++i) {
         const int row = wave + WAVES * i;
         if (row >= rows) break;
-        const float sigma = token_butterfly(v[i], lane, x.log_b);
-        const float s = token_scale(token_max(v[i]));
+        float v[8 * CH];
+        chunk_values<T, CH, 64>(token[i].p, token[i].n, lane, raw[i], v);
+        const float sigma = token_butterfly(v, lane, x.log_b);
+        const float s = token_scale(token_max(v));
         if (lane == 0) scale[row] = s * a.inv_b;
-        store_chunks<CH, 64>(codes + row * pitch, a.k_stride, lane, v[i], sigma, s);
+        store_chunks<CH, 64>(codes + row * pitch, a.k_stride, lane, v, sigma, s);
     }
     __syncthreads();
 

@@ -43,28 +43,79 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef _Float16 f16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef _Float16 f16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
-// Four and eight adjacent elements.
+// Four adjacent elements.
 __device__ __forceinline__ void load4(const float *p, float *v) {
     const f32x4_any a = *reinterpret_cast<const f32x4_any *>(p);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = a[j];
 }
-__device__ __forceinline__ void load8(const float *p, float *v) {
-    load4(p, v);
-    load4(p + 4, v + 4);
-}
-__device__ __forceinline__ void load8(const bf16_t *p, float *v) {
-    const u32x4_any w = *reinterpret_cast<const u32x4_any *>(p);
+
+// Eight adjacent elements as they lie in memory, and their values.
+template <typename T>
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
+template <typename T>
+__device__ __forceinline__ void load_raw(const T *p, Raw8<T> &r) {
+    const u32x4_any *q = reinterpret_cast<const u32x4_any *>(p);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        v[2 * j] = __uint_as_float(w[j] << 16);
-        v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+        const u32x4_any a = q[k];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r.w[4 * k + j] = a[j];
     }
 }
-__device__ __forceinline__ void load8(const _Float16 *p, float *v) {
-    const f16x8_any h = *reinterpret_cast<const f16x8_any *>(p);
+__device__ __forceinline__ void raw_values(const Raw8<float> &r, float *v) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
+    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r.w[j]);
+}
+__device__ __forceinline__ void raw_values(const Raw8<bf16_t> &r, float *v) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        v[2 * j] = __uint_as_float(r.w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(r.w[j] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void raw_values(const Raw8<_Float16> &r, float *v) {
+    typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const v2h h = __builtin_bit_cast(v2h, r.w[j]);
+        v[2 * j] = (float)h[0];
+        v[2 * j + 1] = (float)h[1];
+    }
+}
+
+// A token's chunks of 8 elements, number i * THREADS + t, of n elements at p (n = 0: an
+// empty token, p is not read): the loads, all of them under way at once, and then the
+// values, zeros past the end.  A chunk that the end cuts is read by elements.
+template <typename T, int CH, int THREADS>
+__device__ __forceinline__ void load_chunks(const T *p, int n, int t, Raw8<T> (&raw)[CH]) {
+    if (n < 8) return;   // (no whole chunk)
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int e = (i * THREADS + t) * 8;
+        load_raw(p + (e + 8 <= n ? e : 0), raw[i]);
+    }
+}
+template <typename T, int CH, int THREADS>
+__device__ __forceinline__ void chunk_values(const T *p, int n, int t, const Raw8<T> (&raw)[CH], float (&v)[8 * CH]) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int e = (i * THREADS + t) * 8;
+        raw_values(raw[i], &v[8 * i]);
+        if (e + 8 > n) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 * i + j] = 0.0f;
+            if (e < n) {
+                T one[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) one[j] = p[min(e + j, n - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < n ? to_float(one[j]) : 0.0f;
+            }
+        }
+    }
 }
 
 __device__ __forceinline__ void store4(float *p, const float *v) {

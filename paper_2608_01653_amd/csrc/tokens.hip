@@ -26,17 +26,10 @@ __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int64_t row,
     const T *x = static_cast<const T *>(a.x) + (in ? row : 0) * a.x_stride;
     const int chunks = a.k_stride >> 3;
 
+    Raw8<T> raw[CH] = {};
+    load_chunks<T, CH, RT>(x, a.cin, t, raw);
     float v[CH * 8];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int e = (i * RT + t) * 8;
-        if (e + 8 <= a.cin) {
-            load8(x + e, &v[8 * i]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[8 * i + j] = e + j < a.cin ? to_float(x[e + j]) : 0.0f;
-        }
-    }
+    chunk_values<T, CH, RT>(x, a.cin, t, raw, v);
     const float sigma = token_butterfly(v, t, a.log_b);
     float m = token_max(v);
     if constexpr (WAVES > 1) {
