@@ -373,16 +373,16 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
 }
 
 // ---- small layers, floats in ------------------------------------------------------------
-// A contraction of at most 2048: a block quantizes 16 MT rows (of one expert), a wave a
+// A contraction of at most 2048: a block quantizes 16 rows (of one expert), a wave a
 // row at a time (all of a wave's rows loaded at once), into LDS, and then each wave takes
 // groups of 16 output channels over the whole contraction, the weights straight from the
 // L2s.  blockIdx.y: `per` of the groups, a multiple of the waves.  Bound by latency (a row
 // in, its maximum, the weights' first bytes) until the weights' repeated reads take over:
 // 6144 rows, 320 -> 320, float32, 9.3 us (its 15.8 MB would take 3.1), 12-13 us as two
 // kernels.
-template <typename T, int G, int CH, int MT>
+template <typename T, int G, int CH>
 __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, const TokenArgs x, int per) {
-    constexpr int WAVES = 8, U = 8, ROWS = 16 * MT, TURNS = ROWS / WAVES;
+    constexpr int WAVES = 8, U = 8, ROWS = 16, TURNS = ROWS / WAVES;
     __shared__ __attribute__((aligned(16))) int8_t codes[ROWS * (512 * CH + 16)];
     __shared__ float scale[ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -430,40 +430,27 @@ __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, c
     }
     __syncthreads();
 
-    int mine[MT];
-    const int8_t *from[MT];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        mine[m] = min(16 * m + (lane & 15), rows - 1);
-        from[m] = codes + mine[m] * pitch + (lane >> 4) * 16;
-    }
+    const int mine = min(lane & 15, rows - 1);
+    const int8_t *from = codes + mine * pitch + (lane >> 4) * 16;
     while (c16 < end) {
-        v4i acc[MT][G];
+        v4i acc[G];
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int g = 0; g < G; ++g) acc[m][g] = v4i{0, 0, 0, 0};
+        for (int g = 0; g < G; ++g) acc[g] = v4i{0, 0, 0, 0};
         for (int k0 = 0; k0 < nks; k0 += U) {
             if (k0) weights(c16, k0);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (k0 + u >= nks) break;
+                const v4i fx = *reinterpret_cast<const v4i *>(from + (k0 + u) * 64);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const v4i fx = *reinterpret_cast<const v4i *>(from[m] + (k0 + u) * 64);
-#pragma unroll
-                    for (int g = 0; g < G; ++g)
-                        acc[m][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][g], fx, acc[m][g], 0, 0, 0);
-                }
+                for (int g = 0; g < G; ++g) acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[u][g], fx, acc[g], 0, 0, 0);
             }
         }
         const int c = c16;
         c16 += WAVES;
         if (c16 < end) weights(c16, 0);   // the next group's, under way over the stores
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-            finish16<G>(a, a.w_scale + first, a.bias + first, acc[m], scale[mine[m]], row0 + 16 * m + (lane & 15),
-                        row0 + rows, c, G == 1 ? c : (c >> 1) * 4 + (c & 1), lane);
+        finish16<G>(a, a.w_scale + first, a.bias + first, acc, scale[mine], row0 + (lane & 15), row0 + rows, c,
+                    G == 1 ? c : (c >> 1) * 4 + (c & 1), lane);
     }
 }
 
@@ -757,27 +744,24 @@ void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
     else linear_token_kernel<T, 1, CH><<<grid, 512, bytes, st>>>(a, x);
 }
 
-template <typename T, int CH, int MT>
+template <typename T, int CH>
 void small(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
-    // as few column ranges as fill the card twice: each range quantizes the rows again
-    const int groups = (a.cout + 15) / 16, blocks = (int)most_row_tiles(a, 16 * MT);
-    int ranges = (groups + 7) / 8;
-    if (ranges > (512 + blocks - 1) / blocks) ranges = (512 + blocks - 1) / blocks;
+    // Column ranges, each of which quantizes the rows again: as many as the card holds blocks
+    // of, two a CU (bf16, 512 -> 256, 6144 rows: 384 blocks 8.8 us, 768 11.0).
+    const int groups = (a.cout + 15) / 16, blocks = (int)most_row_tiles(a, 16);
+    const int most = blocks < 512 ? 512 / blocks : 1, ranges = (groups + 7) / 8 < most ? (groups + 7) / 8 : most;
     const int per = ((groups + ranges - 1) / ranges + 7) / 8 * 8;
     const dim3 grid(blocks, (groups + per - 1) / per);
-    if (a.gated) linear_small_kernel<T, 2, CH, MT><<<grid, 512, 0, st>>>(a, x, per);
-    else linear_small_kernel<T, 1, CH, MT><<<grid, 512, 0, st>>>(a, x, per);
+    if (a.gated) linear_small_kernel<T, 2, CH><<<grid, 512, 0, st>>>(a, x, per);
+    else linear_small_kernel<T, 1, CH><<<grid, 512, 0, st>>>(a, x, per);
 }
 
 template <typename T>
 void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
-    // (1024 -> 256, bf16: 16384 rows 20.4 us in tiles of 32 rows, 25.1 of 16; 4096 rows 10.5
-    // and 9.8; 320 -> 320, 6144 rows: 16.2 and 8.9)
-    const bool two = !a.ends && a.rows > 8192;
-    if (a.k_stride <= 512) two ? small<T, 1, 2>(a, x, st) : small<T, 1, 1>(a, x, st);
-    else if (a.k_stride <= 1024) two ? small<T, 2, 2>(a, x, st) : small<T, 2, 1>(a, x, st);
+    if (a.k_stride <= 512) small<T, 1>(a, x, st);
+    else if (a.k_stride <= 1024) small<T, 2>(a, x, st);
     else if (a.k_stride <= 2048 && (a.ends || (int64_t)a.rows * a.k_stride > HATQ_TOKEN_CODES || a.rows > HATQ_TOKEN_ROWS))
-        small<T, 4, 1>(a, x, st);
+        small<T, 4>(a, x, st);
     else if (a.k_stride <= 4096) token<T, 1>(a, x, st);
     else if (a.k_stride <= 8192) token<T, 2>(a, x, st);
     else token<T, 4>(a, x, st);
@@ -800,20 +784,23 @@ double met_tiles(const LinearArgs &a, int bm) {
     return t > groups ? t : groups;
 }
 
-// The small kernel reads the weights again for every 16 rows: it wins while these are
-// few, or cheap against the codes' way through memory.  (us, two kernels and one.  bf16:
-// 320 -> 320, 6144 rows 12.0 and 8.9; 512 -> 2048, 1024 rows 9.7 and 8.9, 2048 rows 11.9
-// and 13.0; 1024 -> 256, 6144 rows 15.6 and 13.2; 1024 -> 4096, 128 rows 9.2 and 8.5, 512
-// rows 11.7 and 13.4.)  By expert, while a tile of 16 rows is mostly all that an expert
-// has.  (Float32: 32 experts of 512 -> 1024, 96 rows 8.1 and 6.0, 384 rows 10.0 and 7.3, 768
-// rows 10.4 and 11.5; 64 of 2048 -> 1024, 48 rows 16.2 and 14.2, 768 rows 30.8 and 29.5,
-// 1536 rows 32.1 and 48.9; 8 of 320 -> 320, 1536 rows 8.7 and 7.4.)
+// The small kernel reads the weights again for every 16 rows, quantizes rows once for each
+// range of columns and writes runs of 16 channels: it wins while rows and columns are few,
+// fitted as rows cout^1.5.  (us, two kernels and one.  bf16: 128 -> 32, 8192 rows 9.2 and
+// 6.2; 512 -> 256, 4096 rows 10.4 and 7.7; 1024 -> 256, 16384 rows 22.9 and 22.3; 512 ->
+// 704, 8192 rows 17.6 and 14.8; 512 -> 2048, 800 rows 9.2 and 8.5, 1500 rows 10.8 and
+// 13.2; 2048 -> 256, 300 rows 9.6 and 10.0, 1500 rows 12.4 and 10.4, 2500 rows 16.8 and
+// 19.1.)  By expert, while a tile of 16 rows is mostly all that an expert has.  (Float32:
+// 32 experts of 512 -> 1024, 96 rows 8.1 and 6.0, 384 rows 10.0 and 7.3, 768 rows 10.4 and
+// 11.5; 64 of 2048 -> 1024, 48 rows 16.2 and 14.2, 768 rows 30.8 and 29.5, 1536 rows 32.1
+// and 48.9; 8 of 320 -> 320, 1536 rows 8.7 and 7.4.)
 bool linear_takes_tokens(const LinearArgs &a) {
     if (!a.ends && a.rows <= HATQ_TOKEN_ROWS && (int64_t)a.rows * a.k_stride <= HATQ_TOKEN_CODES) return true;
-    const double work = met_tiles(a, 16) * 16.0 * a.k_stride * a.cout_pad;
-    if (a.ends) return a.k_stride <= 2048 && (work <= 4e8 || a.rows <= 12 * (int64_t)a.experts);
-    // (1024 to 2048: level in time, with a launch less: 2048 -> 1024, 96 rows 9.1 and 8.8)
-    return a.k_stride <= 2048 && work <= (a.k_stride > 1024 ? 4e8 : a.cout_pad <= 512 ? 5e9 : 1.2e9);
+    if (a.k_stride > 2048) return false;
+    const double rows = a.rows, cols = a.cout_pad;
+    if (a.ends) return met_tiles(a, 16) * 16.0 * a.k_stride * cols <= 4e8 || a.rows <= 12 * (int64_t)a.experts;
+    if (a.k_stride > 1024) return rows >= 500 && rows * cols <= 4e5;
+    return rows * rows * cols * cols * cols <= 7e7 * 7e7;
 }
 
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
