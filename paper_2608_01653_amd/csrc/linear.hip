@@ -547,11 +547,13 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
     constexpr int RING = STAGES * STAGE_BYTES;
     static_assert(NW * 32 * (COLS + 4) * 4 <= KG * RING, "output staging");
     static_assert(KG == 1 || (4 % KG == 0 && KG * NW * FM * FN * 4096 <= KG * RING), "partial sums");
-    static_assert(BN / 4 <= 64 * NW, "column factors");
-    // the ring, then the columns' scales and biases, [2][BN] floats.  (One array: with a
-    // second LDS object the compiler waits for every load under way before each read.)
-    __shared__ __attribute__((aligned(1024))) int8_t lds[KG * RING + 8 * BN];
+    static_assert(BN <= 256 && BM <= 64 * NW * KG && NW * KG >= 2, "a wave's load of the factors");
+    // the ring, then the columns' scales and biases, [2][BN] floats, and the tokens' scales.
+    // (One array: with a second LDS object the compiler waits for every load under way
+    // before each read.)
+    __shared__ __attribute__((aligned(1024))) int8_t lds[KG * RING + 8 * BN + 4 * BM];
     float4 *factor = reinterpret_cast<float4 *>(lds + KG * RING);
+    float *scales = reinterpret_cast<float *>(lds + KG * RING + 8 * BN);
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kg = all / NW, wave = all % NW, wm = wave / WN, wn = wave % WN;
     int8_t *ring = lds + kg * RING;
@@ -567,16 +569,30 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
     const int rows = min(r.end - r.row0, BM);
     if (r.expert < 0) return zero_tile(a, r.row0, rows, tn * BN / G, BN / G);
 
-    if (threadIdx.x < BN / 4) {
-        const int64_t p = (int64_t)r.expert * a.cout_pad + min(tn * BN + (int)threadIdx.x * 4, a.cout_pad - 4);
-        factor[threadIdx.x] = *reinterpret_cast<const float4 *>(a.w_scale + p);
-        factor[BN / 4 + threadIdx.x] = *reinterpret_cast<const float4 *>(a.bias + p);
-    }
-    float scale[FM];   // of this lane's tokens
+    // the tokens of this lane's pieces of the operand, and of a row of the tile
+    const int mine_row = all * 64 + lane;
+    int tok_a[A_INSTR], tok_row = r.row0 + min(mine_row, rows - 1);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int tok = token_of(a, r.row0 + min((wm * FM + i) * 32 + (lane & 31), rows - 1));
-        scale[i] = tok < 0 ? 0.0f : a.sx[tok] * a.inv_b;
+    for (int j = 0; j < A_INSTR; ++j) tok_a[j] = r.row0 + min(16 * (wave + NW * j) + (lane >> 2), rows - 1);
+    if (a.src) {   // (all loaded before one is looked at)
+        tok_row = a.src[tok_row];
+#pragma unroll
+        for (int j = 0; j < A_INSTR; ++j) tok_a[j] = a.src[tok_a[j]];
+        if ((unsigned)tok_row >= (unsigned)a.x_rows) tok_row = -1;
+#pragma unroll
+        for (int j = 0; j < A_INSTR; ++j)
+            if ((unsigned)tok_a[j] >= (unsigned)a.x_rows) tok_a[j] = -1;
+    }
+
+    // Column factors and token scales, wanted at the end: direct loads to LDS as well, older than
+    // the ring's, so that the ring's first wait ends them and no tile starts by waiting for them.
+    if (all < 2 && lane < BN / 4) {
+        const float *from = (all ? a.bias : a.w_scale) + (int64_t)r.expert * a.cout_pad + min(tn * BN + lane * 4, a.cout_pad - 4);
+        __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(from), HATQ_LDS(lds + KG * RING + all * 4 * BN), 16, 0, 0);
+    }
+    if (mine_row < BM) {
+        if (tok_row < 0) scales[mine_row] = 0.0f;
+        else __builtin_amdgcn_global_load_lds(HATQ_GLOBAL(a.sx + tok_row), HATQ_LDS(scales + all * 64), 4, 0, 0);
     }
     // this group's steps: `nks` of them from k0, in a loop of `turns` for every group
     const int steps = a.k_stride >> 6, turns = (steps + KG - 1) / KG;
@@ -585,8 +601,7 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
 #pragma unroll
     for (int j = 0; j < A_INSTR; ++j) {
         const int m = 16 * (wave + NW * j) + (lane >> 2);
-        const int tok = token_of(a, r.row0 + min(m, rows - 1));
-        pa[j] = a.xq + (int64_t)max(tok, 0) * a.k_stride + k0 * 64 + 16 * ((lane & 3) ^ ((m >> 2) & 3));
+        pa[j] = a.xq + (int64_t)max(tok_a[j], 0) * a.k_stride + k0 * 64 + 16 * ((lane & 3) ^ ((m >> 2) & 3));
     }
 #pragma unroll
     for (int j = 0; j < B_INSTR; ++j) {
@@ -691,6 +706,9 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
         __syncthreads();
     }
 
+    float scale[FM];   // of this lane's tokens
+#pragma unroll
+    for (int i = 0; i < FM; ++i) scale[i] = scales[(wm * FM + i) * 32 + (lane & 31)] * a.inv_b;
     float *mine = reinterpret_cast<float *>(lds) + wave * 32 * (COLS + 4);
     const int c0 = (tn * BN + wn * FN * 32) / G;
 #pragma unroll
