@@ -525,7 +525,7 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
 //
 // 4096 x 4096 x 4096, bf16 out: 66 us, 2.1 POP/s; 8192 x 4096 x 16384 gated: 490 us, 2.24
 // POP/s, as the INT8 library product of that size, which writes plain sums.  There the
-// matrix cores are busy 60 % of the cycles at 1.7 GHz, where power holds the clock (2.4
+// matrix cores are busy 62 % of the cycles at 1.6 GHz, where power holds the clock (2.4
 // nominal); without the outputs it is 2.4 POP/s.  Wave tiles of 64 x 64 in blocks of 128 x
 // 256, two a CU, are 3 % behind 128 x 64 in 256 x 256 where all tiles are whole, and ahead
 // elsewhere: 32768 rows over 64 experts 175 us against 200.  Tried without gain: five
