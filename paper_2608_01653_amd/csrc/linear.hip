@@ -106,11 +106,33 @@ __device__ __forceinline__ int token_of(const LinearArgs &a, int row) {
 }
 
 // ---- epilogue -----------------------------------------------------------------------
-// g / (1 + exp(-g)) u by the hardware's exp2 and reciprocal (1 ulp each; the product
-// -g log2 e rounds to |g| 2^-24 of the result, 1e-6 where it is still 1e-6 of g).
-__device__ __forceinline__ float gated_unit(float g, float u) {
-    const float e = __builtin_amdgcn_exp2f(g * -1.44269504f);
-    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+// g[j] = g[j] / (1 + exp(-g[j])) u[j], each operation as its fp32 function: the same bits as
+// g / (1 + expf(-g)) u.  exp(-g) = 2^n 2^f: p = fl(-g log2 e), n = rne(p) in the low bits of
+// p + 1.5 2^23, and f = (p - n) + the product's rest, so its error does not grow with |g|;
+// |g| < 87 keeps 2^n 2^f normal and n its exponent's shift.  The quotient is g times the
+// reciprocal with one step of correction.  Groups with a larger gate, an infinity or a NaN
+// divide.  (The exponential and reciprocal alone, with p for n + f, lost up to 60 ulp at g =
+// -80 and moved a code of the next layer now and then.  8192 x 4096 -> 2 x 8192: 516 us with
+// them, 529 so, 545 with the division for every element.)
+__device__ __forceinline__ void gated4(float *g, const float *u) {
+    float m = 0.0f, y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float p = g[j] * -1.44269504f, t = p + HATQ_MAGIC;
+        // (log2 e = 1.44269504f + 1.92596303e-8f - 4.2e-16)
+        const float f = __builtin_fmaf(g[j], -1.92596303e-8f, __builtin_fmaf(g[j], -1.44269504f, -p)) + (p - (t - HATQ_MAGIC));
+        const float e = __uint_as_float((__float_as_uint(t) << 23) + __float_as_uint(__builtin_amdgcn_exp2f(f)));
+        const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), q = g[j] * r;
+        y[j] = __builtin_fmaf(__builtin_fmaf(-q, d, g[j]), r, q);
+        m = __builtin_elementwise_maximum(m, fabsf(g[j]));
+    }
+    if (!(m < 87.0f)) {
+        asm volatile("");   // a branch: else the compiler divides for every group and selects
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = g[j] / (1.0f + expf(-g[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = y[j] * u[j];
 }
 
 // z of four adjacent packed columns with factors at w_scale and bias (memory or LDS); s =
@@ -162,10 +184,7 @@ __device__ __forceinline__ void finish16(const LinearArgs &a, const float *w_sca
         const int q[4] = {sum[g][0], sum[g][1], sum[g][2], sum[g][3]};
         dequant4(w_scale + p + 32 * g, bias + p + 32 * g, q, scale, z[g]);
     }
-    if (G == 2) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
-    }
+    if (G == 2) gated4(z[0], z[1]);
     if (row < end && c < a.cout) put4(a, row, c, z[0]);
 }
 
@@ -276,10 +295,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const LinearArgs a, 
             const int q[4] = {sum[0], sum[1], sum[2], sum[3]};
             dequant4(w_scale + p + 32 * g, bias + p + 32 * g, q, s[m], z[g]);
         }
-        if (G == 2) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) z[0][j] = gated_unit(z[0][j], z[1][j]);
-        }
+        if (G == 2) gated4(z[0], z[1]);
         const int row = 16 * m + (lane & 15), c = c16 * 16 + (lane >> 4) * 4;
         if (row < rows && c < a.cout && c16 == g0 + wave / wk) put4(a, r.row0 + row, c, z[0]);
     }
@@ -730,10 +746,7 @@ __global__ void __launch_bounds__(64 * WM * WN * KG) linear_tile_kernel(const Li
                     dequant4(reinterpret_cast<const float *>(f + 8 * g), reinterpret_cast<const float *>(f + BN / 4 + 8 * g), v,
                              scale[i], z[g]);
                 }
-                if (G == 2) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) z[0][e] = gated_unit(z[0][e], z[1][e]);
-                }
+                if (G == 2) gated4(z[0], z[1]);
                 *reinterpret_cast<float4 *>(mine + (lane & 31) * (COLS + 4) + j / G * 32 + in) =
                     make_float4(z[0][0], z[0][1], z[0][2], z[0][3]);
             }
