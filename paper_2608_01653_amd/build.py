@@ -20,7 +20,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhatq.so")
-SOURCES = ["api.cpp", "api_linear.cpp", "act_quant.hip", "conv_i8.hip", "linear.hip", "tokens.hip", "weights.hip"]
+SOURCES = ["api.cpp", "api_linear.cpp", "act_quant.hip", "conv_i8.hip", "linear.hip", "linear_choice.cpp", "tokens.hip", "weights.hip"]
 CONV_PARTS = 18         # HATQ_CONV_PART = 0 .. 17 in conv_i8.hip
 OBJ_DIR = os.path.join(ROOT, "_build", "hatq")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -58,9 +58,22 @@ struct LinearArgs {
 };
 hipError_t launch_linear(const LinearArgs &a, hipStream_t st);
 
+// The kernel that launch_linear takes: tiles of rows x packed columns, or the weights streamed
+// past 16 or 32 rows by `waves` waves a group of channels.
+enum { kTile32x64, kTile64x64, kTile64x128, kTile128x128, kTile128x256, kTile256x256, kStream16, kStream32 };
+struct LinearChoice {
+    int kernel, waves;
+};
+LinearChoice choose_linear(const LinearArgs &a);
+
 // One layer's product of tokens that its own blocks quantize (xq and sx unused, no ends):
 // for a few tokens (HATQ_TOKEN_ROWS, HATQ_TOKEN_CODES) and for small layers.
 bool linear_takes_tokens(const LinearArgs &a);
+struct TokenChoice {
+    bool small;   // linear_small_kernel, else linear_token_kernel
+    int ch;       // chunks of 8 elements a lane
+};
+TokenChoice choose_tokens(const LinearArgs &a);
 hipError_t launch_linear_tokens(const LinearArgs &a, const TokenArgs &x, hipStream_t st);
 
 struct OrderArgs {

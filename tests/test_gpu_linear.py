@@ -246,8 +246,9 @@ def test_product(rows, cin, cout, gated):
     assert_close(y.view, ref, err, torch.float32)
 
 
-# Shapes that take each of the kernels, at their edges: the sums stay below 2^24, so that
-# with scales of 1 and no bias float32 outputs are the integers themselves.
+# Large shapes at the tiles' edges (not every kernel: test_gpu_linear_paths.py has those): the
+# sums stay below 2^24, so that with scales of 1 and no bias float32 outputs are the integers
+# themselves.
 LARGE = [(20, 8192, 100), (45, 2048, 4100), (65, 4096, 1030), (129, 16384, 200), (190, 4096, 4097), (385, 4032, 2050), (515, 4096, 4096),
          (1025, 4096, 2100), (1000, 1000, 6000), (2050, 4096, 4100), (4097, 1088, 4100), (9000, 320, 700), (6145, 2048, 1300),
          (70001, 64, 40)]
