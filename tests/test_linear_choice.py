@@ -7,6 +7,7 @@ import subprocess
 
 import pytest
 
+import test_gpu_expert_block as blocks
 import test_gpu_linear_paths as paths
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -80,3 +81,16 @@ def test_floats_meet_every_kernel(choose):
     want = {(f"small {ch}", *f) for ch in (1, 2, 4) for f in FORMS} | {(f"token {ch}", False, g) for ch in (1, 2, 4) for g in (False, True)}
     assert want <= met, sorted(want - met)
     assert None in met
+
+
+def test_blocks_meet_every_path(choose):
+    """Of the expert block: the first launch's instances (waves a row and chunks of a lane),
+    its two fallbacks, and both layouts of the hidden and output rows."""
+    first, layout = set(), set()
+    shapes = [(tokens * topk, hidden, width, e, False) for tokens, topk, e, width, hidden, _ in blocks.BLOCKS]
+    for (tokens, topk, e, width, hidden, _), (_, floats) in zip(blocks.BLOCKS, choose(shapes)):
+        chunks = (width + 63) // 64 * 8
+        first.add("pairs" if tokens * topk > 32768 else next((n for n in (64, 128, 256, 512, 1024) if chunks <= n), "width"))
+        layout.add("beside" if floats else "in place, " + ("wider" if hidden < width else "narrower" if hidden > width else "as wide"))
+    assert first == {64, 128, 256, 512, 1024, "pairs", "width"}
+    assert layout == {"beside", "in place, wider", "in place, narrower", "in place, as wide"}
