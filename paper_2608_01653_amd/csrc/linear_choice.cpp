@@ -23,12 +23,22 @@ double met_tiles(const LinearArgs &a, int bm) {
 // 19.1.)  By expert, while a tile of 16 rows is mostly all that an expert has.  (Float32:
 // 32 experts of 512 -> 1024, 96 rows 8.1 and 6.0, 384 rows 10.0 and 7.3, 768 rows 10.4 and
 // 11.5; 64 of 2048 -> 1024, 48 rows 16.2 and 14.2, 768 rows 30.8 and 29.5, 1536 rows 32.1
-// and 48.9; 8 of 320 -> 320, 1536 rows 8.7 and 7.4.)
+// and 48.9; 8 of 320 -> 320, 1536 rows 8.7 and 7.4.)  The ends are on the device, so the rule
+// has to hold for any: rows that meet in one expert read its weights again for every 16.  Up
+// to 8 an expert that is the better of the two all the same, from 9 on only while the product
+// is small.  (bf16, rows even / by Zipf's law / all in one expert: 64 of 2048 -> 8192, 512
+// rows 272 / 262 / 129 and 226 / 199 / 46, 576 rows 215 / 203 / 28 and 229 / 210 / 47, 768
+// rows 216 / 206 / 28 and 211 / 240 / 55; 256 of 2048 -> 8192, 3072 rows 806 / 760 / 98 and
+// 811 / 943 / 174; 256 of 1024 -> 4096, 2304 rows 215 / 196 / 34 and 207 / 251 / 56; below the
+// limit 64 of 2048 -> 4096, 768 rows 117 / 118 / 19 and 103 / 127 / 32.)
 bool linear_takes_tokens(const LinearArgs &a) {
     if (!a.ends && a.rows <= HATQ_TOKEN_ROWS && (int64_t)a.rows * a.k_stride <= HATQ_TOKEN_CODES) return true;
     if (a.k_stride > 2048) return false;
     const double rows = a.rows, cols = a.cout_pad;
-    if (a.ends) return met_tiles(a, 16) * 16.0 * a.k_stride * cols <= 4e8 || a.rows <= 12 * (int64_t)a.experts;
+    if (a.ends) {
+        if (met_tiles(a, 16) * 16.0 * a.k_stride * cols <= 4e8 || a.rows <= 8 * (int64_t)a.experts) return true;
+        return a.rows <= 12 * (int64_t)a.experts && rows * a.k_stride * cols <= 8e9;
+    }
     if (a.k_stride > 1024) return rows >= 500 && rows * cols <= 4e5;
     return rows * rows * cols * cols * cols <= 7e7 * 7e7;
 }

@@ -94,3 +94,12 @@ def test_blocks_meet_every_path(choose):
         layout.add("beside" if floats else "in place, " + ("wider" if hidden < width else "narrower" if hidden > width else "as wide"))
     assert first == {64, 128, 256, 512, 1024, "pairs", "width"}
     assert layout == {"beside", "in place, wider", "in place, narrower", "in place, as wide"}
+
+
+def test_rows_that_may_meet_in_one_expert(choose):
+    """Floats by expert: the small kernel reads an expert's weights again for every 16 of its
+    rows, so past 8 rows an expert it takes only small products; the ends are not known."""
+    wide = [(12 * e, 2048, cout, e, g) for e, cout, g in ((1024, 8192, 0), (256, 8192, 0), (64, 8192, 0), (64, 4096, 1), (256, 2048, 0))]
+    assert [t for _, t in choose(wide)] == [None] * len(wide)
+    small = [(8 * 256, 2048, 8192, 256, 0), (12 * 64, 2048, 1024, 64, 0), (12 * 1024, 512, 512, 1024, 0), (300, 320, 320, 8, 0)]
+    assert all(t for _, t in choose(small))
