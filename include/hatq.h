@@ -489,8 +489,9 @@ size_t hatq_linear_weights_bytes(int32_t experts, int32_t cin, int32_t cout, int
 /* Weights from floats: w device [experts][held][cin] of w_type (held = cout, or
  * 2 cout for a gated layer: gates, then values), bias device fp32
  * [experts][held] or NULL.  As hatq_prepare_weights: the transform in fp64,
- * rounded once to fp32, w_scale = fl32(max|W'| / 127) (1 for a zero row), codes
- * clamp(rne(fl32(W' / w_scale)), -127, 127).
+ * rounded once to fp32, w_scale = fl32(max|W'| / 127) (1 where that is 0), codes
+ * clamp(rne(fl32(W' / w_scale)), -127, 127).  A channel with a NaN or an infinity
+ * among its W' has the scale NaN and codes 0: its outputs are NaN.
  *   dst: device buffer of at least hatq_linear_weights_bytes, 256-byte aligned;
  *   *out receives the view into it.  Runs on `stream`. */
 int32_t hatq_prepare_linear(int32_t experts, int32_t cin, int32_t cout, int32_t gated, int32_t hblock, const void *w,

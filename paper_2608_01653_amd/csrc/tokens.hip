@@ -92,7 +92,8 @@ __device__ double transformed(const T *w, int d, int b) {
     return acc;
 }
 
-// One block per packed column of an expert.
+// One block per packed column of an expert.  The maximum keeps NaN, as the tokens' does: a
+// channel that is not finite gets the scale NaN and codes 0.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) linear_prepare_kernel(const LinearPrepArgs a) {
     const int p = blockIdx.x, e = blockIdx.y;
@@ -104,17 +105,21 @@ __global__ void __launch_bounds__(kThreads) linear_prepare_kernel(const LinearPr
     if (ch >= 0) {
         float m = 0.0f;
         for (int d = threadIdx.x; d < a.cin; d += kThreads)
-            m = fmaxf(m, fabsf((float)transformed(w, d, a.hblock)));
-        m = wave_max(m);
+            m = __builtin_elementwise_maximum(m, fabsf((float)transformed(w, d, a.hblock)));
+        const float of_lane[2] = {m, 0.0f};
+        m = token_max(of_lane);
         __shared__ float red[kThreads / 64];
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
         __syncthreads();
-        s = act_scale_from_absmax(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
+        m = red[0];
+#pragma unroll
+        for (int k = 1; k < kThreads / 64; ++k) m = __builtin_elementwise_maximum(m, red[k]);
+        s = token_scale(m);
     }
     int8_t *out = a.wpack + ((int64_t)e * a.cout_pad + (p & ~15)) * a.k_stride + (p & 15) * 16;
     for (int d = threadIdx.x; d < a.k_stride; d += kThreads) {
         int8_t q = 0;
-        if (ch >= 0 && d < a.cin) q = (int8_t)(int)rintf(clamp127((float)transformed(w, d, a.hblock) / s));
+        if (s == s && ch >= 0 && d < a.cin) q = (int8_t)(int)rintf(clamp127((float)transformed(w, d, a.hblock) / s));
         out[(int64_t)(d >> 6) * 1024 + ((d >> 4) & 3) * 256 + (d & 15)] = q;
     }
     if (threadIdx.x == 0) {
