@@ -570,7 +570,7 @@ int32_t hatq_expert_order(const int32_t *ids, int32_t tokens, int32_t topk, int3
 
 /* The weighted sum of each token's rows, y[t] = sum_j weights[t,j] h[pos[t,j]],
  * fp32 fma in ascending j, rounded once to y_type.
- *   h: device fp32 [h_rows][cols], row stride h_stride elements.
+ *   h: device fp32 [h_rows][cols], row stride h_stride elements, cols <= 2^30.
  *   pos: device int32 [tokens][topk]; a value outside [0, h_rows) adds nothing
  *   (a token with none gives 0).  weights: device fp32 [tokens][topk]. */
 int32_t hatq_expert_combine(const float *h, int32_t h_rows, int32_t cols, int64_t h_stride, const int32_t *pos,

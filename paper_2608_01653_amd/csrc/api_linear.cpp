@@ -12,6 +12,7 @@ namespace {
 
 constexpr int32_t kMaxWidth = 1 << 16;           // cin, held channels: 65536 * 127^2 < 2^31
 constexpr int64_t kMaxBytes = (int64_t)1 << 46;  // of one tensor
+constexpr int32_t kMaxCols = 1 << 30;            // of a weighted sum: column indices by fours fit 31 bits
 
 bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
@@ -339,6 +340,7 @@ int32_t hatq_expert_combine(const float *h, int32_t h_rows, int32_t cols, int64_
                             const float *weights, int32_t tokens, int32_t topk, void *y, int32_t y_type,
                             int64_t y_stride, void *stream) {
     if (h_rows < 0 || cols <= 0 || tokens < 0 || topk <= 0) return HATQ_EINVAL;
+    if (cols > kMaxCols) return HATQ_EUNSUPPORTED;
     if (tokens == 0) return HATQ_OK;
     int32_t s;
     if ((s = check_rows(y, y_type, tokens, cols, y_stride)) != HATQ_OK) return s;
