@@ -665,11 +665,23 @@ def _dtype(t: torch.dtype, name: str) -> int:
     return d
 
 
+_I32 = 2 ** 31 - 1      # ctypes keeps the low 32 bits of a larger size without a word
+
+
+def _sizes(name: str, *sizes: int):
+    """Raise ValueError where one of them does not fit the library's int32."""
+    for v in sizes:
+        if not -_I32 - 1 <= v <= _I32:
+            raise ValueError(f"{name}: sizes of at most {_I32} expected, got {v}")
+
+
 def _rows(t: torch.Tensor, name: str, cols: Optional[int] = None):
     """(rows, cols, stride, dtype code) of a 2-d device tensor whose rows are dense."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{name}: 2-d tensor expected")
     n, c = t.shape
+    if n > _I32 or c > _I32:
+        _sizes(name, n, c)
     if not t.is_cuda:
         raise ValueError(f"{name}: device tensor expected")
     if cols is not None and c != cols:
@@ -691,6 +703,7 @@ def _held(w: torch.Tensor, gated: bool, name: str):
     if w.dim() != 3:
         raise ValueError(f"{name}: [channels, cin] or [experts, channels, cin] expected, got {tuple(w.shape)}")
     e, held, cin = w.shape
+    _sizes(name, e, held, cin)
     if gated and held % 2:
         raise ValueError(f"{name}: a gated layer holds its gates and as many values, got {held} channels")
     return w.contiguous(), e, held, cin
@@ -698,6 +711,7 @@ def _held(w: torch.Tensor, gated: bool, name: str):
 
 def _linear(call: str, e: int, held: int, cin: int, gated: bool, hblock: int, device, run) -> PreparedLinear:
     cout = held // 2 if gated else held
+    _sizes("hblock", hblock)
     nbytes = int(load().hatq_linear_weights_bytes(e, cin, cout, int(gated), hblock))
     buf = torch.empty(max(nbytes, 1), dtype=torch.int8, device=device)
     out = LinearWeights()
@@ -748,6 +762,7 @@ def hatq_token_quant(x: torch.Tensor, hblock: int = 1, xq: Optional[torch.Tensor
         with torch.cuda.stream(stream):
             return hatq_token_quant(x, hblock, xq, scale)
     n, c, stride, t = _rows(x, "x")
+    _sizes("hblock", hblock)
     ks = (c + 63) // 64 * 64
     if xq is None:
         xq = torch.empty((n, ks), dtype=torch.int8, device=x.device)
@@ -773,9 +788,12 @@ def _out_rows(y: Optional[torch.Tensor], rows: int, cout: int, dtype: torch.dtyp
 def _codes(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor) -> int:
     if xq.dim() != 2 or xq.shape[1] != lin.k_stride:
         raise ValueError(f"xq: [rows, {lin.k_stride}] expected, got {tuple(xq.shape)}")
+    n = xq.shape[0]
+    if n > _I32:
+        _sizes("xq", n)
     _need(xq, "xq", torch.int8, 0)
-    _need(scale, "scale", torch.float32, xq.shape[0])
-    return xq.shape[0]
+    _need(scale, "scale", torch.float32, n)
+    return n
 
 
 def hatq_linear_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor,
@@ -792,6 +810,7 @@ def hatq_linear_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor,
 
 
 def hatq_linear_ws_bytes(lin: PreparedLinear, rows: int) -> int:
+    _sizes("rows", rows)
     return int(load().hatq_linear_ws_bytes(lin.ref, rows))
 
 
@@ -829,7 +848,10 @@ def _grouping(lin: PreparedLinear, ends: torch.Tensor, src: Optional[torch.Tenso
     if src.dim() != 1:
         raise ValueError(f"src: 1-d tensor expected, got shape {tuple(src.shape)}")
     _need(src, "src", torch.int32, 0)
-    return src.shape[0]
+    n = src.shape[0]
+    if n > _I32:
+        _sizes("src", n)
+    return n
 
 
 def hatq_experts_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor, ends: torch.Tensor,
@@ -878,6 +900,7 @@ def hatq_expert_order(ids: torch.Tensor, experts: int, ends: Optional[torch.Tens
         raise ValueError(f"ids: [tokens, topk] expected, got shape {tuple(ids.shape)}")
     _need(ids, "ids", torch.int32, 0)
     t, k = ids.shape
+    _sizes("ids, experts", t, k, experts)
     nbytes = int(load().hatq_expert_order_ws_bytes(t, k, experts))
     if ends is None:
         ends = torch.empty(experts, dtype=torch.int32, device=ids.device)
@@ -912,6 +935,7 @@ def hatq_expert_combine(h: torch.Tensor, pos: torch.Tensor, weights: torch.Tenso
     _need(pos, "pos", torch.int32, 0)
     _need(weights, "weights", torch.float32, 0)
     t, k = pos.shape
+    _sizes("pos", t, k)
     y, ys, yt = _out_rows(y, t, c, out_dtype, h)
     _check(load().hatq_expert_combine(h.data_ptr(), n, c, hs, pos.data_ptr(), weights.data_ptr(), t, k, y.data_ptr(),
                                       yt, ys, _stream()), "hatq_expert_combine")
@@ -919,6 +943,7 @@ def hatq_expert_combine(h: torch.Tensor, pos: torch.Tensor, weights: torch.Tenso
 
 
 def hatq_expert_mlp_ws_bytes(w_in: PreparedLinear, w_out: PreparedLinear, tokens: int, topk: int) -> int:
+    _sizes("tokens, topk", tokens, topk)
     return int(load().hatq_expert_mlp_ws_bytes(w_in.ref, w_out.ref, tokens, topk))
 
 
@@ -937,6 +962,8 @@ def hatq_expert_mlp(w_in: PreparedLinear, w_out: PreparedLinear, x: torch.Tensor
     _need(weights, "weights", torch.float32, 0)
     y, ys, yt = _out_rows(y, n, w_out.cout, out_dtype or x.dtype, x)
     topk = ids.shape[1]
+    if topk > _I32:
+        _sizes("ids", topk)
     if ws is None:
         ws = torch.empty(max(hatq_expert_mlp_ws_bytes(w_in, w_out, n, topk), 256), dtype=torch.int8, device=x.device)
     _need(ws, "ws", torch.int8, 0)
