@@ -448,20 +448,21 @@ int32_t hatq_layer_forward(const hatq_weights *W, int32_t form, const float *x, 
  *   S[t]   = B_cin x[t]                      fp32 butterflies, ascending stages
  *   s[t]   = fl32(max|S[t]| / 127)           1 where that is 0
  *   q[t,d] = clamp(rne(fl32(S[t,d] / s[t])), -127, 127)
- *   z[t,c] = fma(float(sum_d q[t,d] wq[c,d]), fl(s[t] w_scale[c]) (1/b), bias[c])
+ *   z[t,c] = fma(float(sum_d q[t,d] wq[c,d]), fl((s[t] / b) w_scale[c]), bias[c])
+ *            (s[t] / b is exact unless it is below 2^-126)
  *   y[t,c] = z[t,c], or for a gated layer, which holds 2 cout channels, gates
- *            first: g u / (1 + exp(-g)) with g = z[t,c], u = z[t,cout+c].
+ *            first: g / (1 + exp(-g)) u with g = z[t,c], u = z[t,cout+c], each
+ *            operation in fp32 (0 where exp(-g) overflows: g < -88.7).
  * The sums are exact in INT32.  y is rounded once, to y_type.  A token that
  * holds a NaN or an infinity, or whose transform overflows fp32, has the scale
  * NaN and codes 0: its outputs are NaN, every other token's are unaffected.
  *
  * Here rows have strides, in elements; the elements of a row are adjacent.  A
- * call with no rows is HATQ_OK and launches nothing, one of more than 2^24 rows
- * HATQ_EUNSUPPORTED.  x and y may have any
- * alignment of their type (rows at multiples of 16 bytes are read and written
- * faster); codes and prepared weights are 16-byte aligned.  Outputs and the
- * workspace do not overlap the inputs.  No kernel's result depends on the order in
- * which blocks run. */
+ * call with no rows is HATQ_OK and launches nothing (but hatq_expert_order, which
+ * writes its ends), one of more than 2^24 rows HATQ_EUNSUPPORTED.  x and y may have
+ * any alignment of their type; codes and prepared weights are 16-byte aligned.
+ * Outputs and the workspace do not overlap the inputs.  No kernel's result depends
+ * on the order in which blocks run. */
 typedef enum { HATQ_F32 = 0, HATQ_BF16 = 1, HATQ_F16 = 2 } hatq_dtype;
 
 /* Prepared linear weights: a plain view into the caller's device buffer.
@@ -523,7 +524,8 @@ int32_t hatq_linear_int8(const hatq_linear_weights *W, const int8_t *xq, const f
 
 /* The whole layer, floats in: hatq_token_quant into the workspace, then
  * hatq_linear_int8, or for a few tokens (rows <= HATQ_TOKEN_ROWS and rows
- * k_stride <= HATQ_TOKEN_CODES) one kernel that does both, with the same result.
+ * k_stride <= HATQ_TOKEN_CODES) and for small layers one kernel that does both,
+ * with the same result.
  * ws: device memory, 256-byte aligned, of at least hatq_linear_ws_bytes(W, rows)
  * bytes; for a few tokens it is not used and may be NULL. */
 #define HATQ_TOKEN_ROWS 16
@@ -546,7 +548,9 @@ int32_t hatq_experts_int8(const hatq_linear_weights *W, const int8_t *xq, const 
                           const int32_t *ends, const int32_t *src, int32_t rows, void *y, int32_t y_type,
                           int64_t y_stride, void *stream);
 
-/* The same, floats in: the x_rows tokens are quantized once each.  ws: at least
+/* The same, floats in: hatq_token_quant of the x_rows tokens into the workspace, then
+ * hatq_experts_int8, or for few rows and small products one kernel that quantizes
+ * each output row's token, with the same result.  ws: at least
  * hatq_linear_ws_bytes(W, x_rows) bytes, 256-byte aligned. */
 int32_t hatq_experts_forward(const hatq_linear_weights *W, const void *x, int32_t x_type, int32_t x_rows,
                              int64_t x_stride, const int32_t *ends, const int32_t *src, int32_t rows, void *y,

@@ -1,5 +1,5 @@
 // INT8 products of token codes with linear weights, one layer or grouped by expert,
-// and their epilogue: z = fma(float(acc), fl(s w_scale) / b, bias), the gated unit,
+// and their epilogue: z = fma(float(acc), fl((s / b) w_scale), bias), the gated unit,
 // one rounding to the output type.
 //
 // Operand roles: the weights are the MFMA's first operand, the tokens its second, so
@@ -112,8 +112,8 @@ __device__ __forceinline__ int token_of(const LinearArgs &a, int row) {
 // |g| < 87 keeps 2^n 2^f normal and n its exponent's shift.  The quotient is g times the
 // reciprocal with one step of correction.  Groups with a larger gate, an infinity or a NaN
 // divide.  (The exponential and reciprocal alone, with p for n + f, lost up to 60 ulp at g =
-// -80 and moved a code of the next layer now and then.  8192 x 4096 -> 2 x 8192: 516 us with
-// them, 529 so, 545 with the division for every element.)
+// -80 and moved a code of the next layer now and then.  Whole call of 8192 x 4096 -> 2 x 8192: 516
+// us with them, 529 so, 545 with the division for every element.)
 __device__ __forceinline__ void gated4(float *g, const float *u) {
     float m = 0.0f, y[4];
 #pragma unroll
@@ -136,7 +136,7 @@ __device__ __forceinline__ void gated4(float *g, const float *u) {
 }
 
 // z of four adjacent packed columns with factors at w_scale and bias (memory or LDS); s =
-// the token's scale times 1/b, a power of two, so s w is fl(s_token w) / b.
+// the token's scale times 1/b, a power of two: exact unless it is below 2^-126.
 __device__ __forceinline__ void dequant4(const float *w_scale, const float *bias, const int *acc, float s, float *z) {
     const float4 w = *reinterpret_cast<const float4 *>(w_scale), b = *reinterpret_cast<const float4 *>(bias);
     z[0] = __builtin_fmaf((float)acc[0], s * w.x, b.x);
@@ -217,7 +217,7 @@ __device__ __forceinline__ void store_chunks(int8_t *to, int k_stride, int t, co
 // their values) by 16 MT rows: they take the contraction 64 bytes in turn and add up in
 // LDS; 8 / WK groups a block.  The weights go from memory to registers in runs of 1 KB,
 // U of them in flight a wave: the kernel is bound by their bytes.  WK is large where the
-// groups alone would not fill the card.  13 rows, 4096 -> 2 x 8192 gated: 12.7 us, 5.3 TB/s
+// groups alone would not fill the card.  13 rows, 4096 -> 2 x 8192 gated: 13.3 us, 5.1 TB/s
 // of weights (a large copy moves 5.1).  Tried without gain: 4, 12 and 16 runs in flight,
 // nontemporal loads (13.3 us).
 template <int MT, int G, int U>
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(512) linear_token_kernel(const LinearArgs a, c
 // groups of 16 output channels over the whole contraction, the weights straight from the
 // L2s.  blockIdx.y: `per` of the groups, a multiple of the waves.  Bound by latency (a row
 // in, its maximum, the weights' first bytes) until the weights' repeated reads take over:
-// 6144 rows, 320 -> 320, float32, 9.3 us (its 15.8 MB would take 3.1), 12-13 us as two
+// 6144 rows, 320 -> 320, float32, 9.6 us (its 15.8 MB would take 3.1), 12-13 us as two
 // kernels.
 template <typename T, int G, int CH>
 __global__ void __launch_bounds__(512) linear_small_kernel(const LinearArgs a, const TokenArgs x, int per) {
@@ -539,10 +539,11 @@ __device__ void store_rows(const LinearArgs &a, const float *from, int64_t row0,
 // buffer end before it, the loads that refill that buffer and the reads of the next
 // one begin after it.
 //
-// 4096 x 4096 x 4096, bf16 out: 66 us, 2.1 POP/s; 8192 x 4096 x 16384 gated: 490 us, 2.24
-// POP/s, as the INT8 library product of that size, which writes plain sums.  There the
-// matrix cores are busy 62 % of the cycles at 1.6 GHz, where power holds the clock (2.4
-// nominal); without the outputs it is 2.4 POP/s.  Wave tiles of 64 x 64 in blocks of 128 x
+// 4096 x 4096 x 4096, bf16 out: 64 us, 2.1 POP/s; 8192 x 4096 x 16384 gated: 505 us, 2.18
+// POP/s (the INT8 library product of that size, which writes plain sums, 2.24).  There the
+// matrix cores are busy 60 % of the cycles at 1.6 GHz, where power holds the clock (2.4
+// nominal).  (After a pause the clock takes some hundred calls to settle; before, the
+// same take up to 80 and 550 us.)  Wave tiles of 64 x 64 in blocks of 128 x
 // 256, two a CU, are 3 % behind 128 x 64 in 256 x 256 where all tiles are whole, and ahead
 // elsewhere: 32768 rows over 64 experts 175 us against 200.  Tried without gain: five
 // stages, wave priorities, 16 waves on 256 x 256, float32 stores without LDS, codes laid
@@ -777,8 +778,10 @@ void token(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
 
 template <typename T, int CH>
 void small(const LinearArgs &a, const TokenArgs &x, hipStream_t st) {
-    // Column ranges, each of which quantizes the rows again: as many as the card holds blocks
-    // of, two a CU (bf16, 512 -> 256, 6144 rows: 384 blocks 8.8 us, 768 11.0).
+    // Column ranges, each of which quantizes the rows again: up to 512 blocks, two a CU, as the
+    // card holds at once of a plain layer's with one and two chunks a lane and of a gated one's
+    // with one (bf16, 512 -> 256, 6144 rows: 384 blocks 8.8 us, 768 11.0).  The other forms'
+    // registers (138 to 207) leave one block a CU: more than 256 of theirs go in two rounds.
     const int groups = (a.cout + 15) / 16, blocks = (int)most_row_tiles(a, 16);
     const int most = blocks < 512 ? 512 / blocks : 1, ranges = (groups + 7) / 8 < most ? (groups + 7) / 8 : most;
     const int per = ((groups + ranges - 1) / ranges + 7) / 8 * 8;

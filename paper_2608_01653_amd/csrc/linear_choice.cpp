@@ -58,7 +58,9 @@ namespace {
 // Estimates in microseconds, fitted to measurements of all the kernels at 2110 drawn sizes:
 // contractions 100 to 9000, outputs 16 to 9000, 17 to 40000 rows, 1 to 64 experts (MI355X).
 // Over these the kernel chosen is 1 % behind the fastest of them on average, and more
-// than 10 % behind at 4 % of the sizes.
+// than 10 % behind at 4 % of the sizes.  The bytes of the outputs are not in it.  Past 64
+// experts it was not fitted, and streams too long: 256 experts of 2048 -> 8192, 2048 rows
+// streamed 1410 us with their codes, 2304 rows in tiles 795.
 struct TileCost {
     int bm, bn;
     double fixed, step;   // of a launch; a step of 64 bytes of the contraction, latency
@@ -74,7 +76,9 @@ constexpr TileCost kTiles[] = {   // (kTile32x64 to kTile256x256)
     {256, 256, 8.7, 0.77, 256, 2300.0},
 };
 constexpr int kTileKernels = sizeof(kTiles) / sizeof(kTiles[0]);
-constexpr double kWeightRate = 7.8e6;   // bytes a microsecond of weights, from memory
+// bytes a microsecond of weights; fitted to repeated calls, whose weights the memory-side cache
+// holds in part (a large copy moves 5.07e6, and weights that no cache holds come at 5.1e6)
+constexpr double kWeightRate = 7.8e6;
 constexpr double kTileRate = 6.5e4;     // and what one tile's CU takes of them
 struct StreamCost {
     int bm;

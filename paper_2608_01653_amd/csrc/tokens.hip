@@ -16,7 +16,7 @@ constexpr int kThreads = 256;
 // once.  Chunk i of row thread t is number i * 64 * WAVES + t.  The maximum keeps NaN:
 // a token with a value that is not finite gets the scale NaN and codes 0.  Bound by
 // memory with the butterflies (7 adds an element at order 128) close behind: 4096 tokens
-// of 4096, bf16, 13.0 us, 3.9 TB/s; 8192 of them 19.8 us, 5.1 TB/s.
+// of 4096, bf16, 12.1 us, 4.2 TB/s; 8192 of them 20.8 us, 4.8 TB/s.
 // Row `row` by its thread t; red: WAVES floats of LDS for each row of the block.
 template <int WAVES, int CH, typename T>
 __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int64_t row, int t, float *red) {
@@ -164,10 +164,12 @@ __global__ void __launch_bounds__(kThreads) linear_pack_kernel(const LinearPrepA
 // a contiguous part.  The first row of expert e in block b is the rows of the experts
 // before e plus the rows of e in the blocks before b; each wave then ranks its pairs 64
 // at a time in order.  Ranks come from ballots, not from atomics, so equal ids keep
-// their order.  Up to kOrderOne pairs every block counts all of them itself (one launch;
-// 16384 pairs of 32 experts 9.8 us, 18.1 with a launch for the counts before; 96 pairs
-// 4.2); beyond, a
-// first launch leaves the blocks' counts in a table.
+// their order.  Up to kOrderOne pairs every block counts all of them itself, in one launch;
+// beyond, a first launch leaves the blocks' counts in a table.  Not bound by memory: a call
+// is one or two launches (96 pairs 6.5 us through the binding) and then the counting by
+// LDS atomics, where lanes with the same expert wait for each other (32768 pairs of 32
+// experts 9.3 us, of 8 experts 12.3); through the table 65536 pairs of 32 8.5 us, 262144 of
+// 64 15.9, 2^24 of 256 267 (200 MB).
 constexpr int kOrderWaves = 8;
 constexpr int kOrderThreads = 64 * kOrderWaves;
 constexpr int kOrderBlocks = 256;

@@ -873,7 +873,7 @@ def hatq_experts_int8(lin: PreparedLinear, xq: torch.Tensor, scale: torch.Tensor
 def hatq_experts_forward(lin: PreparedLinear, x: torch.Tensor, ends: torch.Tensor,
                          src: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
                          y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """hatq_experts_int8 of tokens x [x_rows, cin], each quantized once."""
+    """hatq_experts_int8 of the codes of tokens x [x_rows, cin]."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return hatq_experts_forward(lin, x, ends, src, out_dtype, y, ws)
