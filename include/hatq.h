@@ -596,6 +596,94 @@ int32_t hatq_expert_mlp(const hatq_linear_weights *W_in, const hatq_linear_weigh
                         int32_t topk, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,
                         void *stream);
 
+/* ---- A cache of keys and values in 4 bits, and attention over it ------------------
+ *
+ * The symmetric quantizer of Eq. symmetric_q with 15 levels in the Hadamard domain, for
+ * heads of `dim` channels.  For a key or value x of one position and head, block b =
+ * hblock, and each group g of 64 adjacent channels (the last one may be shorter):
+ *   S    = B_dim x                           fp32 butterflies, ascending stages
+ *   s[g] = bf16(fl32(max_{d in g}|S[d]| / 7))  rounded half to even, at least 2^-100
+ *   c[d] = clamp(rne(fl32(S[d] / s[g])), -7, 7)
+ * and what they stand for is x' = B_dim (s c) / b.  A head with a NaN, an infinity or a
+ * magnitude of 2^102 (5e30) and more among its S has all its scales NaN and codes 0: it
+ * stands for NaN.
+ *
+ * The cache is made of pages of page_size positions of all heads.  Sequence i's position
+ * p is in page table[i][p / page_size]; a page of which the cache has none (negative, or
+ * >= pages) is absent.  Pages may be shared between sequences as long as no call writes
+ * one of them twice.  The library keeps no table, lengths or free pages of its own.
+ *
+ * The calls below take rows of new tokens, sequence by sequence: sequence i has the rows
+ * [ends[i - 1], ends[i]), n of them, which are its positions lens[i] - n .. lens[i] - 1, so
+ * lens counts the new tokens too.  ends NULL: rows / batch each.
+ *   table: device int32 [batch][width];  lens: device int32 [batch];
+ *   ends:  device int32 [batch], ascending, or NULL (then rows % batch == 0).
+ * Any contents of the three are safe.  Positions below 0, past the table's width or in an
+ * absent page are left out: not written, read as 0, not attended to.  Values of ends that
+ * do not ascend within [0, rows] give rows to some sequence or to none.  Rows past the
+ * last end stay as they are.
+ *
+ * Tensors [rows][heads][dim] have a stride in elements between rows and between heads,
+ * and adjacent channels; outputs' rows and heads do not overlap.  Any alignment of the
+ * type.  rows <= 2^24; no rows: HATQ_OK, nothing launched.  A sequence has at most 2^30
+ * positions (width page_size, else HATQ_EUNSUPPORTED). */
+typedef struct {
+    int32_t pages;
+    int32_t page_size;      /* positions, a power of two in [16, 65536] */
+    int32_t heads, dim;     /* of the keys and values */
+    int32_t hblock;         /* transform block on dim, a power of two in [1, 128] */
+    void *buf;              /* library-internal layout, 68 bytes for 64 codes of both */
+} hatq_cache4;
+
+typedef struct {
+    int32_t type;           /* hatq_dtype */
+    int64_t row_stride, head_stride;
+    void *p;
+} hatq_heads;
+
+/* Bytes of such a cache; 0 for sizes that are not supported (dim % hblock != 0, dim over
+ * 256, heads over 1024, pages page_size over 2^31 - 1).  hatq_cache4_init, host only,
+ * makes the view of a device buffer of at least as many bytes, 256-byte aligned.  The
+ * contents need no clearing: positions are written before a length reaches them. */
+size_t hatq_cache4_bytes(int32_t pages, int32_t page_size, int32_t heads, int32_t dim, int32_t hblock);
+int32_t hatq_cache4_init(int32_t pages, int32_t page_size, int32_t heads, int32_t dim, int32_t hblock, void *buf,
+                         size_t bytes, hatq_cache4 *out);
+
+/* New tokens' keys and values into the cache.  k, v: device [rows][heads][dim]. */
+int32_t hatq_cache4_append(const hatq_cache4 *C, const hatq_heads *k, const hatq_heads *v, int32_t rows,
+                           const int32_t *table, int32_t width, const int32_t *lens, const int32_t *ends,
+                           int32_t batch, void *stream);
+
+/* The values that the cache holds for such rows, written to k and v (each its own type):
+ * the sequences' last positions. */
+int32_t hatq_cache4_read(const hatq_cache4 *C, const hatq_heads *k, const hatq_heads *v, int32_t rows,
+                         const int32_t *table, int32_t width, const int32_t *lens, const int32_t *ends,
+                         int32_t batch, void *stream);
+
+/* Attention of query rows over the cache: for query head h, which reads the cached head
+ * h / (q_heads / heads), and a row of sequence i at position p,
+ *   y = sum_j w_j v'_j,  w = softmax over j of scale q . k'_j,
+ * j over [0, lens[i]), or causal: over [0, p], and with a window over (p - window, p] of
+ * those.  A row that sees no position gives 0.
+ *   q, y: device [rows][q_heads][dim], each its own type; q_heads % C->heads == 0.
+ *   scale: a finite number, mostly dim^-1/2.
+ *   causal: 0 or 1;  window: 0 for none, else at least 1, and causal.
+ *   max_len: 0, or what the lengths will not exceed, for the choice of the launch alone
+ *       (0: width page_size): any value gives the same sums, in another order.
+ *   ws: device memory, 256-byte aligned, of at least hatq_attention4_ws_bytes bytes for
+ *       the same sizes (ragged: ends is given); may be NULL where that is 0.  Calls that may
+ *       overlap need workspaces of their own.
+ * Scores, weights and sums are fp32.  Products: the transformed query in whole numbers of 16
+ * bits of its largest magnitude against the codes, exact sums in each group; the weights
+ * times the values' scales in fp16, relative to the largest.  If q or y is not bf16: 24
+ * bits, and 22 bits of the weights.  No result depends on the order in which blocks run. */
+size_t hatq_attention4_ws_bytes(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch,
+                                int32_t ragged, int32_t max_len);
+int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_heads *y, int32_t rows, int32_t q_heads,
+                        const int32_t *table, int32_t width, const int32_t *lens, const int32_t *ends, int32_t batch,
+                        float scale, int32_t causal, int32_t window, int32_t max_len, void *ws, size_t ws_bytes,
+                        void *stream);
+
 #ifdef __cplusplus
 }
 #endif

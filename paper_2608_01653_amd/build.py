@@ -6,7 +6,8 @@ packed-FP32 instructions disabled.
 
 Every source compiles to an object of its own, in parallel; conv_i8.hip is
 compiled once per part of its dispatch (HATQ_CONV_PART), since its kernel
-instantiations take most of the build time. The objects are linked into one
+instantiations take most of the build time, and attention4.hip once per head
+size (HATQ_ATTENTION_PART). The objects are linked into one
 shared library.
 """
 from __future__ import annotations
@@ -20,8 +21,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhatq.so")
-SOURCES = ["api.cpp", "api_linear.cpp", "act_quant.hip", "conv_i8.hip", "linear.hip", "linear_choice.cpp", "tokens.hip", "weights.hip"]
+SOURCES = ["api.cpp", "api_cache4.cpp", "api_linear.cpp", "act_quant.hip", "attention4.hip", "attention4_plan.cpp",
+           "cache4.hip", "conv_i8.hip", "linear.hip", "linear_choice.cpp", "tokens.hip", "weights.hip"]
 CONV_PARTS = 18         # HATQ_CONV_PART = 0 .. 17 in conv_i8.hip
+ATTENTION_PARTS = 4     # HATQ_ATTENTION_PART = 1 .. 4 in attention4.hip
 OBJ_DIR = os.path.join(ROOT, "_build", "hatq")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -46,6 +49,9 @@ def _units():
         if base == "conv_i8":
             for k in range(CONV_PARTS):
                 units.append((src, [f"-DHATQ_CONV_PART={k}"], os.path.join(OBJ_DIR, f"{base}.part{k}.o")))
+        elif base == "attention4":
+            for k in range(1, ATTENTION_PARTS + 1):
+                units.append((src, [f"-DHATQ_ATTENTION_PART={k}"], os.path.join(OBJ_DIR, f"{base}.part{k}.o")))
         else:
             units.append((src, [], os.path.join(OBJ_DIR, base + ".o")))
     return units

@@ -1,0 +1,25 @@
+// How attention over a 4-bit cache is laid out: host code without a launch, from sizes alone.
+#include "cache4.h"
+
+namespace hatq {
+
+AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t share, int32_t dim, int64_t max_len,
+                             bool ragged) {
+    const int64_t cols = (int64_t)rows * share;
+    AttentionPlan p{};
+    // a sequence's columns on average
+    p.wide = cols / batch >= 256;
+    const int64_t per = p.wide ? wide_cols(dim) * kWideWaves : 16;
+    p.tiles = ragged ? cols / per + (batch < rows ? batch : rows) : batch * ((cols / batch + per - 1) / per);
+    p.waves = dim <= 128 ? 8 : 4;
+    p.splits = 1;
+    if (p.wide) return p;
+    // blocks that fill the card, of at least two steps of 32 positions a wave
+    const int64_t steps = (max_len + 31) / 32, base = p.tiles * heads;
+    int64_t splits = 512 / base;
+    if (splits > steps / (2 * p.waves)) splits = steps / (2 * p.waves);
+    p.splits = splits < 1 ? 1 : (int32_t)splits;
+    return p;
+}
+
+}  // namespace hatq

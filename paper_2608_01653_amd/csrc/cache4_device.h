@@ -1,0 +1,181 @@
+// Device-side layout of the 4-bit cache and the transforms of its heads (gfx950).
+//
+// A head's channels are taken 64 at a time, NB blocks of them, zeros past the end, and
+// its positions 8 at a time.  One octet of positions of one head, 544 NB bytes:
+//   keys    [NB][4 chunks][4][2][8 bytes]: chunk u holds channels 16 u .. 16 u + 15 of the
+//           block, [r][h] position 4 h + r.  Byte b of the chunk's word w holds the codes of
+//           channels 8 w + b (low half) and 8 w + 4 + b (high half) in two's complement.
+//   values  [NB][16 runs][8 positions][2 bytes]: run l holds channels 4 l .. 4 l + 3, the
+//           lowest in the lowest bits, code + 8.
+//   scales  keys [NB][8 positions], values [NB][8 positions], bf16
+// A wave's 16-byte load at each of 64 addresses is then a matrix operand of 32 positions by
+// 64 channels with no exchange between lanes: for the keys, positions are rows and channels
+// the contraction; for the values, channels are rows and positions the contraction.
+#pragma once
+
+#include "cache4.h"
+#include "hatq_device.h"
+#include "linear_device.h"
+
+namespace hatq {
+
+constexpr int kOctet = 544;     // bytes a block of 64 channels of 8 positions of a head
+constexpr int kKeyCodes = 256;
+
+// Byte offsets inside an octet: 16 codes of a key's chunk, 4 of a value's run, a scale.
+__device__ __forceinline__ int key_at(int block, int chunk, int pos8) {
+    return block * kKeyCodes + chunk * 64 + (pos8 & 3) * 16 + (pos8 >> 2) * 8;
+}
+template <int NB>
+__device__ __forceinline__ int value_at(int block, int run, int pos8) {
+    return NB * kKeyCodes + block * 256 + run * 16 + pos8 * 2;
+}
+template <int NB>
+__device__ __forceinline__ int scale_at(int which, int block, int pos8) {
+    return NB * 512 + (which * NB + block) * 16 + pos8 * 2;
+}
+
+// Byte offset of a page's first octet of one head; an octet of it is octet * NB * kOctet on.
+template <int NB>
+__device__ __forceinline__ int64_t page_offset(const Cache4 &c, int page, int head) {
+    return ((int64_t)page * c.heads + head) * ((int64_t)(NB * kOctet) << (c.log_page - 3));
+}
+
+// The sequence of a row of the call, -1 past the last one, and its position, -1 before the
+// first one.
+struct Row4 {
+    int seq, pos;
+};
+__device__ __forceinline__ Row4 row_place(const Places4 &at, int row) {
+    int seq, begin, count;
+    if (!at.ends) {
+        count = at.rows / at.batch;
+        seq = row / count;
+        begin = seq * count;
+    } else {
+        int lo = 0, hi = at.batch;      // the first sequence whose end is past the row
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (at.ends[mid] > row) hi = mid;
+            else lo = mid + 1;
+        }
+        seq = lo;
+        if (seq >= at.batch) return {-1, -1};
+        begin = seq ? at.ends[seq - 1] : 0;
+        count = at.ends[seq] - begin;
+    }
+    const int64_t pos = (int64_t)at.lens[seq] - count + (row - begin);
+    return {seq, pos < 0 || pos > 0x7fffffff ? -1 : (int)pos};
+}
+
+// The page of a position, or -1: past the table, or a page that the cache does not have.
+__device__ __forceinline__ int page_of(const Cache4 &c, const Places4 &at, int seq, int pos) {
+    const int slot = pos >> c.log_page;
+    if (pos < 0 || slot >= at.width) return -1;
+    const int page = at.table[(int64_t)seq * at.width + slot];
+    return (unsigned)page < (unsigned)c.pages ? page : -1;
+}
+
+// Sixteen adjacent channels from c0 on of a head of `dim`, zeros past its end.
+template <typename T>
+__device__ __forceinline__ void load16(const T *p, int c0, int dim, float *v) {
+    if (c0 + 16 <= dim) {
+        Raw8<T> a, b;
+        load_raw(p + c0, a);
+        load_raw(p + c0 + 8, b);
+        raw_values(a, v);
+        raw_values(b, v + 8);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = 0.0f;
+    if (c0 < dim) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c0 + j < dim) v[j] = to_float(p[c0 + j]);
+    }
+}
+__device__ __forceinline__ void load_head16(const Heads4 &x, int64_t at, int c0, int dim, float *v) {
+    if (x.type == kF32) load16(static_cast<const float *>(x.p) + at, c0, dim, v);
+    else if (x.type == kBf16) load16(static_cast<const bf16_t *>(x.p) + at, c0, dim, v);
+    else load16(static_cast<const _Float16 *>(x.p) + at, c0, dim, v);
+}
+
+template <typename T>
+__device__ __forceinline__ void put16(T *p, int c0, int dim, const float *v) {
+    if (c0 + 16 <= dim) {
+#pragma unroll
+        for (int j = 0; j < 16; j += 16 / (int)sizeof(T)) store16(p + c0 + j, v + j);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if (c0 + j < dim) p[c0 + j] = from_float<T>(v[j]);
+}
+__device__ __forceinline__ void store_head16(const Heads4 &x, int64_t at, int c0, int dim, const float *v) {
+    if (x.type == kF32) put16(static_cast<float *>(x.p) + at, c0, dim, v);
+    else if (x.type == kBf16) put16(static_cast<bf16_t *>(x.p) + at, c0, dim, v);
+    else put16(static_cast<_Float16 *>(x.p) + at, c0, dim, v);
+}
+
+// The order-2^lb butterfly of heads held 16 channels a lane and block, ascending stages;
+// other(MASK, v): the value of the lane that holds the chunk ^ MASK, up: whether this lane's
+// chunk number has the bit.
+template <int NB, typename F>
+__device__ __forceinline__ void head_butterfly(float (&v)[NB][16], int lb, int chunk, F other) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        if (lb >= 1) reg_stage<1>(v[n]);
+        if (lb >= 2) reg_stage<2>(v[n]);
+        if (lb >= 3) reg_stage<4>(v[n]);
+        if (lb >= 4) reg_stage<8>(v[n]);
+        if (lb >= 5) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float o = other(std::integral_constant<int, 1>{}, v[n][j]);
+                v[n][j] = (chunk & 1) ? o - v[n][j] : v[n][j] + o;
+            }
+        }
+        if (lb >= 6) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float o = other(std::integral_constant<int, 2>{}, v[n][j]);
+                v[n][j] = (chunk & 2) ? o - v[n][j] : v[n][j] + o;
+            }
+        }
+    }
+    if constexpr (NB % 2 == 0) {    // (a block of 128 divides the head: no odd one)
+        if (lb >= 7) {
+#pragma unroll
+            for (int n = 0; n < NB; n += 2)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float a = v[n][j], b = v[n + 1][j];
+                    v[n][j] = a + b;
+                    v[n + 1][j] = a - b;
+                }
+        }
+    }
+}
+
+// Chunks of a head in adjacent lanes (the cache's own kernels), or 16 lanes apart, as a
+// matrix instruction has them (the attention).
+struct ChunksAdjacent {
+    template <int M>
+    __device__ __forceinline__ float operator()(std::integral_constant<int, M>, float v) const { return lane_xor<M>(v); }
+};
+struct ChunksApart {
+    template <int M>
+    __device__ __forceinline__ float operator()(std::integral_constant<int, M>, float v) const {
+        const uint32_t u = __float_as_uint(v);
+        if constexpr (M == 1) {
+            const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+            return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
+        } else {
+            const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+        }
+    }
+};
+
+}  // namespace hatq

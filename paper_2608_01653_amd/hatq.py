@@ -52,6 +52,16 @@ class LinearWeights(ctypes.Structure):
                 ("bias", ctypes.c_void_p)]
 
 
+class Cache4View(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("hblock", ctypes.c_int32), ("buf", ctypes.c_void_p)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("p", ctypes.c_void_p)]
+
+
 EXPORTS = ["hatq_status_string", "hatq_conv_out_hw", "hatq_weights_bytes", "hatq_prepare_weights",
            "hatq_export_weights", "hatq_pack_weights", "hatq_fwht_quant_ws_bytes", "hatq_fwht_quant_act",
            "hatq_fwht_quant_act_noalloc", "hatq_fwht_quant_act_c64", "hatq_conv_int8",
@@ -63,7 +73,9 @@ EXPORTS = ["hatq_status_string", "hatq_conv_out_hw", "hatq_weights_bytes", "hatq
            "hatq_linear_weights_bytes", "hatq_prepare_linear", "hatq_pack_linear", "hatq_token_quant",
            "hatq_linear_int8", "hatq_linear_ws_bytes", "hatq_linear_forward", "hatq_experts_int8",
            "hatq_experts_forward", "hatq_expert_order_ws_bytes", "hatq_expert_order", "hatq_expert_combine",
-           "hatq_expert_mlp_ws_bytes", "hatq_expert_mlp"]
+           "hatq_expert_mlp_ws_bytes", "hatq_expert_mlp",
+           "hatq_cache4_bytes", "hatq_cache4_init", "hatq_cache4_append", "hatq_cache4_read",
+           "hatq_attention4_ws_bytes", "hatq_attention4"]
 
 _lib = None
 
@@ -164,6 +176,18 @@ def load(build_if_missing: bool = False):
     L.hatq_expert_mlp_ws_bytes.restype = sz
     L.hatq_expert_mlp.argtypes = [W, W, P, i32, i32, i64, P, P, i32, P, i32, i64, P, sz, P]
     L.hatq_expert_mlp.restype = i32
+    C, H, f32 = ctypes.POINTER(Cache4View), ctypes.POINTER(Heads), ctypes.c_float
+    L.hatq_cache4_bytes.argtypes = [i32] * 5
+    L.hatq_cache4_bytes.restype = sz
+    L.hatq_cache4_init.argtypes = [i32, i32, i32, i32, i32, P, sz, C]
+    L.hatq_cache4_init.restype = i32
+    for f in (L.hatq_cache4_append, L.hatq_cache4_read):
+        f.argtypes = [C, H, H, i32, P, i32, P, P, i32, P]
+        f.restype = i32
+    L.hatq_attention4_ws_bytes.argtypes = [C, i32, i32, i32, i32, i32, i32]
+    L.hatq_attention4_ws_bytes.restype = sz
+    L.hatq_attention4.argtypes = [C, H, H, i32, i32, P, i32, P, P, i32, f32, i32, i32, i32, P, sz, P]
+    L.hatq_attention4.restype = i32
     _lib = L
     return L
 
@@ -970,4 +994,164 @@ def hatq_expert_mlp(w_in: PreparedLinear, w_out: PreparedLinear, x: torch.Tensor
     _check(load().hatq_expert_mlp(w_in.ref, w_out.ref, x.data_ptr(), xt, n, xs, ids.data_ptr(), weights.data_ptr(),
                                   topk, y.data_ptr(), yt, ys, ws.data_ptr(), ws.numel(), _stream()),
            "hatq_expert_mlp")
+    return y
+
+
+@dataclass
+class Cache4:
+    """A cache of keys and values in 4 bits: the device buffer and the C view of it."""
+    buf: torch.Tensor
+    c: Cache4View
+    pages: int
+    page_size: int
+    heads: int
+    dim: int
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.c)
+        self.device = self.buf.get_device()
+
+
+def _here(device: int, *tensors: Optional[torch.Tensor]):
+    """Raise ValueError unless the tensors are on `device` and it is the current one (the
+    calls go to its current stream)."""
+    if device != torch._C._cuda_getDevice():
+        raise ValueError(f"device {device} expected to be the current one")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors on device {device} expected, got one on {t.device}")
+
+
+def hatq_cache4_bytes(pages: int, page_size: int, heads: int, dim: int, hblock: int = 1) -> int:
+    _sizes("sizes", pages, page_size, heads, dim, hblock)
+    return int(load().hatq_cache4_bytes(pages, page_size, heads, dim, hblock))
+
+
+def hatq_cache4_init(pages: int, page_size: int, heads: int, dim: int, hblock: int = 1,
+                     buf: Optional[torch.Tensor] = None, device="cuda") -> Cache4:
+    """A cache of `pages` pages of page_size positions, in the given int8 buffer or a new
+    one.  Its contents need no clearing."""
+    nbytes = hatq_cache4_bytes(pages, page_size, heads, dim, hblock)
+    if buf is None:
+        buf = torch.empty(max(nbytes, 1), dtype=torch.int8, device=device)
+    _need(buf, "buf", torch.int8, 0)
+    out = Cache4View()
+    _check(load().hatq_cache4_init(pages, page_size, heads, dim, hblock, buf.data_ptr(), buf.numel(),
+                                   ctypes.byref(out)), "hatq_cache4_init")
+    return Cache4(buf, out, pages, page_size, heads, dim)
+
+
+def _heads(t: torch.Tensor, name: str, dim: int, heads: Optional[int] = None, rows: Optional[int] = None):
+    """(rows, heads, C view) of a device tensor [rows, heads, dim] with adjacent channels."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name}: [rows, heads, {dim}] expected")
+    n, h, d = t.shape
+    if not t.is_cuda:
+        raise ValueError(f"{name}: device tensor expected")
+    if d != dim or (heads is not None and h != heads) or (rows is not None and n != rows):
+        raise ValueError(f"{name}: [{'rows' if rows is None else rows}, {'heads' if heads is None else heads}, {dim}] "
+                         f"expected, got {tuple(t.shape)}")
+    if n > _I32 or h > _I32:
+        _sizes(name, n, h)
+    by_row, by_head, inner = t.stride()
+    if inner != 1 and d > 1:
+        raise ValueError(f"{name}: adjacent channels expected")
+    if h <= 1:
+        by_head = d
+    if n <= 1:
+        by_row = max(h, 1) * by_head
+    return n, h, Heads(_dtype(t.dtype, name), by_row, by_head, t.data_ptr())
+
+
+def _places(cache: Cache4, rows: int, table: torch.Tensor, lens: torch.Tensor, ends: Optional[torch.Tensor]):
+    """(batch, width) of the sequences' table."""
+    if table.dim() != 2:
+        raise ValueError(f"table: [batch, width] expected, got {tuple(table.shape)}")
+    batch, width = table.shape
+    _need(table, "table", torch.int32, 0)
+    _need(lens, "lens", torch.int32, batch)
+    _need(ends, "ends", torch.int32, batch, optional=True)
+    if batch > _I32 or width > _I32:
+        _sizes("table", batch, width)
+    if ends is None and batch and rows % batch:
+        raise ValueError(f"{rows} rows of {batch} sequences: ends expected")
+    return batch, width
+
+
+def hatq_cache4_append(cache: Cache4, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                       ends: Optional[torch.Tensor] = None, stream=None) -> None:
+    """New tokens' keys and values [rows, heads, dim] into the cache, as the last positions
+    of their sequences: table int32 [batch, width], lens int32 [batch] with the new tokens
+    counted, ends int32 [batch] the sequences' row ends (None: as many rows each)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_cache4_append(cache, k, v, table, lens, ends)
+    n, _, hk = _heads(k, "k", cache.dim, cache.heads)
+    _, _, hv = _heads(v, "v", cache.dim, cache.heads, n)
+    batch, width = _places(cache, n, table, lens, ends)
+    _here(cache.device, k, v, table, lens, ends)
+    _check(load().hatq_cache4_append(cache.ref, ctypes.byref(hk), ctypes.byref(hv), n, table.data_ptr(), width,
+                                     lens.data_ptr(), _ptr(ends), batch, _stream()), "hatq_cache4_append")
+
+
+def hatq_cache4_read(cache: Cache4, rows: int, table: torch.Tensor, lens: torch.Tensor,
+                     ends: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32,
+                     k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """What the cache holds of the sequences' last positions, `rows` of them: keys and values
+    [rows, heads, dim] of out_dtype (or of the given k and v).  New tensors are cleared first
+    where ends is given, since rows past the last end are not written."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_cache4_read(cache, rows, table, lens, ends, out_dtype, k, v)
+    _sizes("rows", rows)
+    new = torch.empty if ends is None else torch.zeros
+    if k is None:
+        k = new((rows, cache.heads, cache.dim), dtype=out_dtype, device=cache.buf.device)
+    if v is None:
+        v = new((rows, cache.heads, cache.dim), dtype=out_dtype, device=cache.buf.device)
+    _, _, hk = _heads(k, "k", cache.dim, cache.heads, rows)
+    _, _, hv = _heads(v, "v", cache.dim, cache.heads, rows)
+    batch, width = _places(cache, rows, table, lens, ends)
+    _here(cache.device, k, v, table, lens, ends)
+    _check(load().hatq_cache4_read(cache.ref, ctypes.byref(hk), ctypes.byref(hv), rows, table.data_ptr(), width,
+                                   lens.data_ptr(), _ptr(ends), batch, _stream()), "hatq_cache4_read")
+    return k, v
+
+
+def hatq_attention4_ws_bytes(cache: Cache4, rows: int, q_heads: int, width: int, batch: int, ragged: bool = False,
+                             max_len: int = 0) -> int:
+    _sizes("sizes", rows, q_heads, width, batch, max_len)
+    return int(load().hatq_attention4_ws_bytes(cache.ref, rows, q_heads, width, batch, int(ragged), max_len))
+
+
+def hatq_attention4(cache: Cache4, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                    ends: Optional[torch.Tensor] = None, scale: Optional[float] = None, causal: bool = True,
+                    window: int = 0, max_len: int = 0, out_dtype: Optional[torch.dtype] = None,
+                    y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Query rows q [rows, q_heads, dim] over their sequences' positions in the cache: y
+    [rows, q_heads, dim] of out_dtype (default: q's).  table, lens, ends as
+    hatq_cache4_append, whose tokens the rows are; scale: dim ** -0.5 if None; window: as
+    many positions, the row's own the last of them (0: all); max_len: what the lengths will
+    not exceed, for the choice of the launch.  A new y is cleared first where ends is given,
+    since rows past the last end are not written."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_attention4(cache, q, table, lens, ends, scale, causal, window, max_len, out_dtype, y, ws)
+    n, h, hq = _heads(q, "q", cache.dim)
+    if y is None:
+        y = (q.new_empty if ends is None else q.new_zeros)((n, h, cache.dim), dtype=out_dtype or q.dtype)
+    _, _, hy = _heads(y, "y", cache.dim, h, n)
+    batch, width = _places(cache, n, table, lens, ends)
+    _sizes("window, max_len", window, max_len)
+    _here(cache.device, q, y, table, lens, ends, ws)
+    if ws is None:
+        nbytes = load().hatq_attention4_ws_bytes(cache.ref, n, h, width, batch, int(ends is not None), max_len)
+        if nbytes:
+            ws = torch.empty(nbytes, dtype=torch.int8, device=q.device)
+    _need(ws, "ws", torch.int8, 0, optional=True)
+    _check(load().hatq_attention4(cache.ref, ctypes.byref(hq), ctypes.byref(hy), n, h, table.data_ptr(), width,
+                                  lens.data_ptr(), _ptr(ends), batch, cache.dim ** -0.5 if scale is None else scale,
+                                  int(causal), window, max_len, _ptr(ws), 0 if ws is None else ws.numel(), _stream()),
+           "hatq_attention4")
     return y
