@@ -596,6 +596,61 @@ int32_t hatq_expert_mlp(const hatq_linear_weights *W_in, const hatq_linear_weigh
                         int32_t topk, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,
                         void *stream);
 
+/* ---- Linear layers of 4-bit weights ---------------------------------------------
+ *
+ * hatq_linear_forward's layer with 15 (or 16) levels of weights and a scale for each
+ * channel and group of `group` adjacent input channels, for the bytes that a few tokens
+ * have to read: tokens as there (S, s and q of each token t, its codes INT8), and
+ *   z[t,c] = (s[t] / b) sum_g w_scale[c,g] float(sum_{d in g} q[t,d] wq[c,d]) + bias[c]
+ * with exact sums in each group and fp32 sums over the groups; y from z as there, gated or
+ * not.  A NaN among a channel's scales makes its outputs NaN, a token that is not finite
+ * its own.
+ * Any number of rows is taken; the kernels are made for up to about 128. */
+typedef struct {
+    int32_t cin, cout;
+    int32_t gated;          /* 1: holds 2 cout channels, gives cout */
+    int32_t hblock;         /* transform block on cin, a power of two in [1, 128] */
+    int32_t group;          /* 64 or 128 input channels */
+    int32_t k_stride;       /* cin rounded up to 128 */
+    int32_t cout_pad;       /* the channels held: cout rounded up to 16, twice if gated */
+    uint8_t *wpack;         /* library-internal order, as w_scale and bias */
+    uint16_t *w_scale;      /* bf16 [cout_pad][k_stride / group] */
+    float *bias;
+} hatq_linear4_weights;
+
+/* Bytes of device memory for such weights; 0 for sizes that are not supported (cin %
+ * hblock != 0, cin or held channels over 65536). */
+size_t hatq_linear4_weights_bytes(int32_t cin, int32_t cout, int32_t gated, int32_t hblock, int32_t group);
+
+/* Weights from floats: w device [held][cin] of w_type (held = cout, or 2 cout for a gated
+ * layer: gates, then values), bias device fp32 [held] or NULL.  W' = B w in fp64, rounded
+ * once to fp32; for each group w_scale = bf16(fl32(max|W'| / 7)), at least 2^-100, and codes
+ * clamp(rne(fl32(W' / w_scale)), -7, 7).  A group with a NaN or an infinity among its W'
+ * has the scale NaN and codes 0.
+ *   dst: device buffer of at least hatq_linear4_weights_bytes, 256-byte aligned; *out
+ *   receives the view into it.  Runs on `stream`. */
+int32_t hatq_prepare_linear4(int32_t cin, int32_t cout, int32_t gated, int32_t hblock, int32_t group, const void *w,
+                             int32_t w_type, const float *bias, void *dst, size_t dst_bytes,
+                             hatq_linear4_weights *out, void *stream);
+
+/* The same from codes quantized elsewhere (a deployment checkpoint): codes device int8
+ * [held][cin] of the transformed weights, taken into [-8, 7]; w_scale device bf16
+ * [held][groups], groups = cin / group rounded up. */
+int32_t hatq_pack_linear4(int32_t cin, int32_t cout, int32_t gated, int32_t hblock, int32_t group,
+                          const int8_t *codes, const uint16_t *w_scale, const float *bias, void *dst,
+                          size_t dst_bytes, hatq_linear4_weights *out, void *stream);
+
+/* The whole layer, floats in.
+ *   x: device [rows][cin] of x_type, row stride x_stride >= cin elements;
+ *   y: device [rows][cout] of y_type, row stride y_stride >= cout elements.
+ *   ws: device memory, 256-byte aligned, of at least hatq_linear4_ws_bytes(W, rows) bytes;
+ *       may be NULL where that is 0 (a few tokens: rows <= HATQ_TOKEN_ROWS and rows k_stride
+ *       <= HATQ_TOKEN_CODES).  Calls that may overlap need workspaces of their own. */
+size_t hatq_linear4_ws_bytes(const hatq_linear4_weights *W, int32_t rows);
+int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32_t x_type, int32_t rows,
+                             int64_t x_stride, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,
+                             void *stream);
+
 /* ---- A cache of keys and values in 4 bits, and attention over it ------------------
  *
  * The symmetric quantizer of Eq. symmetric_q with 15 levels in the Hadamard domain, for

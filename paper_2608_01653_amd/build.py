@@ -21,8 +21,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhatq.so")
-SOURCES = ["api.cpp", "api_cache4.cpp", "api_linear.cpp", "act_quant.hip", "attention4.hip", "attention4_plan.cpp",
-           "cache4.hip", "conv_i8.hip", "linear.hip", "linear_choice.cpp", "tokens.hip", "weights.hip"]
+SOURCES = ["api.cpp", "api_cache4.cpp", "api_linear.cpp", "api_linear4.cpp", "act_quant.hip", "attention4.hip",
+           "attention4_plan.cpp", "cache4.hip", "conv_i8.hip", "linear.hip", "linear4.hip", "linear_choice.cpp", "tokens.hip", "weights.hip"]
 CONV_PARTS = 18         # HATQ_CONV_PART = 0 .. 17 in conv_i8.hip
 ATTENTION_PARTS = 4     # HATQ_ATTENTION_PART = 1 .. 4 in attention4.hip
 OBJ_DIR = os.path.join(ROOT, "_build", "hatq")

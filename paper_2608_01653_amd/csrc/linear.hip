@@ -106,35 +106,6 @@ __device__ __forceinline__ int token_of(const LinearArgs &a, int row) {
 }
 
 // ---- epilogue -----------------------------------------------------------------------
-// g[j] = g[j] / (1 + exp(-g[j])) u[j], each operation as its fp32 function: the same bits as
-// g / (1 + expf(-g)) u.  exp(-g) = 2^n 2^f: p = fl(-g log2 e), n = rne(p) in the low bits of
-// p + 1.5 2^23, and f = (p - n) + the product's rest, so its error does not grow with |g|;
-// |g| < 87 keeps 2^n 2^f normal and n its exponent's shift.  The quotient is g times the
-// reciprocal with one step of correction.  Groups with a larger gate, an infinity or a NaN
-// divide.  (The exponential and reciprocal alone, with p for n + f, lost up to 60 ulp at g =
-// -80 and moved a code of the next layer now and then.  Whole call of 8192 x 4096 -> 2 x 8192: 516
-// us with them, 529 so, 545 with the division for every element.)
-__device__ __forceinline__ void gated4(float *g, const float *u) {
-    float m = 0.0f, y[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float p = g[j] * -1.44269504f, t = p + HATQ_MAGIC;
-        // (log2 e = 1.44269504f + 1.92596303e-8f - 4.2e-16)
-        const float f = __builtin_fmaf(g[j], -1.92596303e-8f, __builtin_fmaf(g[j], -1.44269504f, -p)) + (p - (t - HATQ_MAGIC));
-        const float e = __uint_as_float((__float_as_uint(t) << 23) + __float_as_uint(__builtin_amdgcn_exp2f(f)));
-        const float d = 1.0f + e, r = __builtin_amdgcn_rcpf(d), q = g[j] * r;
-        y[j] = __builtin_fmaf(__builtin_fmaf(-q, d, g[j]), r, q);
-        m = __builtin_elementwise_maximum(m, fabsf(g[j]));
-    }
-    if (!(m < 87.0f)) {
-        asm volatile("");   // a branch: else the compiler divides for every group and selects
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = g[j] / (1.0f + expf(-g[j]));
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) g[j] = y[j] * u[j];
-}
-
 // z of four adjacent packed columns with factors at w_scale and bias (memory or LDS); s =
 // the token's scale times 1/b, a power of two: exact unless it is below 2^-126.
 __device__ __forceinline__ void dequant4(const float *w_scale, const float *bias, const int *acc, float s, float *z) {
@@ -143,23 +114,6 @@ __device__ __forceinline__ void dequant4(const float *w_scale, const float *bias
     z[1] = __builtin_fmaf((float)acc[1], s * w.y, b.y);
     z[2] = __builtin_fmaf((float)acc[2], s * w.z, b.z);
     z[3] = __builtin_fmaf((float)acc[3], s * w.w, b.w);
-}
-
-template <typename T>
-__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z) {
-    T *y = static_cast<T *>(a.y) + row * a.y_stride + c;
-    if (c + 4 <= a.cout) {
-        store4(y, z);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < a.cout) y[j] = from_float<T>(z[j]);
-    }
-}
-__device__ __forceinline__ void put4(const LinearArgs &a, int64_t row, int c, const float *z) {
-    if (a.y_type == kBf16) put4<bf16_t>(a, row, c, z);
-    else if (a.y_type == kF16) put4<_Float16>(a, row, c, z);
-    else put4<float>(a, row, c, z);
 }
 
 // Rows of a tile past the last end: BN outputs each of zeros.
@@ -186,30 +140,6 @@ __device__ __forceinline__ void finish16(const LinearArgs &a, const float *w_sca
     }
     if (G == 2) gated4(z[0], z[1]);
     if (row < end && c < a.cout) put4(a, row, c, z[0]);
-}
-
-// A token's row, and the elements that it has (none for an empty one).
-template <typename T>
-struct TokenRow {
-    const T *p;
-    int n;
-};
-template <typename T>
-__device__ __forceinline__ TokenRow<T> token_row(const TokenArgs &x, int row) {
-    return {static_cast<const T *>(x.x) + max(row, 0) * x.x_stride, row < 0 ? 0 : x.cin};
-}
-
-// The codes of a token's chunks (load_chunks), to LDS.
-template <int CH, int THREADS>
-__device__ __forceinline__ void store_chunks(int8_t *to, int k_stride, int t, const float (&v)[8 * CH], float sigma, float s) {
-    const float r = sigma * (1.0f / s);
-    const bool plain = token_plain(s);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        const int c = i * THREADS + t;
-        const uint2 q = token_codes8(&v[8 * i], sigma, s, r, plain);
-        if (c < k_stride >> 3) *reinterpret_cast<uint2 *>(to + c * 8) = q;
-    }
 }
 
 // ---- few rows -------------------------------------------------------------------------

@@ -1,0 +1,385 @@
+// Linear layers of 4-bit weights with a scale for each group of input channels, over a few
+// tokens in INT8 codes:
+//   z = (s / b) sum_g w_scale[c][g] float(sum_{d in g} q[d] wq[c][d]) + bias
+// Exact INT32 sums in each group (INT8 matrix instructions, 64 channels a step; a code enters
+// as 16 times itself, the upper half of a byte), fp32 sums over the groups.
+//
+// Packed weights: 16 channels by 128 input channels, 1 KB in lane order: lane 16 u + c has
+// channel c and input channels 16 u .. 16 u + 15 of both 64-channel steps, 8 bytes each;
+// byte b of a step's word w holds the codes of input channels 8 w + b (low half) and 8 w + 4
+// + b.  Their scales: [4][steps with scales of their own][4 channels] bf16, lane 16 u + c
+// takes the u-th part, which belongs to the channels of its sums.  A gated layer's channels
+// go 16 gates, 16 values in turn.
+#include "linear4.h"
+
+#include "../../include/hatq.h"
+#include "linear_device.h"
+
+namespace hatq {
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+constexpr int kWaves = 8;
+constexpr int kThreads = 256;
+
+// One tile of 16 channels by 128 input channels as it lies in memory: codes, and the scales
+// of this lane's sums (S = 2: of both steps, 1: of the whole).
+template <int S>
+struct Tile {
+    v4u code;
+    uint32_t scale[2 * S];
+};
+template <int S>
+__device__ __forceinline__ void load_tile(const uint8_t *code, const uint16_t *scale, int lane, Tile<S> &t) {
+    t.code = *reinterpret_cast<const v4u *>(code + lane * 16);
+    const uint16_t *s = scale + (lane >> 4) * (4 * S);
+    if constexpr (S == 2) {
+        const v4u w = *reinterpret_cast<const v4u *>(s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t.scale[i] = w[i];
+    } else {
+        const uint2 w = *reinterpret_cast<const uint2 *>(s);
+        t.scale[0] = w.x;
+        t.scale[1] = w.y;
+    }
+}
+__device__ __forceinline__ float bf16_of(const uint32_t *w, int j) {
+    return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+}
+
+// The tile's products with MT times 16 tokens, x: their codes of both steps.
+template <int S, int MT>
+__device__ __forceinline__ void multiply(const Tile<S> &t, const v4i (&x)[MT][2], v4f (&acc)[MT]) {
+    v4i w[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            w[k][2 * i] = (int)((t.code[2 * k + i] << 4) & 0xf0f0f0f0u);
+            w[k][2 * i + 1] = (int)(t.code[2 * k + i] & 0xf0f0f0f0u);
+        }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        v4i sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[0], x[m][0], v4i{0, 0, 0, 0}, 0, 0, 0);
+        if constexpr (S == 2) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[m][r] = __builtin_fmaf((float)sum[r], bf16_of(t.scale, r), acc[m][r]);
+            sum = v4i{0, 0, 0, 0};
+        }
+        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[1], x[m][1], sum, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            acc[m][r] = __builtin_fmaf((float)sum[r], bf16_of(t.scale, 4 * (S - 1) + r), acc[m][r]);
+    }
+}
+
+// This lane's outputs of one 16 x 16 tile: channels 16 c16 + 4 (lane / 16) and on of `row`.
+// s: the token's scale / b.
+template <int G>
+__device__ __forceinline__ void finish(const Linear4Args &a, const v4f (&sum)[G], float s, int row, int c16, int lane) {
+    float z[2][4];
+    const int c = c16 * 16 + (lane >> 4) * 4;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const float4 b = *reinterpret_cast<const float4 *>(a.bias + (c16 * G + g) * 16 + (lane >> 4) * 4);
+        const float bias[4] = {b.x, b.y, b.z, b.w};
+        // (the codes came 16 times too large)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[g][r] = __builtin_fmaf(sum[g][r] * 0.0625f, s, bias[r]);
+    }
+    if (G == 2) gated4(z[0], z[1]);
+    if (row < a.rows && c < a.cout) put4(a, row, c, z[0]);
+}
+
+// ---- a few tokens, floats in -----------------------------------------------------------
+// Every block takes 16 channels (gated: and their values), quantizes the rows itself while
+// its first weights are under way, and its waves take the tiles in turn.
+template <typename T, int G, int S, int CH>
+__global__ void __launch_bounds__(64 * kWaves) linear4_token_kernel(const Linear4Args a, const TokenArgs x) {
+    constexpr int U = 4;
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    v4f(*part)[G][64] = reinterpret_cast<v4f(*)[G][64]>(lds);            // [kWaves][G][64]
+    float *scale = reinterpret_cast<float *>(lds + kWaves * G * 1024);      // [16]
+    float *most = scale + 16;                                              // [kWaves]
+    int8_t *codes = lds + kWaves * G * 1024 + 128;                          // [rows][k_stride + 16]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c16 = blockIdx.x, rows = a.rows;
+    const int pitch = a.k_stride + 16;   // 16 rows' pieces then lie in different banks
+    TokenRow<T> token = token_row<T>(x, 0);
+    Raw8<T> raw[CH] = {};
+    load_chunks<T, CH, 512>(token.p, token.n, threadIdx.x, raw);
+
+    const int tiles = a.k_stride >> 7;
+    const uint8_t *w = a.wp + (int64_t)c16 * G * tiles * 1024;
+    const uint16_t *ws = a.w_scale + (int64_t)c16 * G * tiles * (16 * S);
+    Tile<S> t[U][G];
+    auto weights = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int k = g * tiles + min(k0 + kWaves * u, tiles - 1);
+                load_tile<S>(w + (int64_t)k * 1024, ws + (int64_t)k * (16 * S), lane, t[u][g]);
+            }
+    };
+    weights(wave);
+    __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
+
+    for (int row = 0; row < rows; ++row) {
+        float v[8 * CH];
+        chunk_values<T, CH, 512>(token.p, token.n, threadIdx.x, raw, v);
+        if (row + 1 < rows) {   // the next row, under way over this one's codes
+            token = token_row<T>(x, row + 1);
+            load_chunks<T, CH, 512>(token.p, token.n, threadIdx.x, raw);
+        }
+        const float sigma = token_butterfly(v, lane, x.log_b);
+        float m = token_max(v);
+        if (row) __syncthreads();   // the row before has been read
+        if (lane == 0) most[wave] = m;
+        __syncthreads();
+        m = most[0];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k) m = __builtin_elementwise_maximum(m, most[k]);
+        const float s = token_scale(m);
+        if (threadIdx.x == 0) scale[row] = s * a.inv_b;
+        store_chunks<CH, 512>(codes + row * pitch, a.k_stride, threadIdx.x, v, sigma, s);
+    }
+    __syncthreads();
+
+    const int mine = min(lane & 15, rows - 1);
+    const int8_t *from = codes + mine * pitch + (lane >> 4) * 16;
+    v4f acc[G][1];
+#pragma unroll
+    for (int g = 0; g < G; ++g) acc[g][0] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = wave; k0 < tiles; k0 += kWaves * U) {
+        if (k0 != wave) weights(k0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k0 + kWaves * u >= tiles) break;
+            const v4i *c = reinterpret_cast<const v4i *>(from + (k0 + kWaves * u) * 128);
+            const v4i fx[1][2] = {{c[0], c[4]}};
+#pragma unroll
+            for (int g = 0; g < G; ++g) multiply<S, 1>(t[u][g], fx, acc[g]);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) part[wave][g][lane] = acc[g][0];
+    __syncthreads();
+    if (wave != 0) return;
+    v4f sum[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        sum[g] = part[0][g][lane];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k) sum[g] += part[k][g][lane];
+    }
+    finish<G>(a, sum, scale[mine], (lane & 15) < rows ? lane & 15 : rows, c16, lane);
+}
+
+// ---- codes from memory ------------------------------------------------------------------
+// Waves of a block take 16 channels by 16 MT rows, `wk` of them the tiles of the contraction
+// in turn (they add up in LDS), the others channels further on.
+template <int G, int S, int MT>
+__global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linear4Args a, int wk) {
+    constexpr int U = MT == 1 ? 4 : 2;
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    v4f(*part)[G][MT][64] = reinterpret_cast<v4f(*)[G][MT][64]>(lds);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_k = wave & (wk - 1);
+    const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16;
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int row0 = (int)(block % row_tiles) * (16 * MT);
+    const int64_t c16_ = block / row_tiles * (kWaves / wk) + wave / wk;
+    const int c16 = (int)(c16_ < groups ? c16_ : groups - 1);
+    const int tiles = a.k_stride >> 7;
+    const uint8_t *w = a.wp + (int64_t)c16 * G * tiles * 1024;
+    const uint16_t *ws = a.w_scale + (int64_t)c16 * G * tiles * (16 * S);
+    const int8_t *from[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+        from[m] = a.xq + (int64_t)min(row0 + 16 * m + (lane & 15), a.rows - 1) * a.k_stride + (lane >> 4) * 16;
+    v4f acc[G][MT];
+#pragma unroll
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[g][m] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k0 = part_k; k0 < tiles; k0 += wk * U) {
+        Tile<S> t[U][G];
+        v4i fx[U][MT][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = min(k0 + wk * u, tiles - 1);
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+                load_tile<S>(w + (int64_t)(g * tiles + k) * 1024, ws + (int64_t)(g * tiles + k) * (16 * S), lane, t[u][g]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const v4i *c = reinterpret_cast<const v4i *>(from[m] + k * 128);
+                fx[u][m][0] = c[0];
+                fx[u][m][1] = c[4];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k0 + wk * u >= tiles) break;
+#pragma unroll
+            for (int g = 0; g < G; ++g) multiply<S, MT>(t[u][g], fx[u], acc[g]);
+        }
+    }
+    if (wk > 1) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) part[wave][g][m][lane] = acc[g][m];
+        __syncthreads();
+        if (part_k) return;
+        for (int k = 1; k < wk; ++k)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[g][m] += part[wave + k][g][m][lane];
+    }
+    if (c16_ >= groups) return;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        const int row = row0 + 16 * m + (lane & 15);
+        v4f sum[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) sum[g] = acc[g][m];
+        finish<G>(a, sum, a.sx[min(row, a.rows - 1)] * a.inv_b, row, c16, lane);
+    }
+}
+
+// ---- weights --------------------------------------------------------------------------
+// Held channel of packed column p, or -1 in the padding.
+__device__ __forceinline__ int held_channel(const Linear4PrepArgs &a, int p) {
+    if (!a.gated) return p < a.cout ? p : -1;
+    const int c = (p >> 5) * 16 + (p & 15);
+    return c >= a.cout ? -1 : (p & 16) ? a.cout + c : c;
+}
+
+// Where packed column p keeps the code of input channel d: its byte, and the bits in it.
+__device__ __forceinline__ int64_t code_byte(const Linear4PrepArgs &a, int p, int d) {
+    const int step = (d >> 6) & 1, chunk = (d >> 4) & 3, w = (d >> 3) & 1;
+    return ((int64_t)(p >> 4) * (a.k_stride >> 7) + (d >> 7)) * 1024 + (chunk * 16 + (p & 15)) * 16 + step * 8 + w * 4 + (d & 3);
+}
+__device__ __forceinline__ int64_t scale_index(const Linear4PrepArgs &a, int p, int g) {
+    const int S = 128 / a.group, c = p & 15;
+    return (((int64_t)(p >> 4) * (a.k_stride >> 7) + g / S) * 4 + (c >> 2)) * (4 * S) + g % S * 4 + (c & 3);
+}
+
+template <typename T>
+__device__ float transformed4(const T *w, int d, int b) {
+    const int first = d & ~(b - 1), i = d & (b - 1);
+    double acc = 0.0;
+    for (int j = 0; j < b; ++j) {
+        const double e = (double)to_float(w[first + j]);
+        acc += (__popc(i & j) & 1) ? -e : e;
+    }
+    return (float)acc;
+}
+
+// One wave a packed column and group.  W' = B w in fp64, rounded once to fp32; its scale
+// bf16(fl32(max |W'| / 7)), at least 2^-100, codes clamp(rne(fl32(W' / s)), -7, 7).
+template <typename T, bool CODES>
+__global__ void __launch_bounds__(kThreads) linear4_prepare_kernel(const Linear4PrepArgs a) {
+    const int groups = (a.k_stride + a.group - 1) / a.group;
+    const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+    if (unit >= (int64_t)a.cout_pad * groups) return;
+    const int lane = threadIdx.x & 63, p = (int)(unit / groups), g = (int)(unit - (int64_t)p * groups);
+    const int ch = held_channel(a, p), given = (a.cin + a.group - 1) / a.group;
+    const int per = a.group >> 6;       // values a lane
+    // two codes a byte: channels d and d + 4, lanes 4 apart
+    float v[2] = {0.0f, 0.0f};
+    int q[2] = {0, 0};
+    for (int i = 0; i < per; ++i) {
+        const int d = g * a.group + i * 64 + lane;
+        if (ch < 0 || d >= a.cin) continue;
+        if (CODES) q[i] = max(-8, min(7, (int)a.codes[(int64_t)ch * a.cin + d]));
+        else v[i] = transformed4(static_cast<const T *>(a.w) + (int64_t)ch * a.cin, d, a.hblock);
+    }
+    uint16_t scale = 0;
+    if (CODES) {
+        if (ch >= 0 && g < given) scale = a.scale_in[(int64_t)ch * given + g];
+    } else if (ch >= 0) {
+        const float m = token_max(v);       // NaN kept
+        const bool fine = m < __builtin_inff();
+        const float s = fmaxf(__uint_as_float(bf16_pair(m / 7.0f, 0.0f) << 16), 0x1p-100f);
+        for (int i = 0; i < 2; ++i) q[i] = fine ? (int)__builtin_amdgcn_fmed3f(rintf(v[i] / s), -7.0f, 7.0f) : 0;
+        scale = fine ? (uint16_t)(__float_as_uint(s) >> 16) : (uint16_t)0x7fc0;
+    }
+    for (int i = 0; i < per; ++i) {
+        const int d = g * a.group + i * 64 + lane;
+        const int other = __shfl_xor(q[i], 4, 64);
+        if (!(lane & 4) && d < a.k_stride) a.wpack[code_byte(a, p, d)] = (uint8_t)((q[i] & 15) | (other & 15) << 4);
+    }
+    if (lane == 0) a.w_scale[scale_index(a, p, g)] = scale;
+    if (lane == 0 && g == 0) a.bias[p] = ch >= 0 && a.bias_in ? a.bias_in[ch] : 0.0f;
+}
+
+template <typename T, bool CODES>
+void prepare(const Linear4PrepArgs &a, hipStream_t st) {
+    const int64_t units = (int64_t)a.cout_pad * ((a.k_stride + a.group - 1) / a.group);
+    linear4_prepare_kernel<T, CODES><<<grid_of((units + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
+}
+
+template <typename T, int G, int S>
+void token(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
+    const int grid = (a.cout + 15) / 16;
+    const size_t bytes = kWaves * G * 1024 + 128 + (size_t)a.rows * (a.k_stride + 16);
+    if (a.k_stride <= 4096) linear4_token_kernel<T, G, S, 1><<<grid, 512, bytes, st>>>(a, x);
+    else if (a.k_stride <= 8192) linear4_token_kernel<T, G, S, 2><<<grid, 512, bytes, st>>>(a, x);
+    else linear4_token_kernel<T, G, S, 4><<<grid, 512, bytes, st>>>(a, x);
+}
+template <int G, int S>
+void token(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
+    if (x.x_type == kF32) token<float, G, S>(a, x, st);
+    else if (x.x_type == kBf16) token<bf16_t, G, S>(a, x, st);
+    else token<_Float16, G, S>(a, x, st);
+}
+
+template <int G, int S, int MT>
+void stream(const Linear4Args &a, hipStream_t st) {
+    const int64_t groups = (a.cout + 15) / 16, row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
+    const int tiles = a.k_stride >> 7;
+    // waves on one group while the groups do not fill the card, and while each has a tile
+    int wk = 1;
+    while (wk < kWaves && 2 * wk <= tiles && groups * row_tiles * wk < 4096) wk *= 2;
+    const int cols = kWaves / wk;
+    const size_t bytes = wk > 1 ? (size_t)kWaves * G * MT * 1024 : 0;
+    linear4_stream_kernel<G, S, MT><<<grid_of((groups + cols - 1) / cols * row_tiles), 512, bytes, st>>>(a, wk);
+}
+template <int G, int S>
+void stream(const Linear4Args &a, hipStream_t st) {
+    if (a.rows <= 16) stream<G, S, 1>(a, st);
+    else if (a.rows <= 32) stream<G, S, 2>(a, st);
+    else stream<G, S, 4>(a, st);
+}
+
+}  // namespace
+
+bool linear4_takes_tokens(int32_t rows, int32_t k_stride) {
+    return rows <= HATQ_TOKEN_ROWS && (int64_t)rows * k_stride <= HATQ_TOKEN_CODES;
+}
+
+hipError_t launch_linear4_prepare(const Linear4PrepArgs &a, hipStream_t st) {
+    if (a.codes) prepare<float, true>(a, st);
+    else if (a.w_type == kBf16) prepare<bf16_t, false>(a, st);
+    else if (a.w_type == kF16) prepare<_Float16, false>(a, st);
+    else prepare<float, false>(a, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_linear4_tokens(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
+    if (a.gated) a.group == 64 ? token<2, 2>(a, x, st) : token<2, 1>(a, x, st);
+    else a.group == 64 ? token<1, 2>(a, x, st) : token<1, 1>(a, x, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_linear4(const Linear4Args &a, hipStream_t st) {
+    if (a.gated) a.group == 64 ? stream<2, 2>(a, st) : stream<2, 1>(a, st);
+    else a.group == 64 ? stream<1, 2>(a, st) : stream<1, 1>(a, st);
+    return hipGetLastError();
+}
+
+}  // namespace hatq

@@ -52,6 +52,13 @@ class LinearWeights(ctypes.Structure):
                 ("bias", ctypes.c_void_p)]
 
 
+class Linear4Weights(ctypes.Structure):
+    _fields_ = [("cin", ctypes.c_int32), ("cout", ctypes.c_int32), ("gated", ctypes.c_int32),
+                ("hblock", ctypes.c_int32), ("group", ctypes.c_int32), ("k_stride", ctypes.c_int32),
+                ("cout_pad", ctypes.c_int32), ("wpack", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p)]
+
+
 class Cache4View(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
                 ("dim", ctypes.c_int32), ("hblock", ctypes.c_int32), ("buf", ctypes.c_void_p)]
@@ -74,7 +81,8 @@ EXPORTS = ["hatq_status_string", "hatq_conv_out_hw", "hatq_weights_bytes", "hatq
            "hatq_linear_int8", "hatq_linear_ws_bytes", "hatq_linear_forward", "hatq_experts_int8",
            "hatq_experts_forward", "hatq_expert_order_ws_bytes", "hatq_expert_order", "hatq_expert_combine",
            "hatq_expert_mlp_ws_bytes", "hatq_expert_mlp",
-           "hatq_cache4_bytes", "hatq_cache4_init", "hatq_cache4_append", "hatq_cache4_read",
+           "hatq_linear4_weights_bytes", "hatq_prepare_linear4", "hatq_pack_linear4", "hatq_linear4_ws_bytes",
+           "hatq_linear4_forward", "hatq_cache4_bytes", "hatq_cache4_init", "hatq_cache4_append", "hatq_cache4_read",
            "hatq_attention4_ws_bytes", "hatq_attention4"]
 
 _lib = None
@@ -176,6 +184,17 @@ def load(build_if_missing: bool = False):
     L.hatq_expert_mlp_ws_bytes.restype = sz
     L.hatq_expert_mlp.argtypes = [W, W, P, i32, i32, i64, P, P, i32, P, i32, i64, P, sz, P]
     L.hatq_expert_mlp.restype = i32
+    W4 = ctypes.POINTER(Linear4Weights)
+    L.hatq_linear4_weights_bytes.argtypes = [i32] * 5
+    L.hatq_linear4_weights_bytes.restype = sz
+    L.hatq_prepare_linear4.argtypes = [i32] * 5 + [P, i32, P, P, sz, W4, P]
+    L.hatq_prepare_linear4.restype = i32
+    L.hatq_pack_linear4.argtypes = [i32] * 5 + [P, P, P, P, sz, W4, P]
+    L.hatq_pack_linear4.restype = i32
+    L.hatq_linear4_ws_bytes.argtypes = [W4, i32]
+    L.hatq_linear4_ws_bytes.restype = sz
+    L.hatq_linear4_forward.argtypes = [W4, P, i32, i32, i64, P, i32, i64, P, sz, P]
+    L.hatq_linear4_forward.restype = i32
     C, H, f32 = ctypes.POINTER(Cache4View), ctypes.POINTER(Heads), ctypes.c_float
     L.hatq_cache4_bytes.argtypes = [i32] * 5
     L.hatq_cache4_bytes.restype = sz
@@ -838,7 +857,7 @@ def hatq_linear_ws_bytes(lin: PreparedLinear, rows: int) -> int:
     return int(load().hatq_linear_ws_bytes(lin.ref, rows))
 
 
-def _linear_ws(lin: PreparedLinear, rows: int, ws: Optional[torch.Tensor], x: torch.Tensor) -> torch.Tensor:
+def _linear_ws(lin, rows: int, ws: Optional[torch.Tensor], x: torch.Tensor) -> torch.Tensor:
     if ws is None:
         # hatq_linear_ws_bytes, without the call
         return x.new_empty(((rows * lin.k_stride + 255) & -256) + ((4 * rows + 255) & -256) or 256, dtype=torch.int8)
@@ -994,6 +1013,109 @@ def hatq_expert_mlp(w_in: PreparedLinear, w_out: PreparedLinear, x: torch.Tensor
     _check(load().hatq_expert_mlp(w_in.ref, w_out.ref, x.data_ptr(), xt, n, xs, ids.data_ptr(), weights.data_ptr(),
                                   topk, y.data_ptr(), yt, ys, ws.data_ptr(), ws.numel(), _stream()),
            "hatq_expert_mlp")
+    return y
+
+
+@dataclass
+class PreparedLinear4:
+    """Prepared 4-bit linear weights: the device buffer and the C view into it."""
+    buf: torch.Tensor
+    w: Linear4Weights
+    cin: int
+    cout: int
+    group: int
+    k_stride: int
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.w)
+        self.device = self.buf.get_device()
+
+
+def _linear4(call: str, w: torch.Tensor, gated: bool, hblock: int, group: int, run) -> PreparedLinear4:
+    held, cin = w.shape
+    cout = held // 2 if gated else held
+    _sizes("sizes", held, cin, hblock, group)
+    shape = cin, cout, int(gated), hblock, group
+    nbytes = int(load().hatq_linear4_weights_bytes(*shape))
+    buf = torch.empty(max(nbytes, 1), dtype=torch.int8, device=w.device)
+    out = Linear4Weights()
+    _check(run(shape, buf.data_ptr(), nbytes, ctypes.byref(out)), call)
+    return PreparedLinear4(buf, out, cin, cout, group, out.k_stride)
+
+
+def _held4(w: torch.Tensor, gated: bool, name: str) -> torch.Tensor:
+    if w.dim() != 2:
+        raise ValueError(f"{name}: [channels, cin] expected, got {tuple(w.shape)}")
+    if gated and w.shape[0] % 2:
+        raise ValueError(f"{name}: a gated layer holds its gates and as many values, got {w.shape[0]} channels")
+    return w.contiguous()
+
+
+def hatq_prepare_linear4(w: torch.Tensor, bias: Optional[torch.Tensor] = None, hblock: int = 1, group: int = 128,
+                         gated: bool = False, stream=None) -> PreparedLinear4:
+    """A layer of 4-bit weights from float weights [held, cin], a scale for each channel and
+    `group` input channels (64 or 128).  gated: held = 2 cout, gates first."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_prepare_linear4(w, bias, hblock, group, gated)
+    w = _held4(w, gated, "w")
+    t = _dtype(w.dtype, "w")
+    _need(w, "w", w.dtype, 0)
+    b = None if bias is None else bias.contiguous().float()
+    _need(b, "bias", torch.float32, w.shape[0], optional=True)
+    _here(w.get_device(), b)
+    return _linear4("hatq_prepare_linear4", w, gated, hblock, group,
+                    lambda shape, dst, n, out: load().hatq_prepare_linear4(*shape, _ptr(w), t, _ptr(b), dst, n, out,
+                                                                           _stream()))
+
+
+def hatq_pack_linear4(codes: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      hblock: int = 1, gated: bool = False, stream=None) -> PreparedLinear4:
+    """The same from int8 codes [held, cin] of the transformed weights, within [-8, 7], and
+    their bfloat16 scales [held, groups] (quantized elsewhere); the group is 64 or 128,
+    whichever gives as many groups (128 where both do)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_pack_linear4(codes, w_scale, bias, hblock, gated)
+    codes = _held4(codes, gated, "codes")
+    _need(codes, "codes", torch.int8, 0)
+    held, cin = codes.shape
+    groups = {-(-cin // g): g for g in (64, 128)}
+    if w_scale.dim() != 2 or w_scale.shape[0] != held or w_scale.shape[1] not in groups:
+        raise ValueError(f"w_scale: [{held}, {' or '.join(str(g) for g in groups)}] expected, got {tuple(w_scale.shape)}")
+    s = w_scale.contiguous()
+    b = None if bias is None else bias.contiguous()
+    _need(s, "w_scale", torch.bfloat16, 0)
+    _need(b, "bias", torch.float32, held, optional=True)
+    _here(codes.get_device(), s, b)
+    return _linear4("hatq_pack_linear4", codes, gated, hblock, groups[w_scale.shape[1]],
+                    lambda shape, dst, n, out: load().hatq_pack_linear4(*shape, _ptr(codes), _ptr(s), _ptr(b), dst, n,
+                                                                        out, _stream()))
+
+
+def hatq_linear4_ws_bytes(lin: PreparedLinear4, rows: int) -> int:
+    _sizes("rows", rows)
+    return int(load().hatq_linear4_ws_bytes(lin.ref, rows))
+
+
+def hatq_linear4_forward(lin: PreparedLinear4, x: torch.Tensor, out_dtype: Optional[torch.dtype] = None,
+                         y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+    """Tokens x [rows, cin] through a layer of 4-bit weights: y [rows, cout] of out_dtype
+    (default: x's)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hatq_linear4_forward(lin, x, out_dtype, y, ws)
+    n, _, xs, xt = _rows(x, "x", lin.cin)
+    y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
+    _here(lin.device, x, y, ws)
+    if n <= HATQ_TOKEN_ROWS and n * lin.k_stride <= HATQ_TOKEN_CODES:
+        wp, wn = None, 0                # a few tokens need no workspace
+    else:
+        ws = _linear_ws(lin, n, ws, x)
+        wp, wn = ws.data_ptr(), ws.numel()
+    _check(load().hatq_linear4_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, wp, wn, _stream()),
+           "hatq_linear4_forward")
     return y
 
 
