@@ -728,10 +728,10 @@ int32_t hatq_cache4_read(const hatq_cache4 *C, const hatq_heads *k, const hatq_h
  *   ws: device memory, 256-byte aligned, of at least hatq_attention4_ws_bytes bytes for
  *       the same sizes (ragged: ends is given); may be NULL where that is 0.  Calls that may
  *       overlap need workspaces of their own.
- * Scores, weights and sums are fp32.  Products: the transformed query in whole numbers of 16
- * bits of its largest magnitude against the codes, exact sums in each group; the weights
- * times the values' scales in fp16, relative to the largest.  If q or y is not bf16: 24
- * bits, and 22 bits of the weights.  No result depends on the order in which blocks run. */
+ * Scores, weights and sums are fp32.  Products: the transformed query in two fp16 halves
+ * against the codes; the weights times the values' scales in fp16, relative to the
+ * largest, or if q or y is not bf16 in two halves.  No result depends on the order in
+ * which blocks run. */
 size_t hatq_attention4_ws_bytes(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch,
                                 int32_t ragged, int32_t max_len);
 int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_heads *y, int32_t rows, int32_t q_heads,

@@ -8,13 +8,12 @@
 // product and the contraction of the second, and the 32 positions of a step are dealt to the
 // rows so that a lane's scores are the second product's operand as they are.
 //
-// First product: the query in whole numbers of ND bytes (16 or 24 bits of its largest
-// value), INT8 matrix instructions on the bytes against the codes; sums are exact, the
-// query's rounding is half a step, 2^-16 or 2^-24 of its largest value.
+// First product: the codes in float16, exact, against the query in two float16 halves, 22
+// bits, after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
 // kept relative to the largest of w s_v (not of w), so the float16 range holds whatever the
-// scales are (2^-100 to 2^100): off by 2^-11 of each weight or 2^-25 of the largest.  For float16 and float32 results
-// NP = 2 halves carry 22 bits of it.
+// scales are (2^-100 to 2^100): off by 2^-11 of each weight or 2^-25 of the largest.  For
+// float16 and float32 results NP = 2 halves carry 22 bits of it.
 #include "cache4_device.h"
 
 #ifndef HATQ_ATTENTION_PART
@@ -32,16 +31,11 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896341f;
 
-// Over the four chunks of a column (lanes 16 apart).
+__device__ __forceinline__ int wave_of_block() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// Over the four chunks of a column (lanes 16 apart).  Maxima keep NaN, here and below: one
+// instruction for three values, and where a score is NaN the column's results are.
 __device__ __forceinline__ float chunks_max(float v) {
-    const uint32_t u = __float_as_uint(v);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    const uint32_t w = __float_as_uint(v);
-    const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float chunks_maximum(float v) {   // NaN kept
     const uint32_t u = __float_as_uint(v);
     const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
     v = __builtin_elementwise_maximum(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -98,16 +92,42 @@ __device__ __forceinline__ ColTile col_tile(const AttentionArgs &a, int64_t t) {
 }
 
 // ---- sixteen columns of queries -----------------------------------------------------
-template <int NB, int ND>
 struct Query {
-    v4i digit[ND][NB];      // most significant first
-    float step;             // of the whole numbers, with the scores' factor
+    float step;             // of the products, with the scores' factor and log2 e
     int pos, from;          // last and first position seen
 };
 
-template <int NB, int ND>
+// Eight codes in each half byte of a word to float16: 1024 + code + 8 or 1024 + 16 (code + 8),
+// less what is too much.  XOR: their code is two's complement, not code + 8.  The pairs come
+// as half bytes (0, 4), (1, 5), (2, 6), (3, 7).
+template <bool XOR>
+__device__ __forceinline__ void unpack8(uint32_t x, v2h (&out)[4]) {
+    const uint32_t low = XOR ? 0x64086408u : 0x64006400u, high = XOR ? 0x64806480u : 0x64006400u;
+    const v2h sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f}, c72 = {(_Float16)-72.0f, (_Float16)-72.0f},
+              c1032 = {(_Float16)1032.0f, (_Float16)1032.0f};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const uint32_t w = k ? x >> 8 : x;
+        // (and, then exclusive or, in one instruction)
+        out[2 * k] = __builtin_bit_cast(v2h, __builtin_amdgcn_bitop3_b32(w, 0x000f000fu, low, 0x6a)) - c1032;
+        out[2 * k + 1] = __builtin_elementwise_fma(
+            __builtin_bit_cast(v2h, __builtin_amdgcn_bitop3_b32(w, 0x00f000f0u, high, 0x6a)), sixteenth, c72);
+    }
+}
+__device__ __forceinline__ v8h join8(const v2h (&p)[4]) {
+    return v8h{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+}
+// Which of eight adjacent channels the i-th value of a key's unpacked word is: its half bytes
+// hold channels 0, 4, 1, 5, 2, 6, 3, 7.
+__device__ __forceinline__ constexpr int key_channel(int i) { return (i >> 1) % 2 * 4 + (i >> 2) + (i & 1) * 2; }
+
+// The operand of 16 columns, [NB][2 steps of 32 channels][2 halves][64 lanes] in LDS.
+template <int NB>
+constexpr int kQueryBytes = NB * 4096;
+
+template <int NB>
 __device__ __forceinline__ void load_query(const AttentionArgs &a, const ColTile &t, int head, int length, int col,
-                                           Query<NB, ND> &q) {
+                                           Query &q, v8h *lds) {
     const int lane = threadIdx.x & 63, chunk = lane >> 4;
     const int c = min(t.col0 + col + (lane & 15), t.count * a.share - 1);
     const int i = c / a.share, g = c - i * a.share;
@@ -121,30 +141,24 @@ __device__ __forceinline__ void load_query(const AttentionArgs &a, const ColTile
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < 16; ++j) m = __builtin_elementwise_maximum(m, fabsf(v[b][j]));
-    m = chunks_maximum(m);
-    // whole numbers of at most 127 2^(8 (ND - 1)): their lower bytes, signed, carry no further
-    constexpr float kMost = ND == 2 ? 32512.0f : 8323072.0f;
-    const float up = m > 0x1p-100f ? kMost / m : 0.0f;      // (below, its scores are taken as 0)
+    m = chunks_max(m);
+    const int up = 14 - __builtin_amdgcn_frexp_expf(m);
     const float factor = a.scale * kLog2e * __uint_as_float((uint32_t)(127 - a.c.log_b) << 23);
-    // the codes come 16 times too large; a query that is not finite has scores NaN
-    q.step = m < __builtin_inff() ? m * (1.0f / (kMost * 16.0f)) * factor : __builtin_nanf("");
+    // (a query that is not finite has scores NaN)
+    q.step = m < __builtin_inff() ? __builtin_amdgcn_ldexpf(factor, -up) : __builtin_nanf("");
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            uint32_t d[ND][4];
+        for (int w = 0; w < 2; ++w) {
+            v8h half[2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                int n = (int)rintf(v[b][4 * w + j] * up);
-#pragma unroll
-                for (int k = ND - 1; k > 0; --k) {
-                    d[k][j] = (uint32_t)n;
-                    n = (n + 128) >> 8;
-                }
-                d[0][j] = (uint32_t)n;
+            for (int j = 0; j < 8; ++j) {
+                const float x = __builtin_amdgcn_ldexpf(v[b][8 * w + key_channel(j)], up);
+                half[0][j] = (_Float16)x;
+                half[1][j] = (_Float16)(x - (float)half[0][j]);
             }
 #pragma unroll
-            for (int k = 0; k < ND; ++k) q.digit[k][b][w] = (int)pack_low_bytes(d[k][0], d[k][1], d[k][2], d[k][3]);
+            for (int k = 0; k < 2; ++k) lds[((b * 2 + w) * 2 + k) * 64 + lane] = half[k];
         }
     q.pos = a.causal ? length - t.count + i : length - 1;
     q.from = a.window ? max(q.pos - a.window + 1, 0) : 0;
@@ -157,123 +171,163 @@ struct Sums {
     float m, l;         // the largest log2 of a weight so far; this lane's sum of weights
 };
 
-// One step's operands as they lie in memory.
+// One step's operands as they lie in memory.  Each part is loaded again, for the step after,
+// as soon as it has been used, so a step's loads are under way over the rest of the step
+// before and no second set of registers is kept.
 template <int NB>
 struct Step {
-    v4u key[NB], value[NB], key_scale[NB], value_scale[NB];
+    v4u key[NB], key_scale[NB], value_scale[NB], value[NB];
+};
+
+// A step's pages: of its two halves where pages have 16 positions, else one.
+struct Pages {
+    int a, b;
+};
+template <bool HALF>
+__device__ __forceinline__ Pages pages_of(const Cache4 &c, const Places4 &at, const int32_t *table, int p0) {
+    const int slot = p0 >> c.log_page, slot2 = (p0 + 16) >> c.log_page;
+    const int a = slot < at.width ? table[slot] : -1;
+    return {a, !HALF ? a : slot2 < at.width ? table[slot2] : -1};
+}
+
+// Where the parts of a step are: this lane's octets of the keys and the values, at `base` or,
+// where pages have 16 positions, `half` on for the lanes of the second half.
+struct StepAt {
+    const uint8_t *base;
+    int64_t half;
     bool lacks;         // a page is not there
     bool there;         // the page of this lane's eight scores is
 };
 
-template <int NB>
-__device__ __forceinline__ void load_step(const Cache4 &c, const Places4 &at, int seq, int head, int p0, Step<NB> &s) {
-    // (the step's positions start at a multiple of 32: a page holds a half of it at least)
-    const int lane = threadIdx.x & 63;
-    const int slot = p0 >> c.log_page, slot2 = (p0 + 16) >> c.log_page;
-    const int32_t *table = at.table + (int64_t)seq * at.width;
-    int pa = table[min(slot, at.width - 1)], pb = table[min(slot2, at.width - 1)];
-    const bool in_a = slot < at.width && (unsigned)pa < (unsigned)c.pages;
-    const bool in_b = slot2 < at.width && (unsigned)pb < (unsigned)c.pages;
-    s.lacks = !(in_a && in_b);
+// The parts of a lane's addresses that are the same for every step.
+struct LaneAt {
+    uint32_t key, value, run;
+    bool key_half, value_half;      // in the second page of a step
+};
+template <int NB, bool HALF>
+__device__ __forceinline__ LaneAt lane_at() {
+    const uint32_t lane = threadIdx.x & 63, octet_k = (lane & 15) >> 2, octet_v = lane >> 4;
+    const uint32_t mask = HALF ? 1 : 3;
+    const uint32_t v = (octet_v & mask) * (NB * kOctet);
+    return {(octet_k & mask) * (NB * kOctet) + (lane >> 4) * 64 + (lane & 3) * 16, v + NB * 512, v + NB * kKeyCodes + (lane & 15) * 16,
+            octet_k >= 2, octet_v >= 2};
+}
+
+template <int NB, bool HALF>
+__device__ __forceinline__ StepAt step_at(const Cache4 &c, int64_t head0, const LaneAt &lane, const Pages &p, int p0) {
+    const bool in_a = (unsigned)p.a < (unsigned)c.pages, in_b = (unsigned)p.b < (unsigned)c.pages;
+    const int64_t page = (int64_t)c.heads * ((int64_t)(NB * kOctet) << (c.log_page - 3));
     const int mask = (1 << c.log_page) - 1;
-    const int64_t oa = page_offset<NB>(c, in_a ? pa : 0, head), ob = page_offset<NB>(c, in_b ? pb : 0, head);
-    const int octet_k = (lane & 15) >> 2, octet_v = lane >> 4;      // of the step's four
-    s.there = octet_v < 2 ? in_a : in_b;
-    const uint8_t *k = c.buf + (octet_k < 2 ? oa : ob) + (((p0 + 8 * octet_k) & mask) >> 3) * (NB * kOctet) +
-                       (lane >> 4) * 64 + (lane & 3) * 16;
-    const uint8_t *v = c.buf + (octet_v < 2 ? oa : ob) + (((p0 + 8 * octet_v) & mask) >> 3) * (NB * kOctet);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) s.key[b] = *reinterpret_cast<const v4u *>(k + b * kKeyCodes);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        s.key_scale[b] = *reinterpret_cast<const v4u *>(v + NB * 512 + b * 16);
-        s.value_scale[b] = *reinterpret_cast<const v4u *>(v + NB * 512 + (NB + b) * 16);
+    const uint8_t *base = c.buf + head0 + ((p0 & mask) >> 3) * (NB * kOctet) + (in_a ? p.a : 0) * page;
+    if constexpr (HALF) {
+        return {base, ((int64_t)(in_b ? p.b : 0) - (in_a ? p.a : 0)) * page, !(in_a && in_b), lane.value_half ? in_b : in_a};
+    } else {
+        return {base, 0, !in_a, in_a};
     }
+}
+template <bool HALF>
+__device__ __forceinline__ v4u load_part(const StepAt &at, uint32_t offset, bool second) {
+    const uint8_t *base = at.base;
+    if constexpr (HALF) base += second ? at.half : 0;
+    return *reinterpret_cast<const v4u *>(base + offset);
+}
+template <int NB, bool HALF>
+__device__ __forceinline__ void load_keys(const StepAt &at, const LaneAt &lane, int b, Step<NB> &s) {
+    s.key[b] = load_part<HALF>(at, lane.key + b * kKeyCodes, lane.key_half);
+}
+template <int NB, bool HALF>
+__device__ __forceinline__ void load_scales(const StepAt &at, const LaneAt &lane, int which, v4u (&to)[NB]) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-        s.value[b] = *reinterpret_cast<const v4u *>(v + NB * kKeyCodes + b * 256 + (lane & 15) * 16);
+    for (int b = 0; b < NB; ++b) to[b] = load_part<HALF>(at, lane.value + (which * NB + b) * 16, lane.value_half);
+}
+template <int NB, bool HALF>
+__device__ __forceinline__ void load_values(const StepAt &at, const LaneAt &lane, int b, Step<NB> &s) {
+    s.value[b] = load_part<HALF>(at, lane.run + b * 256, lane.value_half);
 }
 
 __device__ __forceinline__ float scale_of(const v4u &w, int j) {
     return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
 }
 
-// One step of 32 positions from p0 on by NQ times sixteen columns.  EDGE: some of them may be
-// hidden from some columns.
-template <int NB, int ND, int NP, int NQ, bool EDGE>
-__device__ __forceinline__ void step(const Step<NB> &s, const Query<NB, ND> (&q)[NQ], int p0, Sums<NB> (&sum)[NQ]) {
+// One step of 32 positions from p0 on by NQ times sixteen columns, and the next one's loads.
+// EDGE: some positions may be hidden from some columns.
+template <int NB, int NP, int NQ, bool EDGE, bool HALF>
+__device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const StepAt &next, const LaneAt &mine, const Query (&q)[NQ],
+                                     const v8h *query, int p0, Sums<NB> (&sum)[NQ]) {
     const int lane = threadIdx.x & 63;
     const int first = p0 + 8 * (lane >> 4);
-    // scales of this lane's eight positions; log2 of the values' largest, to 0.09 from below
-    float lv[8];
+    float t[NQ][8];
+    uint32_t x_at = lane;
+    asm volatile("" : "+v"(x_at));      // read in every step: kept over the loop, the query's registers spill
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        float most = scale_of(s.value_scale[0], j);
+    for (int b = 0; b < NB; ++b) {
+        v4f acc[NQ][2];
 #pragma unroll
-        for (int b = 1; b < NB; ++b) most = fmaxf(most, scale_of(s.value_scale[b], j));
-        lv[j] = __builtin_fmaf((float)__float_as_int(most), 0x1p-23f, -127.0f);
-    }
-    v4i key[2][NB];
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+            for (int h = 0; h < 2; ++h) acc[n][h] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                key[h][b][2 * w] = (int)((s.key[b][2 * h + w] << 4) & 0xf0f0f0f0u);
-                key[h][b][2 * w + 1] = (int)(s.key[b][2 * h + w] & 0xf0f0f0f0u);
-            }
-    v8h code[NB][4];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v2h pair[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                // 1024 + code + 8 as float16, less 1032
-                const uint32_t bits = ((s.value[b][i] >> (4 * j)) & 0x000f000fu) | 0x64006400u;
-                pair[i] = __builtin_bit_cast(v2h, bits) - v2h{(_Float16)1032.0f, (_Float16)1032.0f};
-            }
-            code[b][j] = v8h{pair[0][0], pair[0][1], pair[1][0], pair[1][1], pair[2][0], pair[2][1], pair[3][0], pair[3][1]};
-        }
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        float t[8];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int w = 0; w < 2; ++w) {
+            v8h key[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                v4i acc[ND];
-#pragma unroll
-                for (int k = 0; k < ND; ++k)
-                    acc[k] = __builtin_amdgcn_mfma_i32_16x16x64_i8(key[h][b], q[n].digit[k][b], v4i{0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    // |sum of one byte's products| < 2^20: two bytes' fit 31 bits
-                    float f = (float)(acc[ND - 2][r] * 256 + acc[ND - 1][r]);
-                    if (ND == 3) f = __builtin_fmaf((float)acc[0][r], 65536.0f, f);
-                    const float w = scale_of(s.key_scale[b], 4 * h + r);
-                    t[4 * h + r] = b == 0 ? f * w : __builtin_fmaf(f, w, t[4 * h + r]);
-                }
+                v2h pair[4];
+                unpack8<true>(s.key[b][2 * h + w], pair);
+                key[h] = join8(pair);
             }
-        float most = kLowest;
-        bool seen[8];
+            if (w) load_keys<NB, HALF>(next, mine, b, s);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const v8h x = query[n * (NB * 256) + ((b * 2 + w) * 2 + k) * 64 + x_at];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) acc[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[h], x, acc[n][h], 0, 0, 0);
+                }
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float f = acc[n][j >> 2][j & 3], w = scale_of(s.key_scale[b], j);
+                t[n][j] = b == 0 ? f * w : __builtin_fmaf(f, w, t[n][j]);
+            }
+    }
+    load_scales<NB, HALF>(next, mine, 0, s.key_scale);
+    // 128 (127 + log2) of the largest scale of a value, to 12 from below: its bf16 bits
+    float lv[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        typedef uint16_t v2s __attribute__((ext_vector_type(2)));
+        // (a word by itself: a cast of a vector's element takes the first one's)
+        const auto pair = [&](int b) {
+            const uint32_t w = s.value_scale[b][i];
+            return __builtin_bit_cast(v2s, w);
+        };
+        v2s most = pair(0);
+#pragma unroll
+        for (int b = 1; b < NB; ++b) most = __builtin_elementwise_max(most, pair(b));
+        lv[2 * i] = (float)most[0];
+        lv[2 * i + 1] = (float)most[1];
+    }
+    uint32_t seen[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        Sums<NB> &o = sum[n];
+        float most = -__builtin_inff();
+        if (EDGE) {
+            // positions first + j that the column sees, as bits
+            const int lo = min(max(q[n].from - first, 0), 8), hi = min(max(q[n].pos + 1 - first, 0), 8);
+            seen[n] = here.there ? ((1u << hi) - 1) & ~((1u << lo) - 1) : 0u;
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            t[j] *= q[n].step;
-            if (EDGE) {
-                seen[j] = s.there && first + j <= q[n].pos && first + j >= q[n].from;
-                t[j] = seen[j] ? t[j] : -__builtin_inff();
-                most = fmaxf(most, seen[j] ? t[j] + lv[j] : kLowest);
-            } else {
-                most = fmaxf(most, t[j] + lv[j]);
-            }
+            const float x = __builtin_fmaf(t[n][j], q[n].step * 128.0f, lv[j]);
+            most = __builtin_elementwise_maximum(most, !EDGE || (seen[n] >> j & 1) ? x : -__builtin_inff());
         }
-        most = chunks_max(most);
-        Sums<NB> &o = sum[n];
+        most = __builtin_fmaf(chunks_max(most), 0x1p-7f, -127.0f);
         if (__any(most > o.m)) {
-            const float m = fmaxf(o.m, most), down = __builtin_amdgcn_exp2f(o.m - m);
+            const float m = most > o.m ? most : o.m, down = __builtin_amdgcn_exp2f(o.m - m);
             o.m = m;
             o.l *= down;
 #pragma unroll
@@ -283,45 +337,80 @@ __device__ __forceinline__ void step(const Step<NB> &s, const Query<NB, ND> (&q)
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            t[j] = __builtin_amdgcn_exp2f(t[j] - o.m);
-            o.l += t[j];
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t[n][j], q[n].step, -o.m));
+            t[n][j] = !EDGE || (seen[n] >> j & 1) ? p : 0.0f;
+            o.l += t[n][j];
         }
+    }
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            v8h high, low;
+    for (int b = 0; b < NB; ++b) {
+        v8h weight[NQ][NP];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                float w = t[j] * scale_of(s.value_scale[b], j);
-                if (EDGE) w = seen[j] ? w : 0.0f;      // (a hidden position's scale may be anything)
+                float w = t[n][j] * scale_of(s.value_scale[b], j);
+                if (EDGE) w = seen[n] >> j & 1 ? w : 0.0f;      // (a hidden position's scale may be anything)
                 // (one rounded product for both halves: else one of them is made by v_fma_mixlo, which
                 // rounds the exact product, and a tie goes up in one and down in the other)
                 if (NP == 2) asm("" : "+v"(w));
-                high[j] = (_Float16)w;
-                if (NP == 2) low[j] = (_Float16)(w - (float)high[j]);
+                weight[n][0][j] = (_Float16)w;
+                if (NP == 2) weight[n][NP - 1][j] = (_Float16)(w - (float)weight[n][0][j]);
             }
+        v2h code[4][4];     // [word: positions][channel of the run]
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                o.o[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(code[b][j], high, o.o[b][j], 0, 0, 0);
-                if (NP == 2) o.o[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(code[b][j], low, o.o[b][j], 0, 0, 0);
-            }
+        for (int i = 0; i < 4; ++i) unpack8<false>(s.value[b][i], code[i]);
+        load_values<NB, HALF>(next, mine, b, s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const v2h word[4] = {code[0][j], code[1][j], code[2][j], code[3][j]};
+            const v8h x = join8(word);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int k = 0; k < NP; ++k)
+                    sum[n].o[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, weight[n][k], sum[n].o[b][j], 0, 0, 0);
         }
     }
+    load_scales<NB, HALF>(next, mine, 1, s.value_scale);
 }
 
-// Positions [from, to) that some column of a wave sees, `from` a multiple of 32.
-template <int NB, int ND, int NP, int NQ>
-__device__ __forceinline__ void walk(const AttentionArgs &a, int seq, int head, const Query<NB, ND> (&q)[NQ], int from,
+// Every stride-th step of the positions [from, to) that some column of a wave sees, `from` a
+// multiple of 32; every column sees all of [sure_from, sure_to).
+template <int NB, int NP, int NQ, bool HALF>
+__device__ __forceinline__ void walk(const AttentionArgs &a, int seq, int head, const Query (&q)[NQ], const v8h *query, int from,
                                      int to, int stride, int sure_from, int sure_to, Sums<NB> (&sum)[NQ]) {
     if (from >= to) return;
-    Step<NB> s[2];
-    load_step<NB>(a.c, a.at, seq, head, from, s[0]);
-    for (int p = from; p < to; p += stride) {
-        const int next = p + stride < to ? p + stride : p;
-        load_step<NB>(a.c, a.at, seq, head, next, s[1]);
-        // every column sees positions [sure_from, sure_to)
-        if (p >= sure_from && p + 32 <= sure_to && !s[0].lacks) step<NB, ND, NP, NQ, false>(s[0], q, p, sum);
-        else step<NB, ND, NP, NQ, true>(s[0], q, p, sum);
-        s[0] = s[1];
+    const int32_t *table = a.at.table + (int64_t)seq * a.at.width;
+    const int64_t head0 = page_offset<NB>(a.c, 0, head);
+    const LaneAt mine = lane_at<NB, HALF>();
+    Step<NB> s;
+    StepAt here = step_at<NB, HALF>(a.c, head0, mine, pages_of<HALF>(a.c, a.at, table, from), from);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) load_keys<NB, HALF>(here, mine, b, s);
+    load_scales<NB, HALF>(here, mine, 0, s.key_scale);
+    load_scales<NB, HALF>(here, mine, 1, s.value_scale);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) load_values<NB, HALF>(here, mine, b, s);
+    // (the step after a wave's last one: the same again, not used)
+    const auto after = [&](int p) { return p + stride < to ? p + stride : p; };
+    Pages pages = pages_of<HALF>(a.c, a.at, table, after(from));
+    const auto sure = [&](int p) { return p >= sure_from && p + 32 <= sure_to && !here.lacks; };
+    // (a loop each: as the branches of one, the compiler makes both kinds' common parts first and
+    // keeps all of them)
+    for (int p = from; p < to;) {
+        for (; p < to && sure(p); p += stride) {
+            const StepAt next = step_at<NB, HALF>(a.c, head0, mine, pages, after(p));
+            pages = pages_of<HALF>(a.c, a.at, table, after(after(p)));
+            step<NB, NP, NQ, false, HALF>(s, here, next, mine, q, query, p, sum);
+            here = next;
+        }
+        for (; p < to && !sure(p); p += stride) {
+            const StepAt next = step_at<NB, HALF>(a.c, head0, mine, pages, after(p));
+            pages = pages_of<HALF>(a.c, a.at, table, after(after(p)));
+            step<NB, NP, NQ, true, HALF>(s, here, next, mine, q, query, p, sum);
+            here = next;
+        }
     }
 }
 
@@ -401,18 +490,19 @@ __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, cha
 
 // Sixteen columns a block, its waves each every W-th step of the block's share of the
 // positions.
-template <int NB, int ND, int NP>
-__global__ void __launch_bounds__(512) attention4_kernel(const AttentionArgs a) {
+template <int NB, int NP, bool HALF>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NB <= 2 ? 4 : 2))) attention4_kernel(const AttentionArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int waves = blockDim.x >> 6, wave = wave_of_block(), lane = threadIdx.x & 63;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int split = (int)(block % a.splits), head = (int)(block / a.splits % a.c.heads);
     const int64_t tile = block / a.splits / a.c.heads;
     const ColTile t = col_tile<16>(a, tile);
     if (t.seq < 0) return;
     const int length = length_of(a, t.seq);
-    Query<NB, ND> q[1];
-    load_query<NB, ND>(a, t, head, length, 0, q[0]);
+    Query q[1];
+    v8h *query = reinterpret_cast<v8h *>(lds);      // (every wave makes it, and of the same values)
+    load_query<NB>(a, t, head, length, 0, q[0], query);
     // rows of the first and last column
     const int i0 = t.col0 / a.share, i1 = (min(t.col0 + 16, t.count * a.share) - 1) / a.share;
     int from = 0, to = length, sure_from = 0, sure_to = length;
@@ -434,7 +524,8 @@ __global__ void __launch_bounds__(512) attention4_kernel(const AttentionArgs a) 
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[0].o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     const int last = end == steps ? to : from + 32 * end;
-    walk<NB, ND, NP, 1>(a, t.seq, head, q, from + 32 * (begin + wave), last, 32 * waves, sure_from, sure_to, s);
+    walk<NB, NP, 1, HALF>(a, t.seq, head, q, query, from + 32 * (begin + wave), last, 32 * waves, sure_from, sure_to, s);
+    __syncthreads();    // the query has been read
     join_waves<NB>(s[0], wave, waves, lds);
     if (wave) return;
     if (a.splits == 1) {
@@ -457,7 +548,7 @@ __global__ void __launch_bounds__(512) attention4_kernel(const AttentionArgs a) 
 template <int NB>
 __global__ void __launch_bounds__(512) attention4_join_kernel(const AttentionArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int waves = blockDim.x >> 6, wave = wave_of_block(), lane = threadIdx.x & 63;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int head = (int)(block % a.c.heads);
     const int64_t tile = block / a.c.heads;
@@ -491,10 +582,11 @@ __global__ void __launch_bounds__(512) attention4_join_kernel(const AttentionArg
 
 // Many query rows: each wave 16 NQ columns of its own over all their positions; the waves of
 // a block have adjacent columns and meet the same pages in its caches.
-template <int NB, int ND, int NP, int NQ>
+template <int NB, int NP, int NQ, bool HALF>
 __global__ void __launch_bounds__(64 * kWideWaves) attention4_wide_kernel(const AttentionArgs a) {
     constexpr int COLS = 16 * NQ, WAVES = kWideWaves;
-    const int wave = threadIdx.x >> 6;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int wave = wave_of_block();
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int head = (int)(block % a.c.heads);
     ColTile t = col_tile<COLS * WAVES>(a, block / a.c.heads);
@@ -503,11 +595,12 @@ __global__ void __launch_bounds__(64 * kWideWaves) attention4_wide_kernel(const 
     const int cols = t.count * a.share;
     if (t.col0 >= cols) return;
     const int length = length_of(a, t.seq);
-    Query<NB, ND> q[NQ];
+    Query q[NQ];
+    v8h *query = reinterpret_cast<v8h *>(lds) + wave * (NQ * NB * 256);
     Sums<NB> s[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        load_query<NB, ND>(a, t, head, length, 16 * n, q[n]);
+        load_query<NB>(a, t, head, length, 16 * n, q[n], query + n * (NB * 256));
         s[n].m = kLowest;
         s[n].l = 0.0f;
 #pragma unroll
@@ -525,7 +618,7 @@ __global__ void __launch_bounds__(64 * kWideWaves) attention4_wide_kernel(const 
             sure_from = length - t.count + i1 - a.window + 1;
         }
     }
-    walk<NB, ND, NP, NQ>(a, t.seq, head, q, from, to, 32, sure_from, sure_to, s);
+    walk<NB, NP, NQ, HALF>(a, t.seq, head, q, query, from, to, 32, sure_from, sure_to, s);
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
         if (t.col0 + 16 * n < cols) store_columns<NB>(a, t, head, 16 * n, s[n].o, chunks_sum(s[n].l));
@@ -536,18 +629,19 @@ dim3 blocks_of(int64_t n) {
     return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
 }
 
-template <int NB, int ND, int NP>
+template <int NB, int NP, bool HALF>
 hipError_t launch(const AttentionArgs &a, const AttentionPlan &p, hipStream_t st) {
     if (p.wide) {
         constexpr int NQ = wide_cols(64 * NB) / 16;
-        attention4_wide_kernel<NB, ND, NP, NQ><<<blocks_of(p.tiles * a.c.heads), 64 * kWideWaves, 0, st>>>(a);
+        const size_t lds = (size_t)kWideWaves * NQ * kQueryBytes<NB>;
+        attention4_wide_kernel<NB, NP, NQ, HALF><<<blocks_of(p.tiles * a.c.heads), 64 * kWideWaves, lds, st>>>(a);
         return hipGetLastError();
     }
-    const size_t lds = (size_t)p.waves * (NB * 2048 + 128);
-    attention4_kernel<NB, ND, NP><<<blocks_of(p.tiles * a.c.heads * p.splits), p.waves * 64, lds, st>>>(a);
+    const size_t join = (size_t)p.waves * (NB * 2048 + 128), lds = join > kQueryBytes<NB> ? join : kQueryBytes<NB>;
+    attention4_kernel<NB, NP, HALF><<<blocks_of(p.tiles * a.c.heads * p.splits), p.waves * 64, lds, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
-    attention4_join_kernel<NB><<<blocks_of(p.tiles * a.c.heads), p.waves * 64, lds, st>>>(a);
+    attention4_join_kernel<NB><<<blocks_of(p.tiles * a.c.heads), p.waves * 64, join, st>>>(a);
     return hipGetLastError();
 }
 
@@ -558,7 +652,9 @@ hipError_t launch(const AttentionArgs &a, const AttentionPlan &p, hipStream_t st
 #define HATQ_LAUNCH(n) HATQ_LAUNCH2(n)
 hipError_t HATQ_LAUNCH(HATQ_ATTENTION_PART)(const AttentionArgs &a, const AttentionPlan &p, hipStream_t st) {
     constexpr int NB = HATQ_ATTENTION_PART;
-    return a.q.type == kBf16 && a.y.type == kBf16 ? launch<NB, 2, 1>(a, p, st) : launch<NB, 3, 2>(a, p, st);
+    const bool half = a.c.log_page == 4;
+    if (a.q.type == kBf16 && a.y.type == kBf16) return half ? launch<NB, 1, true>(a, p, st) : launch<NB, 1, false>(a, p, st);
+    return half ? launch<NB, 2, true>(a, p, st) : launch<NB, 2, false>(a, p, st);
 }
 
 }  // namespace hatq

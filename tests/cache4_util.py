@@ -89,9 +89,9 @@ def attention64(q, k, v, v_scale, hblock, scale, causal, window, fine, there=Non
     keys and values in the transformed basis [len, heads, dim] float64; v_scale [len, heads]:
     the largest of a value's scales; there [len]: positions whose page is.
 
-    The bound (u = 2^-24): a score's error is half a step of the query's whole numbers (of 16
-    or 24 bits) against the keys, and roundings of float32 products and sums, 16 of them at
-    most on the way, 16 u sum |q k|; one of e moves each normalized weight by at most a
+    The bound (u = 2^-24): the query in two float16 halves is off by 2^-22 = 4 u of itself; a
+    product is exact, and a score's sum in float32 (64 products, two scales of up to four
+    groups, the factor) has at most 80 roundings, u sum |q k| each; an error of e moves each normalized weight by at most a
     factor exp(2 e).  A weight times scale in float16 is off by 2^-11 of itself (two halves
     2^-21), or where subnormal by 2^-25 of a unit that is at most 2 of the largest weight times
     scale (a value's codes may be 0, so the scale and not the value counts); the exponential and the products add 8 u.  Float32 sums of len terms add len u each of the
@@ -102,7 +102,6 @@ def attention64(q, k, v, v_scale, hblock, scale, causal, window, fine, there=Non
     qt = butterfly(q.astype(np.float64), hblock)
     y, bound = np.zeros(q.shape), np.zeros(q.shape)
     factor = scale / hblock
-    most = 8323072.0 if fine else 32512.0
     for i in range(n):
         p = length - n + i
         lo, hi = 0, length
@@ -121,8 +120,7 @@ def attention64(q, k, v, v_scale, hblock, scale, causal, window, fine, there=Non
             e = np.exp(t - t.max())
             w = e / e.sum()
             mag = butterfly_abs(w @ np.abs(vv), hblock)
-            size = np.abs(kk).sum(1).max() * np.abs(qt[i, h]).max() * abs(factor)
-            et = 0.5 / most * 1.01 * size + 16 * U * (np.abs(kk) @ np.abs(qt[i, h])).max() * abs(factor)
+            et = 84 * U * (np.abs(kk) @ np.abs(qt[i, h])).max() * abs(factor)
             rel = np.expm1(2 * et) + (2.0 ** -21 if fine else 2.0 ** -11) + (3 * keep.size + 24) * U
             y[i, h] = butterfly(w @ vv, hblock) / hblock
             low = 2.0 ** -24 * np.max(w * v_scale[keep, h // share]) * 1.01 * 7 * keep.size
