@@ -488,23 +488,36 @@ __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, cha
     }
 }
 
-// Sixteen columns a block, its waves each every W-th step of the block's share of the
-// positions.
-template <int NB, int NP, bool HALF>
-__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NB <= 2 ? 4 : 2))) attention4_kernel(const AttentionArgs a) {
+// 16 NQ columns a block, its waves each every W-th step of the block's share of the
+// positions.  NQ > 1 where there are many columns: a step's codes are unpacked once for all of
+// them.  (Its waves share the positions there too, not the columns: blocks then last a
+// fourth as long, and the last ones of a full card leave less of it idle.)
+template <int NB, int NP, int NQ, bool HALF>
+__global__ void __launch_bounds__(NQ > 1 ? 256 : 512) __attribute__((amdgpu_waves_per_eu(NB <= 2 && NQ == 1 ? 4 : 2)))
+attention4_kernel(const AttentionArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int waves = blockDim.x >> 6, wave = wave_of_block(), lane = threadIdx.x & 63;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int split = (int)(block % a.splits), head = (int)(block / a.splits % a.c.heads);
     const int64_t tile = block / a.splits / a.c.heads;
-    const ColTile t = col_tile<16>(a, tile);
+    const ColTile t = col_tile<16 * NQ>(a, tile);
     if (t.seq < 0) return;
-    const int length = length_of(a, t.seq);
-    Query q[1];
+    const int length = length_of(a, t.seq), cols = t.count * a.share;
+    Query q[NQ];
+    Sums<NB> s[NQ];
     v8h *query = reinterpret_cast<v8h *>(lds);      // (every wave makes it, and of the same values)
-    load_query<NB>(a, t, head, length, 0, q[0], query);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        load_query<NB>(a, t, head, length, 16 * n, q[n], query + n * (NB * 256));
+        s[n].m = kLowest;
+        s[n].l = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[n].o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
     // rows of the first and last column
-    const int i0 = t.col0 / a.share, i1 = (min(t.col0 + 16, t.count * a.share) - 1) / a.share;
+    const int i0 = t.col0 / a.share, i1 = (min(t.col0 + 16 * NQ, cols) - 1) / a.share;
     int from = 0, to = length, sure_from = 0, sure_to = length;
     if (a.causal) {
         to = min(length, length - t.count + i1 + 1);
@@ -516,22 +529,16 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(NB <= 
     }
     const int64_t steps = to > from ? (to - from + 31) >> 5 : 0;
     const int begin = (int)(steps * split / a.splits), end = (int)(steps * (split + 1) / a.splits);
-    Sums<NB> s[1];
-    s[0].m = kLowest;
-    s[0].l = 0.0f;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[0].o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     const int last = end == steps ? to : from + 32 * end;
-    walk<NB, NP, 1, HALF>(a, t.seq, head, q, query, from + 32 * (begin + wave), last, 32 * waves, sure_from, sure_to, s);
-    __syncthreads();    // the query has been read
-    join_waves<NB>(s[0], wave, waves, lds);
-    if (wave) return;
-    if (a.splits == 1) {
-        store_columns<NB>(a, t, head, 0, s[0].o, s[0].l);
-        return;
+    walk<NB, NP, NQ, HALF>(a, t.seq, head, q, query, from + 32 * (begin + wave), last, 32 * waves, sure_from, sure_to, s);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        __syncthreads();    // the LDS of before has been read
+        join_waves<NB>(s[n], wave, waves, lds);
+        if (wave == 0 && a.splits == 1 && t.col0 + 16 * n < cols) store_columns<NB>(a, t, head, 16 * n, s[n].o, s[n].l);
     }
+    if (wave || a.splits == 1) return;
+    // (NQ = 1)
     char *part = static_cast<char *>(a.ws) + ((tile * a.c.heads + head) * a.splits + split) * (int64_t)(NB * 4096 + 128);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -580,50 +587,6 @@ __global__ void __launch_bounds__(512) attention4_join_kernel(const AttentionArg
     if (wave == 0) store_columns<NB>(a, t, head, 0, s.o, s.l);
 }
 
-// Many query rows: each wave 16 NQ columns of its own over all their positions; the waves of
-// a block have adjacent columns and meet the same pages in its caches.
-template <int NB, int NP, int NQ, bool HALF>
-__global__ void __launch_bounds__(64 * kWideWaves) attention4_wide_kernel(const AttentionArgs a) {
-    constexpr int COLS = 16 * NQ, WAVES = kWideWaves;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int wave = wave_of_block();
-    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int head = (int)(block % a.c.heads);
-    ColTile t = col_tile<COLS * WAVES>(a, block / a.c.heads);
-    if (t.seq < 0) return;
-    t.col0 += wave * COLS;
-    const int cols = t.count * a.share;
-    if (t.col0 >= cols) return;
-    const int length = length_of(a, t.seq);
-    Query q[NQ];
-    v8h *query = reinterpret_cast<v8h *>(lds) + wave * (NQ * NB * 256);
-    Sums<NB> s[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        load_query<NB>(a, t, head, length, 16 * n, q[n], query + n * (NB * 256));
-        s[n].m = kLowest;
-        s[n].l = 0.0f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[n].o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    const int i0 = t.col0 / a.share, i1 = (min(t.col0 + COLS, cols) - 1) / a.share;
-    int from = 0, to = length, sure_from = 0, sure_to = length;
-    if (a.causal) {
-        to = min(length, length - t.count + i1 + 1);
-        sure_to = length - t.count + i0 + 1;
-        if (a.window) {
-            from = max(length - t.count + i0 - a.window + 1, 0) & ~31;
-            sure_from = length - t.count + i1 - a.window + 1;
-        }
-    }
-    walk<NB, NP, NQ, HALF>(a, t.seq, head, q, query, from, to, 32, sure_from, sure_to, s);
-#pragma unroll
-    for (int n = 0; n < NQ; ++n)
-        if (t.col0 + 16 * n < cols) store_columns<NB>(a, t, head, 16 * n, s[n].o, chunks_sum(s[n].l));
-}
-
 dim3 blocks_of(int64_t n) {
     const int64_t x = n < (1 << 20) ? n : 1 << 20;
     return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
@@ -631,14 +594,12 @@ dim3 blocks_of(int64_t n) {
 
 template <int NB, int NP, bool HALF>
 hipError_t launch(const AttentionArgs &a, const AttentionPlan &p, hipStream_t st) {
-    if (p.wide) {
-        constexpr int NQ = wide_cols(64 * NB) / 16;
-        const size_t lds = (size_t)kWideWaves * NQ * kQueryBytes<NB>;
-        attention4_wide_kernel<NB, NP, NQ, HALF><<<blocks_of(p.tiles * a.c.heads), 64 * kWideWaves, lds, st>>>(a);
-        return hipGetLastError();
-    }
-    const size_t join = (size_t)p.waves * (NB * 2048 + 128), lds = join > kQueryBytes<NB> ? join : kQueryBytes<NB>;
-    attention4_kernel<NB, NP, HALF><<<blocks_of(p.tiles * a.c.heads * p.splits), p.waves * 64, lds, st>>>(a);
+    constexpr int NQ = wide_cols(64 * NB) / 16;
+    const size_t join = (size_t)p.waves * (NB * 2048 + 128), query = (size_t)(p.cols / 16) * NB * 4096;
+    const size_t lds = join > query ? join : query;
+    const dim3 grid = blocks_of(p.tiles * a.c.heads * p.splits);
+    if (p.cols == 16) attention4_kernel<NB, NP, 1, HALF><<<grid, p.waves * 64, lds, st>>>(a);
+    else attention4_kernel<NB, NP, NQ, HALF><<<grid, p.waves * 64, lds, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     attention4_join_kernel<NB><<<blocks_of(p.tiles * a.c.heads), p.waves * 64, join, st>>>(a);

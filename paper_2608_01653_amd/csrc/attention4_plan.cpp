@@ -8,12 +8,12 @@ AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t
     const int64_t cols = (int64_t)rows * share;
     AttentionPlan p{};
     // a sequence's columns on average
-    p.wide = cols / batch >= 256;
-    const int64_t per = p.wide ? wide_cols(dim) * kWideWaves : 16;
-    p.tiles = ragged ? cols / per + (batch < rows ? batch : rows) : batch * ((cols / batch + per - 1) / per);
-    p.waves = dim <= 128 ? 8 : 4;
+    const bool many = cols / batch >= 128;
+    p.cols = many ? wide_cols(dim) : 16;
+    p.tiles = ragged ? cols / p.cols + (batch < rows ? batch : rows) : batch * ((cols / batch + p.cols - 1) / p.cols);
+    p.waves = dim <= 128 && !many ? 8 : 4;
     p.splits = 1;
-    if (p.wide) return p;
+    if (many) return p;
     // blocks that fill the card, of at least two steps of 32 positions a wave
     const int64_t steps = (max_len + 31) / 32, base = p.tiles * heads;
     int64_t splits = 512 / base;

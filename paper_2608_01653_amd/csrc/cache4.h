@@ -47,12 +47,11 @@ struct AttentionArgs {
 
 // How a call is laid out: host code without a launch, from sizes alone.
 struct AttentionPlan {
-    bool wide;          // wide_cols columns a wave, each wave its own; else 16 a block
-    int32_t waves, splits;
-    int64_t tiles;      // of columns of one cached head, over all sequences: an upper bound
+    int32_t cols;           // columns (a query row and head) of a cached head a block takes: 16 or wide_cols
+    int32_t waves, splits;  // splits: 1 where cols is more than 16
+    int64_t tiles;          // blocks of columns of one cached head, over all sequences: an upper bound
 };
-constexpr int kWideWaves = 4;
-constexpr int wide_cols(int dim) { return dim <= 64 ? 64 : 32; }
+constexpr int wide_cols(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 32 : 16; }
 AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t share, int32_t dim, int64_t max_len,
                              bool ragged);
 // Bytes of one partial result: 16 query rows of a head, their maxima and sums.
