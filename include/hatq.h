@@ -733,7 +733,7 @@ int32_t hatq_cache4_read(const hatq_cache4 *C, const hatq_heads *k, const hatq_h
  * largest, or if q or y is not bf16 in two halves.  No result depends on the order in
  * which blocks run. */
 size_t hatq_attention4_ws_bytes(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch,
-                                int32_t ragged, int32_t max_len);
+                                int32_t ragged, int32_t window, int32_t max_len);
 int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_heads *y, int32_t rows, int32_t q_heads,
                         const int32_t *table, int32_t width, const int32_t *lens, const int32_t *ends, int32_t batch,
                         float scale, int32_t causal, int32_t window, int32_t max_len, void *ws, size_t ws_bytes,

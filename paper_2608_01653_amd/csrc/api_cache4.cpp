@@ -95,16 +95,16 @@ int32_t cache_call(const hatq_cache4 *C, const hatq_heads *k, const hatq_heads *
 
 // The checks of an attention's sizes, and its layout.
 int32_t check_attention(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch, bool ragged,
-                        int32_t max_len, hatq::AttentionPlan *p) {
+                        int32_t window, int32_t max_len, hatq::AttentionPlan *p) {
     int32_t s = check_cache(C);
     if (s == HATQ_OK) s = check_sizes(C, rows, width, batch, ragged);
     if (s != HATQ_OK) return s;
-    if (q_heads <= 0 || q_heads % C->heads != 0 || max_len < 0) return HATQ_EINVAL;
+    if (q_heads <= 0 || q_heads % C->heads != 0 || max_len < 0 || window < 0) return HATQ_EINVAL;
     if (q_heads > kMaxHeads * 16 || (int64_t)rows * q_heads > INT32_MAX / 2) return HATQ_EUNSUPPORTED;
     if (rows == 0) return HATQ_OK;
     const int64_t most = (int64_t)width * C->page_size;
     *p = hatq::plan_attention(batch, rows, C->heads, q_heads / C->heads, C->dim,
-                              max_len > 0 && max_len < most ? max_len : most, ragged);
+                              max_len > 0 && max_len < most ? max_len : most, ragged, window);
     return HATQ_OK;
 }
 
@@ -144,9 +144,9 @@ int32_t hatq_cache4_read(const hatq_cache4 *C, const hatq_heads *k, const hatq_h
 }
 
 size_t hatq_attention4_ws_bytes(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch,
-                                int32_t ragged, int32_t max_len) {
+                                int32_t ragged, int32_t window, int32_t max_len) {
     hatq::AttentionPlan p{};
-    if (check_attention(C, rows, q_heads, width, batch, ragged != 0, max_len, &p) != HATQ_OK || rows == 0) return 0;
+    if (check_attention(C, rows, q_heads, width, batch, ragged != 0, window, max_len, &p) != HATQ_OK || rows == 0) return 0;
     return attention_bytes(C, p);
 }
 
@@ -155,9 +155,9 @@ int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_he
                         float scale, int32_t causal, int32_t window, int32_t max_len, void *ws, size_t ws_bytes,
                         void *stream) {
     hatq::AttentionPlan p{};
-    int32_t s = check_attention(C, rows, q_heads, width, batch, ends != nullptr, max_len, &p);
+    int32_t s = check_attention(C, rows, q_heads, width, batch, ends != nullptr, window, max_len, &p);
     if (s != HATQ_OK) return s;
-    if ((causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal) || !std::isfinite(scale)) return HATQ_EINVAL;
+    if ((causal != 0 && causal != 1) || (window > 0 && !causal) || !std::isfinite(scale)) return HATQ_EINVAL;
     if (rows == 0) return HATQ_OK;
     if ((s = check_places(table, lens, ends)) != HATQ_OK) return s;
     if ((s = check_heads(q, rows, q_heads, C->dim, false)) != HATQ_OK) return s;

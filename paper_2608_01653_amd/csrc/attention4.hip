@@ -121,13 +121,13 @@ __device__ __forceinline__ v8h join8(const v2h (&p)[4]) {
 // hold channels 0, 4, 1, 5, 2, 6, 3, 7.
 __device__ __forceinline__ constexpr int key_channel(int i) { return (i >> 1) % 2 * 4 + (i >> 2) + (i & 1) * 2; }
 
-// The operand of 16 columns, [NB][2 steps of 32 channels][2 halves][64 lanes] in LDS.
+// The operand of 16 columns, [NB][2 steps of 32 channels][2 halves][64 lanes], and then
+// their steps, in LDS.
 template <int NB>
-constexpr int kQueryBytes = NB * 4096;
+constexpr int kQueryBytes = NB * 4096 + 64;
 
 template <int NB>
-__device__ __forceinline__ void load_query(const AttentionArgs &a, const ColTile &t, int head, int length, int col,
-                                           Query &q, v8h *lds) {
+__device__ __forceinline__ void make_query(const AttentionArgs &a, const ColTile &t, int head, int col, char *lds) {
     const int lane = threadIdx.x & 63, chunk = lane >> 4;
     const int c = min(t.col0 + col + (lane & 15), t.count * a.share - 1);
     const int i = c / a.share, g = c - i * a.share;
@@ -135,7 +135,7 @@ __device__ __forceinline__ void load_query(const AttentionArgs &a, const ColTile
     const int64_t at = (int64_t)(t.row0 + i) * a.q.row + (int64_t)(head * a.share + g) * a.q.head;
 #pragma unroll
     for (int b = 0; b < NB; ++b) load_head16(a.q, at, b * 64 + chunk * 16, a.c.dim, v[b]);
-    head_butterfly(v, a.c.log_b, chunk, ChunksApart{});
+    head_butterfly(v, a.c.log_b, ChunksApart{});
     float m = 0.0f;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -145,7 +145,10 @@ __device__ __forceinline__ void load_query(const AttentionArgs &a, const ColTile
     const int up = 14 - __builtin_amdgcn_frexp_expf(m);
     const float factor = a.scale * kLog2e * __uint_as_float((uint32_t)(127 - a.c.log_b) << 23);
     // (a query that is not finite has scores NaN)
-    q.step = m < __builtin_inff() ? __builtin_amdgcn_ldexpf(factor, -up) : __builtin_nanf("");
+    if (chunk == 0)
+        reinterpret_cast<float *>(lds + NB * 4096)[lane] =
+            m < __builtin_inff() ? __builtin_amdgcn_ldexpf(factor, -up) : __builtin_nanf("");
+    v8h *const to = reinterpret_cast<v8h *>(lds);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -158,9 +161,15 @@ __device__ __forceinline__ void load_query(const AttentionArgs &a, const ColTile
                 half[1][j] = (_Float16)(x - (float)half[0][j]);
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) lds[((b * 2 + w) * 2 + k) * 64 + lane] = half[k];
+            for (int k = 0; k < 2; ++k) to[((b * 2 + w) * 2 + k) * 64 + lane] = half[k];
         }
-    q.pos = a.causal ? length - t.count + i : length - 1;
+}
+
+// The positions that this lane's column sees.
+template <int NB>
+__device__ __forceinline__ void see(const AttentionArgs &a, const ColTile &t, int length, int col, Query &q) {
+    const int c = min(t.col0 + col + (int)(threadIdx.x & 15), t.count * a.share - 1);
+    q.pos = a.causal ? length - t.count + c / a.share : length - 1;
     q.from = a.window ? max(q.pos - a.window + 1, 0) : 0;
 }
 
@@ -253,11 +262,11 @@ __device__ __forceinline__ float scale_of(const v4u &w, int j) {
 // EDGE: some positions may be hidden from some columns.
 template <int NB, int NP, int NQ, bool EDGE, bool HALF>
 __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const StepAt &next, const LaneAt &mine, const Query (&q)[NQ],
-                                     const v8h *query, int p0, Sums<NB> (&sum)[NQ]) {
+                                     const char *query, int p0, Sums<NB> (&sum)[NQ]) {
     const int lane = threadIdx.x & 63;
     const int first = p0 + 8 * (lane >> 4);
     float t[NQ][8];
-    uint32_t x_at = lane;
+    uint32_t x_at = lane * 16;
     asm volatile("" : "+v"(x_at));      // read in every step: kept over the loop, the query's registers spill
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -280,7 +289,7 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const v8h x = query[n * (NB * 256) + ((b * 2 + w) * 2 + k) * 64 + x_at];
+                    const v8h x = *reinterpret_cast<const v8h *>(query + n * kQueryBytes<NB> + ((b * 2 + w) * 2 + k) * 1024 + x_at);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) acc[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[h], x, acc[n][h], 0, 0, 0);
                 }
@@ -376,43 +385,55 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
 }
 
 // Every stride-th step of the positions [from, to) that some column of a wave sees, `from` a
-// multiple of 32; every column sees all of [sure_from, sure_to).
-template <int NB, int NP, int NQ, bool HALF>
-__device__ __forceinline__ void walk(const AttentionArgs &a, int seq, int head, const Query (&q)[NQ], const v8h *query, int from,
-                                     int to, int stride, int sure_from, int sure_to, Sums<NB> (&sum)[NQ]) {
-    if (from >= to) return;
-    const int32_t *table = a.at.table + (int64_t)seq * a.at.width;
-    const int64_t head0 = page_offset<NB>(a.c, 0, head);
-    const LaneAt mine = lane_at<NB, HALF>();
+// multiple of 32; every column sees all of [sure_from, sure_to).  The first step's loads are
+// made at once, before the queries.
+template <int NB, bool HALF>
+struct Walk {
+    const AttentionArgs &a;
+    const int32_t *table;
+    const int64_t head0;
+    const int from, to, stride;
+    const LaneAt mine;
     Step<NB> s;
-    StepAt here = step_at<NB, HALF>(a.c, head0, mine, pages_of<HALF>(a.c, a.at, table, from), from);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) load_keys<NB, HALF>(here, mine, b, s);
-    load_scales<NB, HALF>(here, mine, 0, s.key_scale);
-    load_scales<NB, HALF>(here, mine, 1, s.value_scale);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) load_values<NB, HALF>(here, mine, b, s);
+    StepAt here;
+    Pages pages;
+
     // (the step after a wave's last one: the same again, not used)
-    const auto after = [&](int p) { return p + stride < to ? p + stride : p; };
-    Pages pages = pages_of<HALF>(a.c, a.at, table, after(from));
-    const auto sure = [&](int p) { return p >= sure_from && p + 32 <= sure_to && !here.lacks; };
-    // (a loop each: as the branches of one, the compiler makes both kinds' common parts first and
-    // keeps all of them)
-    for (int p = from; p < to;) {
-        for (; p < to && sure(p); p += stride) {
-            const StepAt next = step_at<NB, HALF>(a.c, head0, mine, pages, after(p));
-            pages = pages_of<HALF>(a.c, a.at, table, after(after(p)));
-            step<NB, NP, NQ, false, HALF>(s, here, next, mine, q, query, p, sum);
-            here = next;
-        }
-        for (; p < to && !sure(p); p += stride) {
-            const StepAt next = step_at<NB, HALF>(a.c, head0, mine, pages, after(p));
-            pages = pages_of<HALF>(a.c, a.at, table, after(after(p)));
-            step<NB, NP, NQ, true, HALF>(s, here, next, mine, q, query, p, sum);
-            here = next;
+    __device__ __forceinline__ int after(int p) const { return p + stride < to ? p + stride : p; }
+
+    __device__ __forceinline__ Walk(const AttentionArgs &args, int seq, int head, int begin, int end, int by)
+        : a(args), table(args.at.table + (int64_t)seq * args.at.width), head0(page_offset<NB>(args.c, 0, head)), from(begin),
+          to(end), stride(by), mine(lane_at<NB, HALF>()) {
+        if (from >= to) return;
+        here = step_at<NB, HALF>(a.c, head0, mine, pages_of<HALF>(a.c, a.at, table, from), from);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) load_keys<NB, HALF>(here, mine, b, s);
+        load_scales<NB, HALF>(here, mine, 0, s.key_scale);
+        load_scales<NB, HALF>(here, mine, 1, s.value_scale);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) load_values<NB, HALF>(here, mine, b, s);
+        pages = pages_of<HALF>(a.c, a.at, table, after(from));
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    template <int NP, int NQ, bool EDGE>
+    __device__ __forceinline__ void one(int p, const Query (&q)[NQ], const char *query, Sums<NB> (&sum)[NQ]) {
+        const StepAt next = step_at<NB, HALF>(a.c, head0, mine, pages, after(p));
+        pages = pages_of<HALF>(a.c, a.at, table, after(after(p)));
+        step<NB, NP, NQ, EDGE, HALF>(s, here, next, mine, q, query, p, sum);
+        here = next;
+    }
+    template <int NP, int NQ>
+    __device__ __forceinline__ void run(const Query (&q)[NQ], const char *query, int sure_from, int sure_to, Sums<NB> (&sum)[NQ]) {
+        const auto sure = [&](int p) { return p >= sure_from && p + 32 <= sure_to && !here.lacks; };
+        // (a loop each: as the branches of one, the compiler makes both kinds' common parts first and
+        // keeps all of them)
+        for (int p = from; p < to;) {
+            for (; p < to && sure(p); p += stride) one<NP, NQ, false>(p, q, query, sum);
+            for (; p < to && !sure(p); p += stride) one<NP, NQ, true>(p, q, query, sum);
         }
     }
-}
+};
 
 // Sums of a column whose m and l are whole: transformed, divided, stored.
 template <int NB>
@@ -428,7 +449,7 @@ __device__ __forceinline__ void store_columns(const AttentionArgs &a, const ColT
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int j = 0; j < 4; ++j) v[b][4 * r + j] = o[b][j][r];
-    head_butterfly(v, a.c.log_b, chunk, ChunksApart{});
+    head_butterfly(v, a.c.log_b, ChunksApart{});
     if (c >= t.count * a.share) return;
     const int i = c / a.share, g = c - i * a.share;
     const int64_t at = (int64_t)(t.row0 + i) * a.y.row + (int64_t)(head * a.share + g) * a.y.head;
@@ -447,44 +468,47 @@ __device__ __forceinline__ int length_of(const AttentionArgs &a, int seq) {
     return n < most ? n : (int)most;
 }
 
-// Sums of `waves` waves (a power of two) of one tile into wave 0's: scaled to the same
-// maximum and added by halves.  lds: waves * 128 bytes, and waves / 2 * NB * 4 KB.
+// Sums of `waves` waves of one tile into wave 0's: every wave leaves its own in LDS, every
+// thread adds the waves' values of some of them.  lds: waves * (NB * 4 KB + 128 bytes), not in
+// use by others.
 template <int NB>
 __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, char *lds) {
-    float *ml = reinterpret_cast<float *>(lds);
-    v4f *sums = reinterpret_cast<v4f *>(lds + waves * 128);
+    if (waves == 1) {
+        s.l = chunks_sum(s.l);
+        return;
+    }
+    v4f *const sums = reinterpret_cast<v4f *>(lds);
+    float *const ml = reinterpret_cast<float *>(lds + waves * (NB * 4096));
     const int lane = threadIdx.x & 63, col = lane & 15;
     const float l = chunks_sum(s.l);
     if (lane < 16) {
         ml[wave * 32 + col] = s.m;
         ml[wave * 32 + 16 + col] = l;
     }
-    __syncthreads();
-    float m = kLowest, all = 0.0f;
-    for (int w = 0; w < waves; ++w) m = fmaxf(m, ml[w * 32 + col]);
-    for (int w = 0; w < waves; ++w) all += ml[w * 32 + 16 + col] * __builtin_amdgcn_exp2f(ml[w * 32 + col] - m);
-    const float down = __builtin_amdgcn_exp2f(s.m - m);
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s.o[b][j] *= down;
+        for (int j = 0; j < 4; ++j) sums[((wave * NB + b) * 4 + j) * 64 + lane] = s.o[b][j];
+    __syncthreads();
+    float m = kLowest, all = 0.0f;
+    for (int w = 0; w < waves; ++w) m = fmaxf(m, ml[w * 32 + col]);
+    for (int i = wave; i < NB * 4; i += waves) {
+        v4f x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int w = 0; w < waves; ++w) x += sums[(w * NB * 4 + i) * 64 + lane] * __builtin_amdgcn_exp2f(ml[w * 32 + col] - m);
+        // (in the first wave's place, which no other thread reads here)
+        sums[i * 64 + lane] = x;
+    }
+    if (wave == 0)
+        for (int w = 0; w < waves; ++w) all += ml[w * 32 + 16 + col] * __builtin_amdgcn_exp2f(ml[w * 32 + col] - m);
     s.m = m;
     s.l = all;
-    for (int h = waves >> 1; h; h >>= 1) {
-        if (wave >= h && wave < 2 * h) {
+    __syncthreads();
+    if (wave == 0) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sums[(((wave - h) * NB + b) * 4 + j) * 64 + lane] = s.o[b][j];
-        }
-        __syncthreads();
-        if (wave < h) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s.o[b][j] += sums[((wave * NB + b) * 4 + j) * 64 + lane];
-        }
-        __syncthreads();
+            for (int j = 0; j < 4; ++j) s.o[b][j] = sums[(b * 4 + j) * 64 + lane];
     }
 }
 
@@ -493,7 +517,7 @@ __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, cha
 // them.  (Its waves share the positions there too, not the columns: blocks then last a
 // fourth as long, and the last ones of a full card leave less of it idle.)
 template <int NB, int NP, int NQ, bool HALF>
-__global__ void __launch_bounds__(NQ > 1 ? 256 : 512) __attribute__((amdgpu_waves_per_eu(NB <= 2 && NQ == 1 ? 4 : 2)))
+__global__ void __launch_bounds__(NQ > 1 ? 256 : NB <= 2 ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(NB <= 2 && NQ == 1 ? 4 : 2)))
 attention4_kernel(const AttentionArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int waves = blockDim.x >> 6, wave = wave_of_block(), lane = threadIdx.x & 63;
@@ -503,19 +527,6 @@ attention4_kernel(const AttentionArgs a) {
     const ColTile t = col_tile<16 * NQ>(a, tile);
     if (t.seq < 0) return;
     const int length = length_of(a, t.seq), cols = t.count * a.share;
-    Query q[NQ];
-    Sums<NB> s[NQ];
-    v8h *query = reinterpret_cast<v8h *>(lds);      // (every wave makes it, and of the same values)
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        load_query<NB>(a, t, head, length, 16 * n, q[n], query + n * (NB * 256));
-        s[n].m = kLowest;
-        s[n].l = 0.0f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[n].o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    }
     // rows of the first and last column
     const int i0 = t.col0 / a.share, i1 = (min(t.col0 + 16 * NQ, cols) - 1) / a.share;
     int from = 0, to = length, sure_from = 0, sure_to = length;
@@ -529,8 +540,28 @@ attention4_kernel(const AttentionArgs a) {
     }
     const int64_t steps = to > from ? (to - from + 31) >> 5 : 0;
     const int begin = (int)(steps * split / a.splits), end = (int)(steps * (split + 1) / a.splits);
-    const int last = end == steps ? to : from + 32 * end;
-    walk<NB, NP, NQ, HALF>(a, t.seq, head, q, query, from + 32 * (begin + wave), last, 32 * waves, sure_from, sure_to, s);
+    Walk<NB, HALF> walk(a, t.seq, head, from + 32 * (begin + wave), end == steps ? to : from + 32 * end, 32 * waves);
+    Query q[NQ];
+    Sums<NB> s[NQ];
+    // (sixteen columns a wave: made by all, it would take as long as two steps)
+    char *const query = lds;
+    for (int n = wave; n < NQ; n += waves) make_query<NB>(a, t, head, 16 * n, query + n * kQueryBytes<NB>);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) see<NB>(a, t, length, 16 * n, q[n]);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+        q[n].step = *reinterpret_cast<const float *>(query + n * kQueryBytes<NB> + NB * 4096 + 4 * (lane & 15));
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        s[n].m = kLowest;
+        s[n].l = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[n].o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    walk.template run<NP, NQ>(q, query, sure_from, sure_to, s);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         __syncthreads();    // the LDS of before has been read
@@ -553,7 +584,7 @@ attention4_kernel(const AttentionArgs a) {
 
 // The partial results of a tile's splits, joined.
 template <int NB>
-__global__ void __launch_bounds__(512) attention4_join_kernel(const AttentionArgs a) {
+__global__ void __launch_bounds__(1024) attention4_join_kernel(const AttentionArgs a) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int waves = blockDim.x >> 6, wave = wave_of_block(), lane = threadIdx.x & 63;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
@@ -595,7 +626,7 @@ dim3 blocks_of(int64_t n) {
 template <int NB, int NP, bool HALF>
 hipError_t launch(const AttentionArgs &a, const AttentionPlan &p, hipStream_t st) {
     constexpr int NQ = wide_cols(64 * NB) / 16;
-    const size_t join = (size_t)p.waves * (NB * 2048 + 128), query = (size_t)(p.cols / 16) * NB * 4096;
+    const size_t join = p.waves > 1 ? (size_t)p.waves * (NB * 4096 + 128) : 0, query = (size_t)(p.cols / 16) * kQueryBytes<NB>;
     const size_t lds = join > query ? join : query;
     const dim3 grid = blocks_of(p.tiles * a.c.heads * p.splits);
     if (p.cols == 16) attention4_kernel<NB, NP, 1, HALF><<<grid, p.waves * 64, lds, st>>>(a);

@@ -4,21 +4,32 @@
 namespace hatq {
 
 AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t share, int32_t dim, int64_t max_len,
-                             bool ragged) {
+                             bool ragged, int32_t window) {
     const int64_t cols = (int64_t)rows * share;
     AttentionPlan p{};
     // a sequence's columns on average
     const bool many = cols / batch >= 128;
     p.cols = many ? wide_cols(dim) : 16;
     p.tiles = ragged ? cols / p.cols + (batch < rows ? batch : rows) : batch * ((cols / batch + p.cols - 1) / p.cols);
-    p.waves = dim <= 128 && !many ? 8 : 4;
+    p.waves = 4;
     p.splits = 1;
     if (many) return p;
-    // blocks that fill the card, of at least two steps of 32 positions a wave
-    const int64_t steps = (max_len + 31) / 32, base = p.tiles * heads;
-    int64_t splits = 512 / base;
-    if (splits > steps / (2 * p.waves)) splits = steps / (2 * p.waves);
+    // Parts of a sequence while there is not a block for each CU, of at least two steps of 32
+    // positions a wave; 8 waves a block, 16 where each of them has four steps and no other
+    // block would share its CU, fewer where a sequence is shorter.  (us a call in a graph, 8
+    // heads of 128 channels, bf16: 1 sequence of 8192 in 8 parts 18.2, in 16 16.2, in 32 16.6;
+    // 8 of 4096 in 1 part 26, in 4 20.8, in 8 22.1; 32 of 820 to 4096 whole, 8 waves 35.6, 16
+    // 33.6, in 2 parts 34.7; 2 of 131072, 4 heads, fp16, 32 parts, 8 waves 48.3, 16 46.8; 1 of
+    // 300, 64 channels, 4 waves 8.3, 8 7.9, 16 8.9.)
+    int64_t most = max_len;
+    if (window > 0 && window + rows / batch < most) most = window + rows / batch;
+    const int64_t steps = (most + 31) / 32, base = p.tiles * heads;
+    int64_t splits = 256 / base;
+    if (splits > steps / 16) splits = steps / 16;
     p.splits = splits < 1 ? 1 : (int32_t)splits;
+    p.waves = 8;
+    if (dim <= 128 && base * p.splits <= 256 && steps / p.splits >= 64) p.waves = 16;
+    while (p.waves > 1 && p.waves / 2 >= steps) p.waves /= 2;
     return p;
 }
 

@@ -53,7 +53,7 @@ struct AttentionPlan {
 };
 constexpr int wide_cols(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 32 : 16; }
 AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t share, int32_t dim, int64_t max_len,
-                             bool ragged);
+                             bool ragged, int32_t window);
 // Bytes of one partial result: 16 query rows of a head, their maxima and sums.
 inline size_t partial4_bytes(int32_t dim) { return (size_t)((dim + 63) / 64) * 4096 + 128; }
 // For heads of up to 64, 128, 192 and 256 channels.

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs
     float v[NB][16];
 #pragma unroll
     for (int b = 0; b < NB; ++b) load_head16(x, n.row * x.row + n.head * x.head, b * 64 + n.chunk * 16, a.c.dim, v[b]);
-    head_butterfly(v, a.c.log_b, n.chunk, ChunksAdjacent{});
+    head_butterfly(v, a.c.log_b, ChunksAdjacent{});
     float m[NB], all = 0.0f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const CacheArgs a
 #pragma unroll
             for (int j = 0; j < 16; ++j) v[b][j] = 0.0f;
     }
-    head_butterfly(v, a.c.log_b, n.chunk, ChunksAdjacent{});
+    head_butterfly(v, a.c.log_b, ChunksAdjacent{});
     const Heads4 &x = a.x[n.which];
     const float inv_b = __uint_as_float((uint32_t)(127 - a.c.log_b) << 23);
 #pragma unroll

@@ -118,31 +118,56 @@ __device__ __forceinline__ void store_head16(const Heads4 &x, int64_t at, int c0
     else put16(static_cast<_Float16 *>(x.p) + at, c0, dim, v);
 }
 
-// The order-2^lb butterfly of heads held 16 channels a lane and block, ascending stages;
-// other(MASK, v): the value of the lane that holds the chunk ^ MASK, up: whether this lane's
-// chunk number has the bit.
-template <int NB, typename F>
-__device__ __forceinline__ void head_butterfly(float (&v)[NB][16], int lb, int chunk, F other) {
+// Chunks of a head in adjacent lanes (the cache's own kernels), or 16 lanes apart, as a
+// matrix instruction has them (the attention): the stage with the chunk ^ MASK of 16 values.
+struct ChunksAdjacent {
+    template <int MASK>
+    static __device__ __forceinline__ void stage(float (&v)[16]) {
+        const float c = (threadIdx.x & MASK) ? -1.0f : 1.0f;    // other + c own, exactly
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = __builtin_fmaf(v[j], c, lane_xor<MASK>(v[j]));
+    }
+};
+struct ChunksApart {
+    // A swap of two values between the lanes of a pair leaves each lane with both partners of
+    // one of the values; their sum and difference go back the same way.
+    template <int MASK>
+    static __device__ __forceinline__ void swap(float &x, float &y) {
+        const uint32_t u = __float_as_uint(x), w = __float_as_uint(y);
+        if constexpr (MASK == 1) {
+            const auto r = __builtin_amdgcn_permlane16_swap(u, w, false, false);
+            x = __uint_as_float(r[0]);
+            y = __uint_as_float(r[1]);
+        } else {
+            const auto r = __builtin_amdgcn_permlane32_swap(u, w, false, false);
+            x = __uint_as_float(r[0]);
+            y = __uint_as_float(r[1]);
+        }
+    }
+    template <int MASK>
+    static __device__ __forceinline__ void stage(float (&v)[16]) {
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            swap<MASK>(v[j], v[j + 1]);
+            float sum = v[j] + v[j + 1], less = v[j] - v[j + 1];
+            swap<MASK>(sum, less);
+            v[j] = sum;
+            v[j + 1] = less;
+        }
+    }
+};
+
+// The order-2^lb butterfly of heads held 16 channels a lane and block, ascending stages.
+template <int NB, typename C>
+__device__ __forceinline__ void head_butterfly(float (&v)[NB][16], int lb, C) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         if (lb >= 1) reg_stage<1>(v[n]);
         if (lb >= 2) reg_stage<2>(v[n]);
         if (lb >= 3) reg_stage<4>(v[n]);
         if (lb >= 4) reg_stage<8>(v[n]);
-        if (lb >= 5) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float o = other(std::integral_constant<int, 1>{}, v[n][j]);
-                v[n][j] = (chunk & 1) ? o - v[n][j] : v[n][j] + o;
-            }
-        }
-        if (lb >= 6) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float o = other(std::integral_constant<int, 2>{}, v[n][j]);
-                v[n][j] = (chunk & 2) ? o - v[n][j] : v[n][j] + o;
-            }
-        }
+        if (lb >= 5) C::template stage<1>(v[n]);
+        if (lb >= 6) C::template stage<2>(v[n]);
     }
     if constexpr (NB % 2 == 0) {    // (a block of 128 divides the head: no odd one)
         if (lb >= 7) {
@@ -157,25 +182,5 @@ __device__ __forceinline__ void head_butterfly(float (&v)[NB][16], int lb, int c
         }
     }
 }
-
-// Chunks of a head in adjacent lanes (the cache's own kernels), or 16 lanes apart, as a
-// matrix instruction has them (the attention).
-struct ChunksAdjacent {
-    template <int M>
-    __device__ __forceinline__ float operator()(std::integral_constant<int, M>, float v) const { return lane_xor<M>(v); }
-};
-struct ChunksApart {
-    template <int M>
-    __device__ __forceinline__ float operator()(std::integral_constant<int, M>, float v) const {
-        const uint32_t u = __float_as_uint(v);
-        if constexpr (M == 1) {
-            const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-            return __uint_as_float((threadIdx.x & 16) ? r[0] : r[1]);
-        } else {
-            const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-            return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
-        }
-    }
-};
 
 }  // namespace hatq

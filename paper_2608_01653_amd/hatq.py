@@ -203,7 +203,7 @@ def load(build_if_missing: bool = False):
     for f in (L.hatq_cache4_append, L.hatq_cache4_read):
         f.argtypes = [C, H, H, i32, P, i32, P, P, i32, P]
         f.restype = i32
-    L.hatq_attention4_ws_bytes.argtypes = [C, i32, i32, i32, i32, i32, i32]
+    L.hatq_attention4_ws_bytes.argtypes = [C] + [i32] * 7
     L.hatq_attention4_ws_bytes.restype = sz
     L.hatq_attention4.argtypes = [C, H, H, i32, i32, P, i32, P, P, i32, f32, i32, i32, i32, P, sz, P]
     L.hatq_attention4.restype = i32
@@ -1242,9 +1242,9 @@ def hatq_cache4_read(cache: Cache4, rows: int, table: torch.Tensor, lens: torch.
 
 
 def hatq_attention4_ws_bytes(cache: Cache4, rows: int, q_heads: int, width: int, batch: int, ragged: bool = False,
-                             max_len: int = 0) -> int:
-    _sizes("sizes", rows, q_heads, width, batch, max_len)
-    return int(load().hatq_attention4_ws_bytes(cache.ref, rows, q_heads, width, batch, int(ragged), max_len))
+                             window: int = 0, max_len: int = 0) -> int:
+    _sizes("sizes", rows, q_heads, width, batch, window, max_len)
+    return int(load().hatq_attention4_ws_bytes(cache.ref, rows, q_heads, width, batch, int(ragged), window, max_len))
 
 
 def hatq_attention4(cache: Cache4, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
@@ -1268,7 +1268,7 @@ def hatq_attention4(cache: Cache4, q: torch.Tensor, table: torch.Tensor, lens: t
     _sizes("window, max_len", window, max_len)
     _here(cache.device, q, y, table, lens, ends, ws)
     if ws is None:
-        nbytes = load().hatq_attention4_ws_bytes(cache.ref, n, h, width, batch, int(ends is not None), max_len)
+        nbytes = load().hatq_attention4_ws_bytes(cache.ref, n, h, width, batch, int(ends is not None), window, max_len)
         if nbytes:
             ws = torch.empty(nbytes, dtype=torch.int8, device=q.device)
     _need(ws, "ws", torch.int8, 0, optional=True)

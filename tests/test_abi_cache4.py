@@ -126,7 +126,7 @@ def test_attention_refusals(L):
         assert attend(L, **kw) == EUNSUPPORTED, kw
     # a long table: the positions are split, and need a workspace
     kw = dict(width=4096)
-    need = L.hatq_attention4_ws_bytes(ctypes.byref(cache()), 8, 8, 4096, 4, 0, 0)
+    need = L.hatq_attention4_ws_bytes(ctypes.byref(cache()), 8, 8, 4096, 4, 0, 0, 0)
     assert need > 0
     assert attend(L, **kw, ws=None) == EINVAL
     assert attend(L, **kw, ws=P + 128) == EINVAL
@@ -136,10 +136,10 @@ def test_attention_refusals(L):
 def test_workspace_bytes(L):
     def size(c, *a):
         return L.hatq_attention4_ws_bytes(ctypes.byref(c), *a)
-    assert size(cache(), 0, 8, 4096, 4, 0, 0) == 0
-    assert size(cache(), 8, 8, 1, 4, 0, 0) == 0
-    assert size(cache(), 8, 8, 4096, 4, 0, 32) == 0
-    assert size(cache(), 8, 7, 4096, 4, 0, 0) == 0
-    assert L.hatq_attention4_ws_bytes(None, 8, 8, 4096, 4, 0, 0) == 0
+    assert size(cache(), 0, 8, 4096, 4, 0, 0, 0) == 0
+    assert size(cache(), 8, 8, 1, 4, 0, 0, 0) == 0
+    assert size(cache(), 8, 8, 4096, 4, 0, 0, 32) == 0
+    assert size(cache(), 8, 7, 4096, 4, 0, 0, 0) == 0
+    assert L.hatq_attention4_ws_bytes(None, 8, 8, 4096, 4, 0, 0, 0) == 0
     # as many parts as fit, none larger than the other: bounded however long the table
-    assert size(cache(), 1, 4, 2 ** 24, 1, 0, 0) <= 2 ** 26
+    assert size(cache(), 1, 4, 2 ** 24, 1, 0, 0, 0) <= 2 ** 26
