@@ -133,8 +133,7 @@ __device__ __forceinline__ void make_query(const AttentionArgs &a, const ColTile
     const int i = c / a.share, g = c - i * a.share;
     float v[NB][16];
     const int64_t at = (int64_t)(t.row0 + i) * a.q.row + (int64_t)(head * a.share + g) * a.q.head;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) load_head16(a.q, at, b * 64 + chunk * 16, a.c.dim, v[b]);
+    load_head<NB>(a.q, at, chunk, a.c.dim, v, [] {});
     head_butterfly(v, a.c.log_b, ChunksApart{});
     float m = 0.0f;
 #pragma unroll

@@ -76,29 +76,45 @@ __device__ __forceinline__ int page_of(const Cache4 &c, const Places4 &at, int s
     return (unsigned)page < (unsigned)c.pages ? page : -1;
 }
 
-// Sixteen adjacent channels from c0 on of a head of `dim`, zeros past its end.
-template <typename T>
-__device__ __forceinline__ void load16(const T *p, int c0, int dim, float *v) {
-    if (c0 + 16 <= dim) {
-        Raw8<T> a, b;
-        load_raw(p + c0, a);
-        load_raw(p + c0 + 8, b);
-        raw_values(a, v);
-        raw_values(b, v + 8);
-        return;
+// A head's values from element `at` on: 16 channels of each block, chunk `chunk` of it, zeros
+// past the head's end; all loads under way before the first value is used, and `between`,
+// which does not read them, before that.
+template <int NB, typename T, typename F>
+__device__ __forceinline__ void load_head(const T *p, int chunk, int dim, float (&v)[NB][16], F between) {
+    Raw8<T> raw[NB][2];
+    T one[16];      // (of a chunk that the head's end cuts: one block's at most)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int c0 = b * 64 + chunk * 16;
+        if (c0 + 16 <= dim) {
+            load_raw(p + c0, raw[b][0]);
+            load_raw(p + c0 + 8, raw[b][1]);
+        }
     }
+    between();
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = 0.0f;
-    if (c0 < dim) {
+    for (int b = 0; b < NB; ++b) {
+        const int c0 = b * 64 + chunk * 16;
+        if (c0 + 16 <= dim) {
+            raw_values(raw[b][0], v[b]);
+            raw_values(raw[b][1], v[b] + 8);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (c0 + j < dim) v[j] = to_float(p[c0 + j]);
+            for (int j = 0; j < 16; ++j) v[b][j] = 0.0f;
+            if (c0 < dim) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) one[j] = p[min(c0 + j, dim - 1)];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[b][j] = c0 + j < dim ? to_float(one[j]) : 0.0f;
+            }
+        }
     }
 }
-__device__ __forceinline__ void load_head16(const Heads4 &x, int64_t at, int c0, int dim, float *v) {
-    if (x.type == kF32) load16(static_cast<const float *>(x.p) + at, c0, dim, v);
-    else if (x.type == kBf16) load16(static_cast<const bf16_t *>(x.p) + at, c0, dim, v);
-    else load16(static_cast<const _Float16 *>(x.p) + at, c0, dim, v);
+template <int NB, typename F>
+__device__ __forceinline__ void load_head(const Heads4 &x, int64_t at, int chunk, int dim, float (&v)[NB][16], F between) {
+    if (x.type == kF32) load_head<NB>(static_cast<const float *>(x.p) + at, chunk, dim, v, between);
+    else if (x.type == kBf16) load_head<NB>(static_cast<const bf16_t *>(x.p) + at, chunk, dim, v, between);
+    else load_head<NB>(static_cast<const _Float16 *>(x.p) + at, chunk, dim, v, between);
 }
 
 template <typename T>
@@ -120,12 +136,13 @@ __device__ __forceinline__ void store_head16(const Heads4 &x, int64_t at, int c0
 
 // Chunks of a head in adjacent lanes (the cache's own kernels), or 16 lanes apart, as a
 // matrix instruction has them (the attention): the stage with the chunk ^ MASK of 16 values.
+// Returns the sign of the values held relative to the transform's.
 struct ChunksAdjacent {
     template <int MASK>
-    static __device__ __forceinline__ void stage(float (&v)[16]) {
-        const float c = (threadIdx.x & MASK) ? -1.0f : 1.0f;    // other + c own, exactly
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = __builtin_fmaf(v[j], c, lane_xor<MASK>(v[j]));
+    static __device__ __forceinline__ float stage(float (&v)[16]) {
+        const float c = (threadIdx.x & MASK) ? -1.0f : 1.0f;
+        token_cross<MASK>(v, c);
+        return c;
     }
 };
 struct ChunksApart {
@@ -145,7 +162,7 @@ struct ChunksApart {
         }
     }
     template <int MASK>
-    static __device__ __forceinline__ void stage(float (&v)[16]) {
+    static __device__ __forceinline__ float stage(float (&v)[16]) {
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
             swap<MASK>(v[j], v[j + 1]);
@@ -154,20 +171,24 @@ struct ChunksApart {
             v[j] = sum;
             v[j + 1] = less;
         }
+        return 1.0f;
     }
 };
 
-// The order-2^lb butterfly of heads held 16 channels a lane and block, ascending stages.
+// The order-2^lb butterfly of heads held 16 channels a lane and block, ascending stages;
+// returns the sign of the values held relative to the transform's.
 template <int NB, typename C>
-__device__ __forceinline__ void head_butterfly(float (&v)[NB][16], int lb, C) {
+__device__ __forceinline__ float head_butterfly(float (&v)[NB][16], int lb, C) {
+    float sigma = 1.0f;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         if (lb >= 1) reg_stage<1>(v[n]);
         if (lb >= 2) reg_stage<2>(v[n]);
         if (lb >= 3) reg_stage<4>(v[n]);
         if (lb >= 4) reg_stage<8>(v[n]);
-        if (lb >= 5) C::template stage<1>(v[n]);
-        if (lb >= 6) C::template stage<2>(v[n]);
+        // (the same sign for every block)
+        if (lb >= 5) sigma = C::template stage<1>(v[n]);
+        if (lb >= 6) sigma *= C::template stage<2>(v[n]);
     }
     if constexpr (NB % 2 == 0) {    // (a block of 128 divides the head: no odd one)
         if (lb >= 7) {
@@ -181,6 +202,7 @@ __device__ __forceinline__ void head_butterfly(float (&v)[NB][16], int lb, C) {
                 }
         }
     }
+    return sigma;
 }
 
 }  // namespace hatq
