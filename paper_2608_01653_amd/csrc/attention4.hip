@@ -9,7 +9,7 @@
 // rows so that a lane's scores are the second product's operand as they are.
 //
 // First product: the codes in float16, exact, against the query in two float16 halves, 22
-// bits, after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
+// bits (many rows of bf16: one half, 11 bits), after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
 // kept relative to the largest of w s_v (not of w), so the float16 range holds whatever the
 // scales are (2^-100 to 2^100): off by 2^-11 of each weight or 2^-25 of the largest.  For
@@ -125,6 +125,10 @@ __device__ __forceinline__ constexpr int key_channel(int i) { return (i >> 1) % 
 // their steps, in LDS.
 template <int NB>
 constexpr int kQueryBytes = NB * 4096 + 64;
+// Halves of the query that count: both, or one for many columns of bf16, where the second's
+// products would take a third of the matrix instructions for bits that a bf16 output hides.
+template <int NP, int NQ>
+constexpr int kQueryHalves = NP == 1 && NQ > 1 ? 1 : 2;
 
 template <int NB>
 __device__ __forceinline__ void make_query(const AttentionArgs &a, const ColTile &t, int head, int col, char *lds) {
@@ -287,7 +291,7 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < kQueryHalves<NP, NQ>; ++k) {
                     const v8h x = *reinterpret_cast<const v8h *>(query + n * kQueryBytes<NB> + ((b * 2 + w) * 2 + k) * 1024 + x_at);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) acc[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[h], x, acc[n][h], 0, 0, 0);
@@ -628,7 +632,7 @@ hipError_t launch(const AttentionArgs &a, const AttentionPlan &p, hipStream_t st
     const size_t join = p.waves > 1 ? (size_t)p.waves * (NB * 4096 + 128) : 0, query = (size_t)(p.cols / 16) * kQueryBytes<NB>;
     const size_t lds = join > query ? join : query;
     const dim3 grid = blocks_of(p.tiles * a.c.heads * p.splits);
-    if (p.cols == 16) attention4_kernel<NB, NP, 1, HALF><<<grid, p.waves * 64, lds, st>>>(a);
+    if (NQ == 1 || p.cols == 16) attention4_kernel<NB, NP, 1, HALF><<<grid, p.waves * 64, lds, st>>>(a);
     else attention4_kernel<NB, NP, NQ, HALF><<<grid, p.waves * 64, lds, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;

@@ -7,13 +7,20 @@ AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t
                              bool ragged, int32_t window) {
     const int64_t cols = (int64_t)rows * share;
     AttentionPlan p{};
-    // a sequence's columns on average
-    const bool many = cols / batch >= 128;
-    p.cols = many ? wide_cols(dim) : 16;
-    p.tiles = ragged ? cols / p.cols + (batch < rows ? batch : rows) : batch * ((cols / batch + p.cols - 1) / p.cols);
+    const auto tiles = [&](int64_t by) {
+        return ragged ? cols / by + (batch < rows ? batch : rows) : batch * ((cols / batch + by - 1) / by);
+    };
+    // Wide blocks where they fill the card twice.  (us, 4 sequences of 4096, 4 heads of 128
+    // channels, bf16, wide and not: 128 columns each 66 and 31, 512 columns 70 and 63, 8192 columns
+    // 492 and 747; heads of 192 channels, 8192 columns 696 and 1239, of 64 303 and 463.  Of 256,
+    // whose two tiles do not fit the registers: 1846 and 1571.)
+    p.cols = wide_cols(dim);
+    p.tiles = tiles(p.cols);
     p.waves = 4;
     p.splits = 1;
-    if (many) return p;
+    if (p.cols > 16 && p.tiles * heads >= 512) return p;
+    p.cols = 16;
+    p.tiles = tiles(16);
     // Parts of a sequence while there is not a block for each CU, of at least two steps of 32
     // positions a wave; 8 waves a block, 16 where each of them has four steps and no other
     // block would share its CU, fewer where a sequence is shorter.  (us a call in a graph, 8

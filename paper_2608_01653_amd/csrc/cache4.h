@@ -51,7 +51,7 @@ struct AttentionPlan {
     int32_t waves, splits;  // splits: 1 where cols is more than 16
     int64_t tiles;          // blocks of columns of one cached head, over all sequences: an upper bound
 };
-constexpr int wide_cols(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 32 : 16; }
+constexpr int wide_cols(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 48 : dim <= 192 ? 32 : 16; }
 AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t share, int32_t dim, int64_t max_len,
                              bool ragged, int32_t window);
 // Bytes of one partial result: 16 query rows of a head, their maxima and sums.

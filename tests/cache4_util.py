@@ -89,8 +89,8 @@ def attention64(q, k, v, v_scale, hblock, scale, causal, window, fine, there=Non
     keys and values in the transformed basis [len, heads, dim] float64; v_scale [len, heads]:
     the largest of a value's scales; there [len]: positions whose page is.
 
-    The bound (u = 2^-24): the query in two float16 halves is off by 2^-22 = 4 u of itself; a
-    product is exact, and a score's sum in float32 (64 products, two scales of up to four
+    The bound (u = 2^-24): the query in two float16 halves is off by 2^-22 = 4 u of itself (many
+    rows of bfloat16, in one half, by 2^-11); a product is exact, and a score's sum in float32 (64 products, two scales of up to four
     groups, the factor) has at most 80 roundings, u sum |q k| each; an error of e moves each normalized weight by at most a
     factor exp(2 e).  A weight times scale in float16 is off by 2^-11 of itself (two halves
     2^-21), or where subnormal by 2^-25 of a unit that is at most 2 of the largest weight times
@@ -102,35 +102,42 @@ def attention64(q, k, v, v_scale, hblock, scale, causal, window, fine, there=Non
     qt = butterfly(q.astype(np.float64), hblock)
     y, bound = np.zeros(q.shape), np.zeros(q.shape)
     factor = scale / hblock
-    for i in range(n):
-        p = length - n + i
-        lo, hi = 0, length
-        if causal:
-            hi = min(length, p + 1)
-            if window:
-                lo = max(0, p - window + 1)
-        keep = np.arange(lo, max(lo, hi))
-        if there is not None:
-            keep = keep[there[keep]]
-        if keep.size == 0:
-            continue
-        for h in range(heads_q):
-            kk, vv = k[keep, h // share], v[keep, h // share]
-            t = kk @ qt[i, h] * factor
-            e = np.exp(t - t.max())
-            w = e / e.sum()
-            mag = butterfly_abs(w @ np.abs(vv), hblock)
-            et = 84 * U * (np.abs(kk) @ np.abs(qt[i, h])).max() * abs(factor)
-            rel = np.expm1(2 * et) + (2.0 ** -21 if fine else 2.0 ** -11) + (3 * keep.size + 24) * U
-            y[i, h] = butterfly(w @ vv, hblock) / hblock
-            low = 2.0 ** -24 * np.max(w * v_scale[keep, h // share]) * 1.01 * 7 * keep.size
-            bound[i, h] = rel * mag + low
+    at, key = length - n + np.arange(n)[:, None], np.arange(length)[None, :]
+    keep = np.ones((n, length), bool)
+    if causal:
+        keep &= key <= at
+        if window:
+            keep &= key > at - window
+    if there is not None:
+        keep &= there[None, :]
+    rows = keep.any(1)      # of the others all is 0
+    if not rows.any():
+        return y, bound
+    keep, count = keep[rows], keep[rows].sum(1)[:, None]
+    for h in range(heads_q):
+        # (what no row sees may be anything; what some row does not see is taken out of its sums)
+        kk, vv, vs = (np.where(keep.any(0).reshape(-1, *[1] * (x[:, h // share].ndim - 1)), x[:, h // share], 0.0) for x in (k, v, v_scale))
+        bad = keep & (np.isnan(kk).any(1) | np.isnan(vv).any(1))[None, :]
+        kk, vv, vs = np.nan_to_num(kk, nan=0.0), np.nan_to_num(vv, nan=0.0), np.nan_to_num(vs, nan=0.0)
+        qq = qt[rows, h]
+        t = np.where(keep, qq @ kk.T * factor, -np.inf)
+        e = np.exp(t - t.max(1, keepdims=True))
+        w = e / e.sum(1, keepdims=True)
+        size = np.where(keep, np.abs(qq) @ np.abs(kk).T, 0.0).max(1, keepdims=True) * abs(factor)
+        rel = np.expm1(2 * (80 * U + (2.0 ** -22 if fine else 2.0 ** -11)) * size) + (2.0 ** -21 if fine else 2.0 ** -11)
+        rel = rel + (3 * count + 24) * U
+        one = butterfly(w @ vv, hblock) / hblock
+        low = 2.0 ** -24 * (w * vs[None, :]).max(1, keepdims=True) * 1.01 * 7 * count
+        off = rel * butterfly_abs(w @ np.abs(vv), hblock) + low
+        one[bad.any(1)] = np.nan
+        off[bad.any(1)] = np.nan
+        y[rows, h], bound[rows, h] = one, off
     return y, bound
 
 
 def butterfly_abs(x, b):
     """(1 / b) sum over each block of |x|: what an error of x can move a transform by."""
-    s = x.reshape(-1, b).sum(1, keepdims=True) / b
+    s = np.abs(x).reshape(-1, b).sum(1, keepdims=True) / b
     return np.broadcast_to(s, (s.shape[0], b)).reshape(x.shape)
 
 

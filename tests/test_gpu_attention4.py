@@ -88,6 +88,32 @@ def test_parts_of_prompts(dim, hblock, share, dtype):
         run(s, new, share, dtype, causal, window)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("dim,hblock", [(64, 64), (40, 8), (128, 128), (80, 16), (192, 64), (136, 8)])
+def test_blocks_of_many_columns(dim, hblock, page, dtype):
+    """Rows enough for blocks of 32, 48 or 64 columns, of which there have to be 512."""
+    new = [130, 7, 0, 370, 1]
+    s = Sequences([130, 60, 33, 400, 65], 8, dim, hblock, page, dtype, seed=dim + page)
+    s.write()
+    for causal, window in ((True, 0), (True, 70), (False, 0)):
+        run(s, new, 8, dtype, causal, window)
+
+
+def test_blocks_of_many_columns_absent_pages_and_nan():
+    new = [400, 100]
+    s = Sequences([450, 100], 8, 128, 64, 16, torch.bfloat16, seed=5)
+    s.k[50, 3], s.v[450 + 20, 5, 1] = float("nan"), float("inf")
+    s.write()
+    table, there = s.table_np.copy(), [np.ones(450, bool), np.ones(100, bool)]
+    for i, p in ((0, 1), (0, 17), (1, 0), (1, 6)):
+        table[i, p] = [-1, s.cache.pages][p & 1]
+        there[i][16 * p:16 * p + 16] = False
+    q = queries(s, new, 64, torch.bfloat16)
+    y = hatq.hatq_attention4(s.cache, q.to(DEV), dev(table), s.lens, ends=dev(np.cumsum(new).astype(np.int32)))
+    compare(s, q, new, y, there=there)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_even_prompts(dtype):
     s = Sequences([96, 96, 96], 1, 64, 64, 16, dtype, seed=4)
