@@ -10,15 +10,17 @@ AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t
     const auto tiles = [&](int64_t by) {
         return ragged ? cols / by + (batch < rows ? batch : rows) : batch * ((cols / batch + by - 1) / by);
     };
-    // Wide blocks where they fill the card twice.  (us, 4 sequences of 4096, 4 heads of 128
-    // channels, bf16, wide and not: 128 columns each 66 and 31, 512 columns 70 and 63, 8192 columns
-    // 492 and 747; heads of 192 channels, 8192 columns 696 and 1239, of 64 303 and 463.  Of 256,
-    // whose two tiles do not fit the registers: 1846 and 1571.)
+    // Wide blocks for more than one narrow one's columns, where they fill the card twice.  (us, 8
+    // heads of 128 channels, bf16, wide and not: 64 sequences of 2048, 16 columns each 68 and
+    // 42, 24 73 and 77, 48 73 and 102, 64 125 and 131, 128 175 and 240; 4 heads, 4 sequences of
+    // 4096, too few blocks, 128 columns 66 and 31, 512 70 and 63; 8192 columns 492 and 747, heads
+    // of 192 channels 696 and 1239, of 64 303 and 463; of 256, whose two tiles do not fit the
+    // registers, 1846 and 1571.)
     p.cols = wide_cols(dim);
     p.tiles = tiles(p.cols);
     p.waves = 4;
     p.splits = 1;
-    if (p.cols > 16 && p.tiles * heads >= 512) return p;
+    if (p.cols > 16 && cols / batch > 16 && p.tiles * heads >= 512) return p;
     p.cols = 16;
     p.tiles = tiles(16);
     // Parts of a sequence while there is not a block for each CU, of at least two steps of 32
