@@ -279,48 +279,83 @@ __device__ float transformed4(const T *w, int d, int b) {
     return (float)acc;
 }
 
-// One wave a packed column and group.  W' = B w in fp64, rounded once to fp32; its scale
-// bf16(fl32(max |W'| / 7)), at least 2^-100, codes clamp(rne(fl32(W' / s)), -7, 7).
-template <typename T, bool CODES>
+// Floats: one wave a packed column and group.  W' = B w in fp64, rounded once to fp32; its
+// scale bf16(fl32(max |W'| / 7)), at least 2^-100, codes clamp(rne(fl32(W' / s)), -7, 7).
+template <typename T>
 __global__ void __launch_bounds__(kThreads) linear4_prepare_kernel(const Linear4PrepArgs a) {
-    const int groups = (a.k_stride + a.group - 1) / a.group;
+    const int groups = a.k_stride / a.group;
     const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
     if (unit >= (int64_t)a.cout_pad * groups) return;
     const int lane = threadIdx.x & 63, p = (int)(unit / groups), g = (int)(unit - (int64_t)p * groups);
-    const int ch = held_channel(a, p), given = (a.cin + a.group - 1) / a.group;
-    const int per = a.group >> 6;       // values a lane
-    // two codes a byte: channels d and d + 4, lanes 4 apart
+    const int ch = held_channel(a, p), per = a.group >> 6;   // values a lane
     float v[2] = {0.0f, 0.0f};
-    int q[2] = {0, 0};
     for (int i = 0; i < per; ++i) {
         const int d = g * a.group + i * 64 + lane;
-        if (ch < 0 || d >= a.cin) continue;
-        if (CODES) q[i] = max(-8, min(7, (int)a.codes[(int64_t)ch * a.cin + d]));
-        else v[i] = transformed4(static_cast<const T *>(a.w) + (int64_t)ch * a.cin, d, a.hblock);
+        if (ch >= 0 && d < a.cin) v[i] = transformed4(static_cast<const T *>(a.w) + (int64_t)ch * a.cin, d, a.hblock);
     }
-    uint16_t scale = 0;
-    if (CODES) {
-        if (ch >= 0 && g < given) scale = a.scale_in[(int64_t)ch * given + g];
-    } else if (ch >= 0) {
-        const float m = token_max(v);       // NaN kept
-        const bool fine = m < __builtin_inff();
-        const float s = fmaxf(__uint_as_float(bf16_pair(m / 7.0f, 0.0f) << 16), 0x1p-100f);
-        for (int i = 0; i < 2; ++i) q[i] = fine ? (int)__builtin_amdgcn_fmed3f(rintf(v[i] / s), -7.0f, 7.0f) : 0;
-        scale = fine ? (uint16_t)(__float_as_uint(s) >> 16) : (uint16_t)0x7fc0;
-    }
+    const float m = token_max(v);       // NaN kept
+    const bool fine = m < __builtin_inff();
+    const float s = fmaxf(__uint_as_float(bf16_pair(m / 7.0f, 0.0f) << 16), 0x1p-100f);
     for (int i = 0; i < per; ++i) {
-        const int d = g * a.group + i * 64 + lane;
-        const int other = __shfl_xor(q[i], 4, 64);
-        if (!(lane & 4) && d < a.k_stride) a.wpack[code_byte(a, p, d)] = (uint8_t)((q[i] & 15) | (other & 15) << 4);
+        const int q = fine ? (int)__builtin_amdgcn_fmed3f(rintf(v[i] / s), -7.0f, 7.0f) : 0;
+        // two codes a byte: input channels d and d + 4, lanes 4 apart
+        const int other = __shfl_xor(q, 4, 64);
+        if (!(lane & 4)) a.wpack[code_byte(a, p, g * a.group + i * 64 + lane)] = (uint8_t)((q & 15) | (other & 15) << 4);
     }
-    if (lane == 0) a.w_scale[scale_index(a, p, g)] = scale;
+    if (lane == 0)
+        a.w_scale[scale_index(a, p, g)] = ch < 0 ? (uint16_t)0 : fine ? (uint16_t)(__float_as_uint(s) >> 16) : (uint16_t)0x7fc0;
     if (lane == 0 && g == 0) a.bias[p] = ch >= 0 && a.bias_in ? a.bias_in[ch] : 0.0f;
 }
 
-template <typename T, bool CODES>
+// Codes that are there already: a lane the 16 packed bytes of its channel and chunk, a wave the
+// 1 KB of 16 channels by 128 input channels, and their scales.
+__global__ void __launch_bounds__(kThreads) linear4_pack_kernel(const Linear4PrepArgs a) {
+    const int tiles = a.k_stride >> 7, S = 128 / a.group;
+    const int64_t unit = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+    if (unit >= (int64_t)(a.cout_pad >> 4) * tiles) return;
+    const int lane = threadIdx.x & 63, p16 = (int)(unit / tiles), k = (int)(unit - (int64_t)p16 * tiles);
+    const int ch = held_channel(a, p16 * 16 + (lane & 15)), given = (a.cin + a.group - 1) / a.group;
+    const bool whole = (reinterpret_cast<uintptr_t>(a.codes) & 15) == 0 && a.cin % 16 == 0;
+    uint32_t out[4];
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+        const int d = k * 128 + step * 64 + (lane >> 4) * 16;
+        const int8_t *from = a.codes + (int64_t)ch * a.cin + d;
+        int8_t q[16] = {};
+        if (ch >= 0 && d < a.cin) {
+            if (whole) {
+                *reinterpret_cast<v4u *>(q) = *reinterpret_cast<const v4u *>(from);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (d + j < a.cin) q[j] = from[j];
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int code = max(-8, min(7, (int)q[8 * w + j]));
+                word |= (uint32_t)(code & 15) << ((j & 3) * 8 + (j & 4));
+            }
+            out[step * 2 + w] = word;
+        }
+    }
+    *reinterpret_cast<v4u *>(a.wpack + unit * 1024 + lane * 16) = v4u{out[0], out[1], out[2], out[3]};
+    if (lane < 16 * S) {
+        // [4][S][4 channels]
+        const int c = (lane / (4 * S)) * 4 + (lane & 3), g = k * S + (lane >> 2) % S;
+        const int own = held_channel(a, p16 * 16 + c);
+        a.w_scale[unit * (16 * S) + lane] = own >= 0 && g < given ? a.scale_in[(int64_t)own * given + g] : (uint16_t)0;
+    }
+    if (k == 0 && lane < 16) a.bias[p16 * 16 + lane] = ch >= 0 && a.bias_in ? a.bias_in[ch] : 0.0f;
+}
+
+template <typename T>
 void prepare(const Linear4PrepArgs &a, hipStream_t st) {
-    const int64_t units = (int64_t)a.cout_pad * ((a.k_stride + a.group - 1) / a.group);
-    linear4_prepare_kernel<T, CODES><<<grid_of((units + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
+    const int64_t units = (int64_t)a.cout_pad * (a.k_stride / a.group);
+    linear4_prepare_kernel<T><<<grid_of((units + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
 }
 
 template <typename T, int G, int S>
@@ -363,10 +398,16 @@ bool linear4_takes_tokens(int32_t rows, int32_t k_stride) {
 }
 
 hipError_t launch_linear4_prepare(const Linear4PrepArgs &a, hipStream_t st) {
-    if (a.codes) prepare<float, true>(a, st);
-    else if (a.w_type == kBf16) prepare<bf16_t, false>(a, st);
-    else if (a.w_type == kF16) prepare<_Float16, false>(a, st);
-    else prepare<float, false>(a, st);
+    if (a.codes) {
+        const int64_t units = (int64_t)(a.cout_pad >> 4) * (a.k_stride >> 7);
+        linear4_pack_kernel<<<grid_of((units + kThreads / 64 - 1) / (kThreads / 64)), kThreads, 0, st>>>(a);
+    } else if (a.w_type == kBf16) {
+        prepare<bf16_t>(a, st);
+    } else if (a.w_type == kF16) {
+        prepare<_Float16>(a, st);
+    } else {
+        prepare<float>(a, st);
+    }
     return hipGetLastError();
 }
 
