@@ -4,6 +4,7 @@
 ``synth``     -- seeded synthetic inputs (no method arithmetic)
 ``workloads`` -- the layer shapes and input recipes
 ``experts``   -- a feed-forward block of gated experts on the linear layers over tokens
+``decoder``   -- attention over a 4-bit cache and a gated feed-forward block on the linear layers
 ``build``     -- hipcc build of libhatq.so for gfx950
 """
 from . import synth, workloads  # noqa: F401
