@@ -11,7 +11,7 @@
 // First product: the codes in float16, exact, against the query in two float16 halves, 22
 // bits (many rows of bf16: one half, 11 bits), after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
-// kept relative to the largest of w s_v (not of w), so the float16 range holds whatever the
+// kept relative to the largest of w s_v (not of w), or to one up to 2^8 smaller, so the float16 range holds whatever the
 // scales are (2^-100 to 2^100): off by 2^-11 of each weight or 2^-25 of the largest.  For
 // float16 and float32 results NP = 2 halves carry 22 bits of it.
 #include "cache4_device.h"
@@ -50,6 +50,14 @@ __device__ __forceinline__ float chunks_sum(float v) {
     const uint32_t w = __float_as_uint(v);
     const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// a b and c d, exact products rounded once, as two float16.  (Written out: the compiler rounds
+// each to float32, or packs the halves in an instruction of its own.)
+__device__ __forceinline__ uint32_t product_pair(float a, float b, float c, float d) {
+    uint32_t r;
+    asm("v_fma_mixlo_f16 %0, %1, %2, 0\n\tv_fma_mixhi_f16 %0, %3, %4, 0" : "=&v"(r) : "v"(a), "v"(b), "v"(c), "v"(d));
+    return r;
 }
 
 // ---- which rows a tile has --------------------------------------------------------
@@ -306,7 +314,10 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
             }
     }
     load_scales<NB, HALF>(next, mine, 0, s.key_scale);
-    // 128 (127 + log2) of the largest scale of a value, to 12 from below: its bf16 bits
+    // log2 of the largest scale of a value, to 0.09 from below, from its bf16 bits; one column
+    // tile takes it as they are, 128 (127 + log2), and many spare the registers of 128 times
+    // their steps, which spill
+    constexpr bool kBits = NQ == 1;
     float lv[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -319,8 +330,9 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
         v2s most = pair(0);
 #pragma unroll
         for (int b = 1; b < NB; ++b) most = __builtin_elementwise_max(most, pair(b));
-        lv[2 * i] = (float)most[0];
-        lv[2 * i + 1] = (float)most[1];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            lv[2 * i + k] = kBits ? (float)most[k] : __builtin_fmaf((float)most[k], 0x1p-7f, -127.0f);
     }
     uint32_t seen[NQ];
 #pragma unroll
@@ -334,11 +346,14 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float x = __builtin_fmaf(t[n][j], q[n].step * 128.0f, lv[j]);
+            const float x = __builtin_fmaf(t[n][j], kBits ? q[n].step * 128.0f : q[n].step, lv[j]);
             most = __builtin_elementwise_maximum(most, !EDGE || (seen[n] >> j & 1) ? x : -__builtin_inff());
         }
-        most = __builtin_fmaf(chunks_max(most), 0x1p-7f, -127.0f);
-        if (__any(most > o.m)) {
+        most = chunks_max(most);
+        if (kBits) most = __builtin_fmaf(most, 0x1p-7f, -127.0f);
+        // (A weight may be up to 2^8 of the unit before the unit follows: float16 has room for
+        // that, and most columns' largest grows by less after its first step.)
+        if (__any(most > o.m + 8.0f)) {
             const float m = most > o.m ? most : o.m, down = __builtin_amdgcn_exp2f(o.m - m);
             o.m = m;
             o.l *= down;
@@ -358,17 +373,26 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
     for (int b = 0; b < NB; ++b) {
         v8h weight[NQ][NP];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
+        for (int n = 0; n < NQ; ++n) {
+            // (a hidden position's scale may be anything)
+            const auto scale = [&](int j) { return !EDGE || (seen[n] >> j & 1) ? scale_of(s.value_scale[b], j) : 0.0f; };
+            if constexpr (NP == 1 && NQ == 1) {
+                uint32_t pair[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float w = t[n][j] * scale_of(s.value_scale[b], j);
-                if (EDGE) w = seen[n] >> j & 1 ? w : 0.0f;      // (a hidden position's scale may be anything)
-                // (one rounded product for both halves: else one of them is made by v_fma_mixlo, which
-                // rounds the exact product, and a tie goes up in one and down in the other)
-                if (NP == 2) asm("" : "+v"(w));
-                weight[n][0][j] = (_Float16)w;
-                if (NP == 2) weight[n][NP - 1][j] = (_Float16)(w - (float)weight[n][0][j]);
+                for (int j = 0; j < 8; j += 2) pair[j >> 1] = product_pair(t[n][j], scale(j), t[n][j + 1], scale(j + 1));
+                weight[n][0] = __builtin_bit_cast(v8h, v4u{pair[0], pair[1], pair[2], pair[3]});
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float w = t[n][j] * scale(j);
+                    // (one rounded product for both halves: else one of them is made by v_fma_mixlo, which
+                    // rounds the exact product, and a tie goes up in one and down in the other)
+                    if (NP == 2) asm("" : "+v"(w));
+                    weight[n][0][j] = (_Float16)w;
+                    if (NP == 2) weight[n][NP - 1][j] = (_Float16)(w - (float)weight[n][0][j]);
+                }
             }
+        }
         v2h code[4][4];     // [word: positions][channel of the run]
 #pragma unroll
         for (int i = 0; i < 4; ++i) unpack8<false>(s.value[b][i], code[i]);
@@ -546,9 +570,9 @@ attention4_kernel(const AttentionArgs a) {
     Walk<NB, HALF> walk(a, t.seq, head, from + 32 * (begin + wave), end == steps ? to : from + 32 * end, 32 * waves);
     Query q[NQ];
     Sums<NB> s[NQ];
-    // (sixteen columns a wave: made by all, it would take as long as two steps)
+    // (sixteen columns a wave, NQ waves at least: made by all, it would take as long as two steps)
     char *const query = lds;
-    for (int n = wave; n < NQ; n += waves) make_query<NB>(a, t, head, 16 * n, query + n * kQueryBytes<NB>);
+    if (wave < NQ) make_query<NB>(a, t, head, 16 * wave, query + wave * kQueryBytes<NB>);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) see<NB>(a, t, length, 16 * n, q[n]);
     __syncthreads();
