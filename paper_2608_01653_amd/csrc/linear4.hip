@@ -177,6 +177,82 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_token_kernel(const Linear
     finish<G>(a, sum, scale[mine], (lane & 15) < rows ? lane & 15 : rows, c16, lane);
 }
 
+// ---- more tokens of a short contraction, floats in ------------------------------------------
+// A contraction of at most 2048: a block quantizes 16 rows, a wave a row at a time (both of a
+// wave's rows loaded at once), into LDS, and then each wave takes groups of 16 channels over
+// the whole contraction.  blockIdx.y: `per` of the groups, a multiple of the waves.  One launch
+// instead of two; bound by latency.
+template <typename T, int G, int S, int CH>
+__global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear4Args a, const TokenArgs x, int per) {
+    constexpr int U = 4, ROWS = 16, TURNS = ROWS / kWaves;
+    __shared__ __attribute__((aligned(16))) int8_t codes[ROWS * (512 * CH + 16)];
+    __shared__ float scale[ROWS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row0 = blockIdx.x * ROWS, rows = min(a.rows - row0, ROWS);
+    const int tiles = a.k_stride >> 7, pitch = a.k_stride + 16;
+    const int end = min(((int)blockIdx.y + 1) * per, (a.cout + 15) / 16);
+    int c16 = blockIdx.y * per + wave;
+
+    TokenRow<T> token[TURNS];
+    Raw8<T> raw[TURNS][CH] = {};
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) token[i] = token_row<T>(x, row0 + min(wave + kWaves * i, rows - 1));
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) load_chunks<T, CH, 64>(token[i].p, token[i].n, lane, raw[i]);
+
+    Tile<S> t[U][G];
+    auto weights = [&](int c, int k0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int64_t k = (int64_t)(c * G + g) * tiles + min(k0 + u, tiles - 1);
+                load_tile<S>(a.wp + k * 1024, a.w_scale + k * (16 * S), lane, t[u][g]);
+            }
+    };
+    if (c16 < end) weights(c16, 0);
+    __builtin_amdgcn_sched_barrier(0);   // the first weights are under way
+
+#pragma unroll
+    for (int i = 0; i < TURNS; ++i) {
+        const int row = wave + kWaves * i;
+        if (row >= rows) break;
+        float v[8 * CH];
+        chunk_values<T, CH, 64>(token[i].p, token[i].n, lane, raw[i], v);
+        const float sigma = token_butterfly(v, lane, x.log_b);
+        const float s = token_scale(token_max(v));
+        if (lane == 0) scale[row] = s * a.inv_b;
+        store_chunks<CH, 64>(codes + row * pitch, a.k_stride, lane, v, sigma, s);
+    }
+    __syncthreads();
+
+    const int mine = min(lane & 15, rows - 1);
+    const int8_t *from = codes + mine * pitch + (lane >> 4) * 16;
+    while (c16 < end) {
+        v4f acc[G][1];
+#pragma unroll
+        for (int g = 0; g < G; ++g) acc[g][0] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int k0 = 0; k0 < tiles; k0 += U) {
+            if (k0) weights(c16, k0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (k0 + u >= tiles) break;
+                const v4i *c = reinterpret_cast<const v4i *>(from + (k0 + u) * 128);
+                const v4i fx[1][2] = {{c[0], c[4]}};
+#pragma unroll
+                for (int g = 0; g < G; ++g) multiply<S, 1>(t[u][g], fx, acc[g]);
+            }
+        }
+        const int c = c16;
+        c16 += kWaves;
+        if (c16 < end) weights(c16, 0);   // the next group's, under way over the stores
+        v4f sum[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) sum[g] = acc[g][0];
+        finish<G>(a, sum, scale[mine], (lane & 15) < rows ? row0 + (lane & 15) : a.rows, c, lane);
+    }
+}
+
 // ---- codes from memory ------------------------------------------------------------------
 // Waves of a block take 16 channels by 16 MT rows, `wk` of them the tiles of the contraction
 // in turn (they add up in LDS), the others channels further on.
@@ -360,6 +436,17 @@ void prepare(const Linear4PrepArgs &a, hipStream_t st) {
 
 template <typename T, int G, int S>
 void token(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
+    if (a.rows > HATQ_TOKEN_ROWS || (int64_t)a.rows * a.k_stride > HATQ_TOKEN_CODES) {
+        // column ranges, each of which quantizes the rows again: up to 512 blocks
+        const int groups = (a.cout + 15) / 16, blocks = (a.rows + 15) / 16;
+        const int most = blocks < 512 ? 512 / blocks : 1, ranges = (groups + 7) / 8 < most ? (groups + 7) / 8 : most;
+        const int per = ((groups + ranges - 1) / ranges + 7) / 8 * 8;
+        const dim3 grid(blocks, (groups + per - 1) / per);
+        if (a.k_stride <= 512) linear4_small_kernel<T, G, S, 1><<<grid, 512, 0, st>>>(a, x, per);
+        else if (a.k_stride <= 1024) linear4_small_kernel<T, G, S, 2><<<grid, 512, 0, st>>>(a, x, per);
+        else linear4_small_kernel<T, G, S, 4><<<grid, 512, 0, st>>>(a, x, per);
+        return;
+    }
     const int grid = (a.cout + 15) / 16;
     const size_t bytes = kWaves * G * 1024 + 128 + (size_t)a.rows * (a.k_stride + 16);
     if (a.k_stride <= 4096) linear4_token_kernel<T, G, S, 1><<<grid, 512, bytes, st>>>(a, x);
@@ -393,8 +480,12 @@ void stream(const Linear4Args &a, hipStream_t st) {
 
 }  // namespace
 
+// (us in a graph, two kernels and one, bf16, 128 input channels a scale: 17 rows, 512 -> 512 6.3
+// and 4.7; 77, 1000 -> 1001 9.0 and 6.7; 128, 1024 -> 16384 22.3 and 15.0; 128, 2048 -> 8192 22.6
+// and 22.0; 4096, 2048 -> 4096 254 and 108; behind only for few groups of a long contraction,
+// 16, 2048 -> 4096 7.2 and 8.6.)
 bool linear4_takes_tokens(int32_t rows, int32_t k_stride) {
-    return rows <= HATQ_TOKEN_ROWS && (int64_t)rows * k_stride <= HATQ_TOKEN_CODES;
+    return k_stride <= 2048 || (rows <= HATQ_TOKEN_ROWS && (int64_t)rows * k_stride <= HATQ_TOKEN_CODES);
 }
 
 hipError_t launch_linear4_prepare(const Linear4PrepArgs &a, hipStream_t st) {

@@ -1109,11 +1109,10 @@ def hatq_linear4_forward(lin: PreparedLinear4, x: torch.Tensor, out_dtype: Optio
     n, _, xs, xt = _rows(x, "x", lin.cin)
     y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
     _here(lin.device, x, y, ws)
-    if n <= HATQ_TOKEN_ROWS and n * lin.k_stride <= HATQ_TOKEN_CODES:
-        wp, wn = None, 0                # a few tokens need no workspace
-    else:
+    if ws is None and not (lin.k_stride <= 2048 or (n <= HATQ_TOKEN_ROWS and n * lin.k_stride <= HATQ_TOKEN_CODES)):
         ws = _linear_ws(lin, n, ws, x)
-        wp, wn = ws.data_ptr(), ws.numel()
+    _need(ws, "ws", torch.int8, 0, optional=True)
+    wp, wn = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
     _check(load().hatq_linear4_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, wp, wn, _stream()),
            "hatq_linear4_forward")
     return y

@@ -25,7 +25,7 @@ def L():
 
 
 def weights(**over):
-    w = hatq.Linear4Weights(1000, 100, 0, 8, 64, 1024, 112, P, P, P)
+    w = hatq.Linear4Weights(4000, 100, 0, 8, 64, 4096, 112, P, P, P)
     for k, v in over.items():
         setattr(w, k, v)
     return w
@@ -44,13 +44,15 @@ def test_bytes(L):
                 (64, 16, 0, 1, 32), (64, 16, 0, 1, 0), (65537, 16, 0, 1, 64), (64, 65537, 0, 1, 64), (64, 32769, 1, 1, 64), (192, 16, 0, 192, 64)]:
         assert L.hatq_linear4_weights_bytes(*bad) == 0, bad
     w = weights()
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 16) == 0
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 17) == 17 * 1024 + 256
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 2 ** 24) == (1024 << 24) + (4 << 24)
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 4) == 0
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 5) == 5 * 4096 + 256
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 2 ** 24) == (4096 << 24) + (4 << 24)
+    short = weights(cin=2000, k_stride=2048)
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(short), 2 ** 24) == 0
     for rows in (0, -1, 2 ** 24 + 1):
         assert L.hatq_linear4_ws_bytes(ctypes.byref(w), rows) == 0
     assert L.hatq_linear4_ws_bytes(None, 17) == 0
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(weights(k_stride=1008)), 17) == 0
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(weights(k_stride=4032)), 17) == 0
 
 
 @cpu_only
@@ -74,15 +76,15 @@ def test_weights_refusals(L):
 
 @cpu_only
 def test_forward_refusals(L):
-    def call(w=None, x=P, xt=0, rows=40, xs=1000, y=P, yt=0, ys=100, ws=P, size=2 ** 30):
+    def call(w=None, x=P, xt=0, rows=40, xs=4000, y=P, yt=0, ys=100, ws=P, size=2 ** 30):
         return L.hatq_linear4_forward(ctypes.byref(w or weights()), x, xt, rows, xs, y, yt, ys, ws, size, None)
     assert call(rows=0) == OK
-    assert L.hatq_linear4_forward(None, P, 0, 40, 1000, P, 0, 100, P, 2 ** 30, None) == EINVAL
-    for kw in (dict(x=None), dict(x=P + 1), dict(xt=3), dict(xs=999), dict(xs=2 ** 60), dict(y=None), dict(y=P + 3), dict(yt=-1), dict(ys=99),
+    assert L.hatq_linear4_forward(None, P, 0, 40, 4000, P, 0, 100, P, 2 ** 30, None) == EINVAL
+    for kw in (dict(x=None), dict(x=P + 1), dict(xt=3), dict(xs=3999), dict(xs=2 ** 60), dict(y=None), dict(y=P + 3), dict(yt=-1), dict(ys=99),
                dict(ws=None), dict(ws=P + 16), dict(rows=-1)):
         assert call(**kw) == EINVAL, kw
-    for over in (dict(k_stride=1000), dict(cout_pad=100), dict(wpack=None), dict(wpack=P + 8), dict(w_scale=P + 2), dict(bias=None), dict(group=256),
+    for over in (dict(k_stride=4000), dict(cout_pad=100), dict(wpack=None), dict(wpack=P + 8), dict(w_scale=P + 2), dict(bias=None), dict(group=256),
                  dict(gated=1)):
         assert call(w=weights(**over)) == EINVAL, over
-    assert call(size=40 * 1024 + 255) == EWORKSPACE
+    assert call(size=40 * 4096 + 255) == EWORKSPACE
     assert call(rows=2 ** 24 + 1) == EUNSUPPORTED
