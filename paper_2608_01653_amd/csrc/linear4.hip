@@ -254,22 +254,24 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear
 }
 
 // ---- codes from memory ------------------------------------------------------------------
-// Waves of a block take 16 channels by 16 MT rows, `wk` of them the tiles of the contraction
-// in turn (they add up in LDS), the others channels further on.
-template <int G, int S, int MT>
+// Waves of a block take G groups of 16 channels by 16 MT rows, `wk` of them the tiles of the
+// contraction in turn (they add up in LDS), the others channels further on.  The groups are a
+// gated layer's gates and values, or G adjacent ones, which share the rows' codes: of those a
+// wave reads 2 KB for 1 KB of weights and 16 rows, and of long calls they are what the L2s give.
+template <int G, int S, int MT, bool GATED>
 __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linear4Args a, int wk) {
-    constexpr int U = MT == 1 ? 4 : 2;
+    constexpr int U = MT * G >= 16 ? 1 : MT == 1 ? 4 : 2;   // tiles loaded at once
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     v4f(*part)[G][MT][64] = reinterpret_cast<v4f(*)[G][MT][64]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_k = wave & (wk - 1);
-    const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16;
+    const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16, sets = GATED ? groups : (groups + G - 1) / G;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int row0 = (int)(block % row_tiles) * (16 * MT);
     const int64_t c16_ = block / row_tiles * (kWaves / wk) + wave / wk;
-    const int c16 = (int)(c16_ < groups ? c16_ : groups - 1);
+    const int c16 = (int)(c16_ < sets ? c16_ : sets - 1);
+    // (past the last group: the last one again, not stored)
+    const auto group = [&](int g) { return GATED ? c16 * G + g : min(c16 * G + g, groups - 1); };
     const int tiles = a.k_stride >> 7;
-    const uint8_t *w = a.wp + (int64_t)c16 * G * tiles * 1024;
-    const uint16_t *ws = a.w_scale + (int64_t)c16 * G * tiles * (16 * S);
     const int8_t *from[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -287,7 +289,8 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linea
             const int k = min(k0 + wk * u, tiles - 1);
 #pragma unroll
             for (int g = 0; g < G; ++g)
-                load_tile<S>(w + (int64_t)(g * tiles + k) * 1024, ws + (int64_t)(g * tiles + k) * (16 * S), lane, t[u][g]);
+                load_tile<S>(a.wp + ((int64_t)group(g) * tiles + k) * 1024, a.w_scale + ((int64_t)group(g) * tiles + k) * (16 * S), lane,
+                             t[u][g]);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const v4i *c = reinterpret_cast<const v4i *>(from[m] + k * 128);
@@ -315,14 +318,21 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linea
 #pragma unroll
                 for (int m = 0; m < MT; ++m) acc[g][m] += part[wave + k][g][m][lane];
     }
-    if (c16_ >= groups) return;
+    if (c16_ >= sets) return;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int row = row0 + 16 * m + (lane & 15);
-        v4f sum[G];
+        const float s = a.sx[min(row, a.rows - 1)] * a.inv_b;
+        if constexpr (GATED) {
+            const v4f sum[2] = {acc[0][m], acc[G - 1][m]};
+            finish<2>(a, sum, s, row, c16, lane);
+        } else {
 #pragma unroll
-        for (int g = 0; g < G; ++g) sum[g] = acc[g][m];
-        finish<G>(a, sum, a.sx[min(row, a.rows - 1)] * a.inv_b, row, c16, lane);
+            for (int g = 0; g < G; ++g) {
+                const v4f sum[1] = {acc[g][m]};
+                if (c16 * G + g < groups) finish<1>(a, sum, s, row, c16 * G + g, lane);
+            }
+        }
     }
 }
 
@@ -460,22 +470,35 @@ void token(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
     else token<_Float16, G, S>(a, x, st);
 }
 
-template <int G, int S, int MT>
+template <int G, int S, int MT, bool GATED>
 void stream(const Linear4Args &a, hipStream_t st) {
-    const int64_t groups = (a.cout + 15) / 16, row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
+    const int64_t groups = (a.cout + 15) / 16, sets = GATED ? groups : (groups + G - 1) / G;
+    const int64_t row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
     const int tiles = a.k_stride >> 7;
-    // waves on one group while the groups do not fill the card, and while each has a tile
+    // waves on one set of groups while the sets do not fill the card, and while each has a tile
     int wk = 1;
-    while (wk < kWaves && 2 * wk <= tiles && groups * row_tiles * wk < 4096) wk *= 2;
+    while (wk < kWaves && 2 * wk <= tiles && sets * row_tiles * wk < 4096) wk *= 2;
     const int cols = kWaves / wk;
     const size_t bytes = wk > 1 ? (size_t)kWaves * G * MT * 1024 : 0;
-    linear4_stream_kernel<G, S, MT><<<grid_of((groups + cols - 1) / cols * row_tiles), 512, bytes, st>>>(a, wk);
+    linear4_stream_kernel<G, S, MT, GATED><<<grid_of((sets + cols - 1) / cols * row_tiles), 512, bytes, st>>>(a, wk);
 }
-template <int G, int S>
+// Adjacent groups a wave: as many as leave the card sets enough, 512 of 4 groups or 256 of 2.
+// In us at 1, 2 and 4 groups: 64 rows of 4096 -> 4096 (128 sets of 2) 14.9, 17.3, 21.0; 128 rows
+// (256 of 2) 22.6, 17.7, 22.4; 128 of 4096 -> 16384 (512 of 4) 68.1, 42.9, 39.9; 2048 rows of
+// 4096 -> 4096: 251, 143, 94.7.
+template <int S, int MT>
 void stream(const Linear4Args &a, hipStream_t st) {
-    if (a.rows <= 16) stream<G, S, 1>(a, st);
-    else if (a.rows <= 32) stream<G, S, 2>(a, st);
-    else stream<G, S, 4>(a, st);
+    const int64_t groups = (a.cout + 15) / 16, row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
+    if (a.gated) stream<2, S, MT, true>(a, st);
+    else if ((groups + 3) / 4 * row_tiles >= 512) stream<4, S, MT, false>(a, st);
+    else if ((groups + 1) / 2 * row_tiles >= 256) stream<2, S, MT, false>(a, st);
+    else stream<1, S, MT, false>(a, st);
+}
+template <int S>
+void stream(const Linear4Args &a, hipStream_t st) {
+    if (a.rows <= 16) stream<S, 1>(a, st);
+    else if (a.rows <= 32) stream<S, 2>(a, st);
+    else stream<S, 4>(a, st);
 }
 
 }  // namespace
@@ -509,8 +532,7 @@ hipError_t launch_linear4_tokens(const Linear4Args &a, const TokenArgs &x, hipSt
 }
 
 hipError_t launch_linear4(const Linear4Args &a, hipStream_t st) {
-    if (a.gated) a.group == 64 ? stream<2, 2>(a, st) : stream<2, 1>(a, st);
-    else a.group == 64 ? stream<1, 2>(a, st) : stream<1, 1>(a, st);
+    a.group == 64 ? stream<2>(a, st) : stream<1>(a, st);
     return hipGetLastError();
 }
 

@@ -89,7 +89,7 @@ def compare(x, y, codes, scale, bias, hblock, group, gated, what=""):
 @pytest.mark.parametrize("group", [64, 128])
 @pytest.mark.parametrize("rows,cin,cout,hblock", [(1, 512, 64, 128), (1, 4096, 16, 64), (3, 64, 17, 64), (16, 1000, 33, 8), (1, 8192, 40, 1),
                                                   (2, 8192, 16, 128), (1, 16384, 18, 128), (1, 1, 1, 1), (5, 65, 15, 1), (16, 1024, 100, 32),
-                                                  (17, 512, 50, 64), (6, 4096, 70, 128), (33, 129, 31, 1), (64, 640, 48, 128), (65, 200, 9, 8),
+                                                  (17, 512, 50, 64), (6, 4096, 70, 128), (33, 129, 31, 1), (64, 640, 48, 128), (65, 200, 9, 8), (9, 2176, 33, 128), (20, 2200, 97, 8), (40, 2304, 65, 64),
                                                   (130, 384, 257, 128), (3, 8320, 20, 64), (300, 100, 40, 4), (1, 20480, 24, 64)])
 def test_against_64_bits(rows, cin, cout, hblock, group, gated, dtype):
     rng = np.random.default_rng(rows * cin + cout)
@@ -164,17 +164,17 @@ def test_not_finite(rows):
 
 
 @pytest.mark.parametrize("dtype,out", [(torch.bfloat16, torch.float32), (torch.float32, torch.float16), (torch.float16, torch.bfloat16)])
-@pytest.mark.parametrize("rows", [1, 5, 70])
-def test_strides_and_types(rows, dtype, out):
+@pytest.mark.parametrize("rows,cin", [(1, 200), (5, 200), (70, 200), (9, 2056), (40, 2200)])
+def test_strides_and_types(rows, cin, dtype, out):
     rng = np.random.default_rng(rows)
-    codes, scale, bias = layer(rng, 37, 200, 128, True)
+    codes, scale, bias = layer(rng, 37, cin, 128, True)
     lin = packed(codes, scale, bias, 8, False)
-    x = tokens(rng, rows, 200, dtype)
-    wide = torch.zeros((rows, 211), dtype=dtype, device=DEV)
-    wide[:, 7:207] = x.to(DEV)
+    x = tokens(rng, rows, cin, dtype)
+    wide = torch.zeros((rows, cin + 11), dtype=dtype, device=DEV)
+    wide[:, 7:7 + cin] = x.to(DEV)
     y = torch.full((rows, 45), 3.0, dtype=out, device=DEV)
     ws = Guarded((max(256, hatq.hatq_linear4_ws_bytes(lin, rows)),), torch.int8)
-    hatq.hatq_linear4_forward(lin, wide[:, 7:207], y=y[:, 5:42], ws=ws.view)
+    hatq.hatq_linear4_forward(lin, wide[:, 7:7 + cin], y=y[:, 5:42], ws=ws.view)
     ws.check("workspace")
     compare(x, y[:, 5:42], codes, scale, bias, 8, 128, False)
     assert bool((y[:, :5] == 3).all()) and bool((y[:, 42:] == 3).all())
@@ -184,8 +184,10 @@ def test_captured_and_replayed():
     rng = np.random.default_rng(5)
     codes, scale, bias = layer(rng, 64, 512, 64, True)
     lin = packed(codes, scale, bias, 64, True)
-    for rows in (2, 40):
-        x = torch.zeros((rows, 512), dtype=torch.bfloat16, device=DEV)
+    long = packed(*layer(rng, 64, 2240, 64, True), 64, True)
+    for rows, lin in ((2, lin), (40, lin), (40, long)):
+        cin = lin.cin
+        x = torch.zeros((rows, cin), dtype=torch.bfloat16, device=DEV)
         y = torch.zeros((rows, 32), dtype=torch.bfloat16, device=DEV)
         ws = torch.empty(max(256, hatq.hatq_linear4_ws_bytes(lin, rows)), dtype=torch.int8, device=DEV)
         hatq.hatq_linear4_forward(lin, x, y=y, ws=ws)
@@ -194,7 +196,7 @@ def test_captured_and_replayed():
         with torch.cuda.graph(graph):
             hatq.hatq_linear4_forward(lin, x, y=y, ws=ws)
         for _ in range(3):
-            x.copy_(torch.randn((rows, 512)))
+            x.copy_(torch.randn((rows, cin)))
             graph.replay()
             eager = hatq.hatq_linear4_forward(lin, x)
             torch.cuda.synchronize()
@@ -215,7 +217,8 @@ def test_refusals():
     bad(hatq.hatq_linear4_forward, lin, x.cpu())
     bad(hatq.hatq_linear4_forward, lin, x, y=torch.zeros((20, 33), device=DEV))
     bad(hatq.hatq_linear4_forward, lin, x, y=torch.zeros((1, 32), device=DEV).expand(20, 32))
-    bad(hatq.hatq_linear4_forward, lin, x, ws=torch.empty(256, dtype=torch.int8, device=DEV))
+    long = packed(*layer(rng, 32, 2176, 128, False), 64, False)
+    bad(hatq.hatq_linear4_forward, long, torch.zeros((20, 2176), device=DEV), ws=torch.empty(256, dtype=torch.int8, device=DEV))
     bad(hatq.hatq_linear4_forward, lin, x, out_dtype=torch.int8)
     s = dev(scale).to(torch.bfloat16)
     bad(hatq.hatq_pack_linear4, dev(codes).float(), s)
@@ -229,3 +232,16 @@ def test_refusals():
     bad(hatq.hatq_prepare_linear4, x, group=32)
     bad(hatq.hatq_prepare_linear4, x, hblock=192)
     assert hatq.hatq_linear4_forward(lin, x[:0]).shape == (0, 32)
+
+
+@pytest.mark.parametrize("rows,gated", [(12, False), (30, False), (100, False), (12, True), (100, True)])
+def test_many_groups(rows, gated):
+    """Channels enough for waves that take several groups of them, and one group past the last
+    whole set; the reference in float64 on the GPU."""
+    rng = np.random.default_rng(rows)
+    cin, cout, group = 2176, 16 * 1025 - 3, 64
+    held = cout * (2 if gated else 1)
+    codes, scale, bias = layer(rng, held, cin, group, True)
+    x = tokens(rng, rows, cin, torch.float32)
+    y = hatq.hatq_linear4_forward(packed(codes, scale, bias, 64, gated), x.to(DEV))
+    compare(x, y, codes, scale, bias, 64, group, gated)
