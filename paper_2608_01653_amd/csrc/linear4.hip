@@ -446,7 +446,11 @@ void prepare(const Linear4PrepArgs &a, hipStream_t st) {
 
 template <typename T, int G, int S>
 void token(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
-    if (a.rows > HATQ_TOKEN_ROWS || (int64_t)a.rows * a.k_stride > HATQ_TOKEN_CODES) {
+    // A row or a few of a contraction that its split over 8 waves shortens go to the kernel of a
+    // block a group (us, that one and the other: 1 row, 1024 -> 4096 3.9 and 4.8; 2 rows, 2048 ->
+    // 4096 4.9 and 6.5; 4 rows, 2048 -> 4096 6.3 and 6.5; 16 rows, 1024 -> 4096 14.6 and 6.3; 1 row,
+    // 1024 -> 16384 6.5 and 5.0).
+    if (a.k_stride <= 512 || (a.k_stride <= 2048 && (a.rows >= 4 || a.cout > 8192))) {
         // column ranges, each of which quantizes the rows again: up to 512 blocks
         const int groups = (a.cout + 15) / 16, blocks = (a.rows + 15) / 16;
         const int most = blocks < 512 ? 512 / blocks : 1, ranges = (groups + 7) / 8 < most ? (groups + 7) / 8 : most;
@@ -507,8 +511,12 @@ void stream(const Linear4Args &a, hipStream_t st) {
 // and 4.7; 77, 1000 -> 1001 9.0 and 6.7; 128, 1024 -> 16384 22.3 and 15.0; 128, 2048 -> 8192 22.6
 // and 22.0; 4096, 2048 -> 4096 254 and 108; behind only for few groups of a long contraction,
 // 16, 2048 -> 4096 7.2 and 8.6.)
-bool linear4_takes_tokens(int32_t rows, int32_t k_stride) {
-    return k_stride <= 2048 || (rows <= HATQ_TOKEN_ROWS && (int64_t)rows * k_stride <= HATQ_TOKEN_CODES);
+// Longer ones: where every block quantizes all rows, up to 16 K codes, but 8 K of more than 512
+// blocks (so and from memory: 4 rows, 4096 -> 4096 6.9 and 7.7; 1 row, 16384 -> 4096 11.2 and
+// 13.4; 1 row, 8192 -> 16384 16.1 and 16.1; 4 rows, 4096 -> 16384 13.8 and 10.9; 1 row, 16384 ->
+// 16384 38.9 and 26.3).
+bool linear4_takes_tokens(int32_t rows, int32_t cout, int32_t k_stride) {
+    return k_stride <= 2048 || (int64_t)rows * k_stride <= (cout <= 8192 ? HATQ_TOKEN_CODES : HATQ_TOKEN_CODES / 2);
 }
 
 hipError_t launch_linear4_prepare(const Linear4PrepArgs &a, hipStream_t st) {

@@ -1109,7 +1109,7 @@ def hatq_linear4_forward(lin: PreparedLinear4, x: torch.Tensor, out_dtype: Optio
     n, _, xs, xt = _rows(x, "x", lin.cin)
     y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
     _here(lin.device, x, y, ws)
-    if ws is None and not (lin.k_stride <= 2048 or (n <= HATQ_TOKEN_ROWS and n * lin.k_stride <= HATQ_TOKEN_CODES)):
+    if ws is None and lin.k_stride > 2048 and n * lin.k_stride > HATQ_TOKEN_CODES >> (lin.cout > 8192):
         ws = _linear_ws(lin, n, ws, x)
     _need(ws, "ws", torch.int8, 0, optional=True)
     wp, wn = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())

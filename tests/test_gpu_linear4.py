@@ -234,6 +234,18 @@ def test_refusals():
     assert hatq.hatq_linear4_forward(lin, x[:0]).shape == (0, 32)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,cin,cout", [(1, 600, 20), (3, 2048, 33), (4, 2048, 33), (1, 1000, 8200), (2, 4096, 8200), (3, 4096, 8200), (4, 4000, 8192)])
+def test_few_rows(rows, cin, cout, gated, dtype):
+    """The sizes at which a few rows change kernels."""
+    rng = np.random.default_rng(rows + cin + cout)
+    codes, scale, bias = layer(rng, cout * (2 if gated else 1), cin, 64, True)
+    x = tokens(rng, rows, cin, dtype)
+    y = hatq.hatq_linear4_forward(packed(codes, scale, bias, 8, gated), x.to(DEV))
+    compare(x, y, codes, scale, bias, 8, 64, gated)
+
+
 @pytest.mark.parametrize("rows,gated", [(12, False), (30, False), (100, False), (12, True), (100, True)])
 def test_many_groups(rows, gated):
     """Channels enough for waves that take several groups of them, and one group past the last
