@@ -255,22 +255,23 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear
 
 // ---- codes from memory ------------------------------------------------------------------
 // Waves of a block take G groups of 16 channels by 16 MT rows, `wk` of them the tiles of the
-// contraction in turn (they add up in LDS), the others channels further on.  The groups are a
-// gated layer's gates and values, or G adjacent ones, which share the rows' codes: of those a
-// wave reads 2 KB for 1 KB of weights and 16 rows, and of long calls they are what the L2s give.
+// contraction in turn (they add up in LDS), the others channels further on.  Adjacent groups (and
+// a gated layer's gates and values) share the rows' codes: of those a wave reads 2 KB for 1 KB of
+// weights and 16 rows, and of long calls they are what the L2s give.
 template <int G, int S, int MT, bool GATED>
 __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linear4Args a, int wk) {
     constexpr int U = MT * G >= 16 ? 1 : MT == 1 ? 4 : 2;   // tiles loaded at once
+    constexpr int R = GATED ? 2 : 1, N = G / R;             // products an output, output groups a wave
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     v4f(*part)[G][MT][64] = reinterpret_cast<v4f(*)[G][MT][64]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_k = wave & (wk - 1);
-    const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16, sets = GATED ? groups : (groups + G - 1) / G;
+    const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16, sets = (groups + N - 1) / N;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int row0 = (int)(block % row_tiles) * (16 * MT);
     const int64_t c16_ = block / row_tiles * (kWaves / wk) + wave / wk;
     const int c16 = (int)(c16_ < sets ? c16_ : sets - 1);
     // (past the last group: the last one again, not stored)
-    const auto group = [&](int g) { return GATED ? c16 * G + g : min(c16 * G + g, groups - 1); };
+    const auto group = [&](int g) { return min(c16 * N + g / R, groups - 1) * R + g % R; };
     const int tiles = a.k_stride >> 7;
     const int8_t *from[MT];
 #pragma unroll
@@ -323,15 +324,12 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linea
     for (int m = 0; m < MT; ++m) {
         const int row = row0 + 16 * m + (lane & 15);
         const float s = a.sx[min(row, a.rows - 1)] * a.inv_b;
-        if constexpr (GATED) {
-            const v4f sum[2] = {acc[0][m], acc[G - 1][m]};
-            finish<2>(a, sum, s, row, c16, lane);
-        } else {
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const v4f sum[1] = {acc[g][m]};
-                if (c16 * G + g < groups) finish<1>(a, sum, s, row, c16 * G + g, lane);
-            }
+        for (int n = 0; n < N; ++n) {
+            v4f sum[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) sum[r] = acc[n * R + r][m];
+            if (c16 * N + n < groups) finish<R>(a, sum, s, row, c16 * N + n, lane);
         }
     }
 }
@@ -476,7 +474,8 @@ void token(const Linear4Args &a, const TokenArgs &x, hipStream_t st) {
 
 template <int G, int S, int MT, bool GATED>
 void stream(const Linear4Args &a, hipStream_t st) {
-    const int64_t groups = (a.cout + 15) / 16, sets = GATED ? groups : (groups + G - 1) / G;
+    constexpr int N = GATED ? G / 2 : G;
+    const int64_t groups = (a.cout + 15) / 16, sets = (groups + N - 1) / N;
     const int64_t row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
     const int tiles = a.k_stride >> 7;
     // waves on one set of groups while the sets do not fill the card, and while each has a tile
@@ -486,15 +485,22 @@ void stream(const Linear4Args &a, hipStream_t st) {
     const size_t bytes = wk > 1 ? (size_t)kWaves * G * MT * 1024 : 0;
     linear4_stream_kernel<G, S, MT, GATED><<<grid_of((sets + cols - 1) / cols * row_tiles), 512, bytes, st>>>(a, wk);
 }
-// Adjacent groups a wave: as many as leave the card sets enough, 512 of 4 groups or 256 of 2.
-// In us at 1, 2 and 4 groups: 64 rows of 4096 -> 4096 (128 sets of 2) 14.9, 17.3, 21.0; 128 rows
-// (256 of 2) 22.6, 17.7, 22.4; 128 of 4096 -> 16384 (512 of 4) 68.1, 42.9, 39.9; 2048 rows of
-// 4096 -> 4096: 251, 143, 94.7.
+// Groups a wave (a gated layer's count twice): as many as leave the card 256 sets, of up to 16 rows
+// at most 2.  In us at 1, 2 and 4 groups: 64 rows of 4096 -> 4096 (64 sets of 4) 14.9, 17.3, 21.0;
+// 128 rows (256 of 2) 22.6, 17.7, 22.4; 256 rows (256 of 4) 26.6 at 2, 23.1 at 4; 2048 rows 251,
+// 143, 94.7; 16 rows of 8192 -> 16384 (256 of 4) 19.0 and 20.6.  Gated, at 2 and 4: 64 rows of 4096
+// -> 4096 (128 of 4) 17.8 and 21.7; 128 rows 26.0 and 22.5; 128 of 8192 -> 16384 139 and 94.
 template <int S, int MT>
 void stream(const Linear4Args &a, hipStream_t st) {
-    const int64_t groups = (a.cout + 15) / 16, row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
+    const int64_t groups = (int64_t)((a.cout + 15) / 16) * (a.gated ? 2 : 1), row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
+    if constexpr (MT > 1) {
+        if ((groups + 3) / 4 * row_tiles >= 256) {
+            if (a.gated) stream<4, S, MT, true>(a, st);
+            else stream<4, S, MT, false>(a, st);
+            return;
+        }
+    }
     if (a.gated) stream<2, S, MT, true>(a, st);
-    else if ((groups + 3) / 4 * row_tiles >= 512) stream<4, S, MT, false>(a, st);
     else if ((groups + 1) / 2 * row_tiles >= 256) stream<2, S, MT, false>(a, st);
     else stream<1, S, MT, false>(a, st);
 }

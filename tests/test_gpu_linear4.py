@@ -246,7 +246,7 @@ def test_few_rows(rows, cin, cout, gated, dtype):
     compare(x, y, codes, scale, bias, 8, 64, gated)
 
 
-@pytest.mark.parametrize("rows,gated", [(12, False), (30, False), (100, False), (12, True), (100, True)])
+@pytest.mark.parametrize("rows,gated", [(12, False), (30, False), (100, False), (12, True), (20, True), (100, True)])
 def test_many_groups(rows, gated):
     """Channels enough for waves that take several groups of them, and one group past the last
     whole set; the reference in float64 on the GPU."""
