@@ -173,7 +173,7 @@ int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_he
     a.y = heads_of(y);
     a.share = q_heads / C->heads;
     a.causal = causal;
-    a.window = window > kMaxPositions ? (int32_t)kMaxPositions : window;
+    a.window = window;
     a.scale = scale;
     a.splits = p.splits;
     a.ws = ws;

@@ -11,9 +11,9 @@
 // First product: the codes in float16, exact, against the query in two float16 halves, 22
 // bits (many rows of bf16: one half, 11 bits), after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
-// kept relative to the largest of w s_v (not of w), or to one up to 2^8 smaller, so the float16 range holds whatever the
-// scales are (2^-100 to 2^100): off by 2^-11 of each weight or 2^-25 of the largest.  For
-// float16 and float32 results NP = 2 halves carry 22 bits of it.
+// kept relative to the largest of w s_v (not of w) or to one up to 2^8 smaller, so the
+// float16 range holds whatever the scales are (2^-100 to 2^100): off by 2^-11 of each weight
+// or 2^-25 of the largest.  For float16 and float32 results NP = 2 halves carry 22 bits of it.
 #include "cache4_device.h"
 
 #ifndef HATQ_ATTENTION_PART
@@ -176,12 +176,15 @@ __device__ __forceinline__ void make_query(const AttentionArgs &a, const ColTile
         }
 }
 
+// The first position that a row at `pos` sees.
+__device__ __forceinline__ int first_seen(int pos, int window) { return window <= 0 || window > pos ? 0 : pos - window + 1; }
+
 // The positions that this lane's column sees.
 template <int NB>
 __device__ __forceinline__ void see(const AttentionArgs &a, const ColTile &t, int length, int col, Query &q) {
     const int c = min(t.col0 + col + (int)(threadIdx.x & 15), t.count * a.share - 1);
     q.pos = a.causal ? length - t.count + c / a.share : length - 1;
-    q.from = a.window ? max(q.pos - a.window + 1, 0) : 0;
+    q.from = first_seen(q.pos, a.window);
 }
 
 // ---- running result of sixteen columns ------------------------------------------------
@@ -488,13 +491,6 @@ __device__ __forceinline__ void store_columns(const AttentionArgs &a, const ColT
     }
 }
 
-// Length of a sequence in the cache, by its table at most.
-__device__ __forceinline__ int length_of(const AttentionArgs &a, int seq) {
-    const int64_t most = (int64_t)a.at.width << a.c.log_page;
-    const int n = max(a.at.lens[seq], 0);
-    return n < most ? n : (int)most;
-}
-
 // Sums of `waves` waves of one tile into wave 0's: every wave leaves its own in LDS, every
 // thread adds the waves' values of some of them.  lds: waves * (NB * 4 KB + 128 bytes), not in
 // use by others.
@@ -553,18 +549,20 @@ attention4_kernel(const AttentionArgs a) {
     const int64_t tile = block / a.splits / a.c.heads;
     const ColTile t = col_tile<16 * NQ>(a, tile);
     if (t.seq < 0) return;
-    const int length = length_of(a, t.seq), cols = t.count * a.share;
+    const int length = max(a.at.lens[t.seq], 0), cols = t.count * a.share;
+    const int most = a.at.width << a.c.log_page;    // positions of a table, up to 2^30
     // rows of the first and last column
     const int i0 = t.col0 / a.share, i1 = (min(t.col0 + 16 * NQ, cols) - 1) / a.share;
     int from = 0, to = length, sure_from = 0, sure_to = length;
     if (a.causal) {
         to = min(length, length - t.count + i1 + 1);
         sure_to = length - t.count + i0 + 1;
-        if (a.window) {
-            from = max(length - t.count + i0 - a.window + 1, 0) & ~31;
-            sure_from = length - t.count + i1 - a.window + 1;
-        }
+        from = first_seen(length - t.count + i0, a.window) & ~31;
+        sure_from = first_seen(length - t.count + i1, a.window);
     }
+    // (a length may pass its table: its rows' positions count from there all the same)
+    to = min(to, most);
+    from = min(from, to);
     const int64_t steps = to > from ? (to - from + 31) >> 5 : 0;
     const int begin = (int)(steps * split / a.splits), end = (int)(steps * (split + 1) / a.splits);
     Walk<NB, HALF> walk(a, t.seq, head, from + 32 * (begin + wave), end == steps ? to : from + 32 * end, 32 * waves);

@@ -31,7 +31,8 @@ AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t
     // 33.6, in 2 parts 34.7; 2 of 131072, 4 heads, fp16, 32 parts, 8 waves 48.3, 16 46.8; 1 of
     // 300, 64 channels, 4 waves 8.3, 8 7.9, 16 8.9.)
     int64_t most = max_len;
-    if (window > 0 && window + rows / batch < most) most = window + rows / batch;
+    const int64_t seen = (int64_t)window + rows / batch;
+    if (window > 0 && seen < most) most = seen;
     const int64_t steps = (most + 31) / 32, base = p.tiles * heads;
     int64_t splits = 256 / base;
     if (splits > steps / 16) splits = steps / 16;

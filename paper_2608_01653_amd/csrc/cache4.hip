@@ -42,8 +42,8 @@ __device__ __forceinline__ uint8_t *octet_of(const Cache4 &c, int page, int head
 // codes; the codes are made with the rounded scale, so the rounding (2^-9) costs nothing
 // but the clamp of a maximum up to 7.03 steps away.
 // Codes without a division for each: with r within 2^-23 of 1 / s, v r and v / s differ by at
-// most 7.03 (2^-23 + 2^-24) < 2^-19, so k = rne(v r) is rne(fl(v / s)) where v r is within 0.5 - 2^-16 of k; a
-// chunk with a value nearer to the middle of two codes divides.
+// most 7.03 (2^-23 + 2^-24) < 2^-19, so k = rne(v r) is rne(fl(v / s)) where v r is within
+// 0.5 - 2^-16 of k; a chunk with a value nearer to the middle of two codes divides.
 // LB: log2 of the transform's block, -1 where it is known at run time only.
 template <int NB, int LB>
 __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs a, int log_heads) {

@@ -90,12 +90,14 @@ def attention64(q, k, v, v_scale, hblock, scale, causal, window, fine, there=Non
     the largest of a value's scales; there [len]: positions whose page is.
 
     The bound (u = 2^-24): the query in two float16 halves is off by 2^-22 = 4 u of itself (many
-    rows of bfloat16, in one half, by 2^-11); a product is exact, and a score's sum in float32 (64 products, two scales of up to four
-    groups, the factor) has at most 80 roundings, u sum |q k| each; an error of e moves each normalized weight by at most a
-    factor exp(2 e).  A weight times scale in float16 is off by 2^-11 of itself (two halves
-    2^-21), or where subnormal by 2^-25 of a unit that is at most 2 of the largest weight times
-    scale (a value's codes may be 0, so the scale and not the value counts); the exponential and the products add 8 u.  Float32 sums of len terms add len u each of the
-    magnitudes.  In the end the transform's sums add 8 u of the magnitudes."""
+    rows of bfloat16, in one half, by 2^-11); a product is exact, and a score's sum in float32
+    (64 products, two scales of up to four groups, the factor) has at most 80 roundings, u sum
+    |q k| each; an error of e moves each normalized weight by at most a factor exp(2 e).  A
+    weight times scale in float16 is off by 2^-11 of itself (two halves 2^-21), or where
+    subnormal by 2^-25 of a unit that is at most 2 of the largest weight times scale (a value's
+    codes may be 0, so the scale and not the value counts); the exponential and the products
+    add 8 u.  Float32 sums of len terms add len u each of the magnitudes.  In the end the
+    transform's sums add 8 u of the magnitudes."""
     n, heads_q, dim = q.shape
     length, heads = k.shape[:2]
     share = heads_q // heads

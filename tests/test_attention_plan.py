@@ -83,3 +83,10 @@ def test_the_gpu_tests_shapes(plan):
     assert plan([(5, 508, 8, 8, 256, 400, 1, 0)])[0][0] == 16
     # one token a sequence is never wide
     assert plan([(64, 64, 8, 8, 128, 16384, 0, 0)])[0][:3] == (16, 8, 1)
+
+
+def test_the_widest_window(plan):
+    """A window of any size is at most all positions."""
+    for batch, rows, max_len in ((1, 1, 65536), (2, 64, 4096), (1, 2 ** 24, 2 ** 30)):
+        whole = plan([(batch, rows, 8, 4, 128, max_len, 0, 0)])
+        assert plan([(batch, rows, 8, 4, 128, max_len, 0, 2 ** 31 - 1)]) == whole

@@ -157,6 +157,34 @@ def test_absent_pages(new):
     compare(s, q[:new], [new], y, causal=False, there=[there])
 
 
+@pytest.mark.parametrize("new,window", [(1, 0), (6, 0), (100, 0), (100, 20), (6, 30), (150, 7)])
+@pytest.mark.parametrize("page,share", [(16, 4), (32, 1), (16, 1)])
+def test_lengths_past_the_table(new, window, page, share):
+    """A row's position counts from its sequence's length, also where that is past the table:
+    it sees the table's positions before its own."""
+    s = Sequences([150], 2, 128, 64, page, torch.float32, seed=22)
+    s.write()
+    width = 80 // page
+    q = queries(s, [new], 2 * share, torch.float32)
+    y = hatq.hatq_attention4(s.cache, q.to(DEV), s.table[:, :width].contiguous(), s.lens, window=window)
+    there = np.arange(150) < width * page
+    compare(s, q, [new], y, window=window, there=[there])
+
+
+def test_the_longest_length():
+    s = Sequences([64], 1, 64, 64, 16, torch.bfloat16, seed=23)
+    s.write()
+    q = queries(s, [2], 1, torch.bfloat16).to(DEV)
+    long = dev(np.array([2 ** 31 - 1], np.int32))
+    y = hatq.hatq_attention4(s.cache, q, s.table, long)
+    assert torch.equal(y, hatq.hatq_attention4(s.cache, q, s.table, s.lens, causal=False))
+    assert bool((hatq.hatq_attention4(s.cache, q, s.table, long, window=2 ** 31 - 1 - 2 ** 30) == 0).all())
+    assert bool((hatq.hatq_attention4(s.cache, q, s.table, long, window=1) == 0).all())
+    assert torch.equal(y, hatq.hatq_attention4(s.cache, q, s.table, long, window=2 ** 31 - 1))
+    none = dev(np.array([0], np.int32))
+    assert bool((hatq.hatq_attention4(s.cache, q, s.table, none, window=2 ** 31 - 1) == 0).all())
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_not_finite(dtype):
     """A NaN key or value in one sequence makes its own rows NaN that see it, no others; what
