@@ -4,7 +4,7 @@
 namespace hatq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 
 // s = bf16(fl32(m / 7)), at least 2^-100, as a float.  With the largest magnitude below 2^102
 // a scale is within [2^-100, 2^100], so that a weight relative to weight times scale, as the
@@ -14,17 +14,18 @@ __device__ __forceinline__ float cache_scale(float m) {
     return fmaxf(__uint_as_float(bf16_pair(m / 7.0f, 0.0f) << 16), kLeastScale);
 }
 
-// A lane's place: a chunk of one head of one row, of keys or values (blockIdx.z).  The four
-// chunks of a head are adjacent lanes, so its transform and maxima stay inside a quad; eight
-// adjacent rows, mostly an octet of the cache, are in one half of a wave, whose stores and
-// loads then meet in few lines of it; a block has up to eight heads (2^log_heads), and as many
-// more rows where there are fewer.
+// A lane's place: a chunk of one head of one row, of keys (the first half of a block's threads) or
+// values.  The four chunks of a head are adjacent lanes, so its transform and maxima stay inside a
+// quad; eight adjacent rows, mostly an octet of the cache, are in one half of a wave, whose stores
+// and loads then meet in few lines of it; a block has up to eight heads (2^log_heads), and as many
+// more rows where there are fewer.  (Keys and values in one block, since an octet's lines hold
+// both: in blocks of their own 90 us for 83, 32768 rows of 8 heads of 128 bf16 in and out.)
 struct Unit {
     int row, head, chunk;
     bool in;
 };
 __device__ __forceinline__ Unit this_unit(const CacheArgs &a, int log_heads) {
-    const int t = threadIdx.x, u = t >> 5;
+    const int t = threadIdx.x & 255, u = t >> 5;
     const int row = (blockIdx.x * (8 >> log_heads) + (u >> log_heads)) * 8 + ((t >> 2) & 7);
     const int head = (blockIdx.y << log_heads) + (u & ((1 << log_heads) - 1));
     return {row, head, t & 3, row < a.at.rows && head < a.c.heads};
@@ -49,7 +50,7 @@ template <int NB, int LB>
 __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs a, int log_heads) {
     const Unit n = this_unit(a, log_heads);
     if (!n.in) return;
-    const int which = blockIdx.z;
+    const int which = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     const Heads4 x = which ? a.x[1] : a.x[0];
     float v[NB][16];
     Row4 r;
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const CacheArgs a
     const Row4 r = row_place(a.at, n.row);
     if (r.seq < 0) return;
     const int page = page_of(a.c, a.at, r.seq, r.pos);
-    const int which = blockIdx.z;
+    const int which = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
     float v[NB][16];
     if (page >= 0) {
         const uint8_t *const octet = octet_of<NB>(a.c, page, n.head, r.pos);
@@ -173,37 +174,50 @@ __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const CacheArgs a
 int log_heads_of(const CacheArgs &a) { return a.c.heads >= 5 ? 3 : a.c.heads >= 3 ? 2 : a.c.heads - 1; }
 dim3 unit_grid(const CacheArgs &a) {
     const int log = log_heads_of(a), rows = 64 >> log;
-    return dim3((a.at.rows + rows - 1) / rows, (a.c.heads + (1 << log) - 1) >> log, 2);
+    return dim3((a.at.rows + rows - 1) / rows, (a.c.heads + (1 << log) - 1) >> log);
+}
+
+// A kernel for the call's blocks of channels and its transform: of 64 and 128 as constants, 722 ->
+// 600 vector instructions a wave.
+#define HATQ_CACHE_LAUNCH(kernel, nb)                                                            \
+    do {                                                                                          \
+        if constexpr (nb % 2 == 0)                                                                \
+            if (a.c.log_b == 7) { kernel<nb, 7><<<grid, kThreads, 0, st>>>(a, log); break; }      \
+        if (a.c.log_b == 6) kernel<nb, 6><<<grid, kThreads, 0, st>>>(a, log);                     \
+        else kernel<nb, -1><<<grid, kThreads, 0, st>>>(a, log);                                   \
+    } while (0)
+
+template <int NB>
+void append(const CacheArgs &a, hipStream_t st) {
+    const dim3 grid = unit_grid(a);
+    const int log = log_heads_of(a);
+    HATQ_CACHE_LAUNCH(cache4_append_kernel, NB);
+}
+template <int NB>
+void read(const CacheArgs &a, hipStream_t st) {
+    const dim3 grid = unit_grid(a);
+    const int log = log_heads_of(a);
+    HATQ_CACHE_LAUNCH(cache4_read_kernel, NB);
 }
 
 }  // namespace
 
-// (the blocks of 64 and 128 as constants: 722 -> 600 vector instructions a wave)
-#define HATQ_CACHE_LAUNCH(kernel, nb)                                                                        \
-    if (a.c.log_b == 6) kernel<nb, 6><<<grid, kThreads, 0, st>>>(a, log);                                       \
-    else if (a.c.log_b == 7 && nb % 2 == 0) kernel<nb, 7><<<grid, kThreads, 0, st>>>(a, log);                   \
-    else kernel<nb, -1><<<grid, kThreads, 0, st>>>(a, log)
-
 hipError_t launch_cache4_append(const CacheArgs &a, hipStream_t st) {
-    const dim3 grid = unit_grid(a);
-    const int log = log_heads_of(a);
     switch ((a.c.dim + 63) / 64) {
-        case 1: HATQ_CACHE_LAUNCH(cache4_append_kernel, 1); break;
-        case 2: HATQ_CACHE_LAUNCH(cache4_append_kernel, 2); break;
-        case 3: HATQ_CACHE_LAUNCH(cache4_append_kernel, 3); break;
-        default: HATQ_CACHE_LAUNCH(cache4_append_kernel, 4); break;
+        case 1: append<1>(a, st); break;
+        case 2: append<2>(a, st); break;
+        case 3: append<3>(a, st); break;
+        default: append<4>(a, st); break;
     }
     return hipGetLastError();
 }
 
 hipError_t launch_cache4_read(const CacheArgs &a, hipStream_t st) {
-    const dim3 grid = unit_grid(a);
-    const int log = log_heads_of(a);
     switch ((a.c.dim + 63) / 64) {
-        case 1: HATQ_CACHE_LAUNCH(cache4_read_kernel, 1); break;
-        case 2: HATQ_CACHE_LAUNCH(cache4_read_kernel, 2); break;
-        case 3: HATQ_CACHE_LAUNCH(cache4_read_kernel, 3); break;
-        default: HATQ_CACHE_LAUNCH(cache4_read_kernel, 4); break;
+        case 1: read<1>(a, st); break;
+        case 2: read<2>(a, st); break;
+        case 3: read<3>(a, st); break;
+        default: read<4>(a, st); break;
     }
     return hipGetLastError();
 }
