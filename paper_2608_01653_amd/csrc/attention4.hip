@@ -539,6 +539,12 @@ __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, cha
 // positions.  NQ > 1 where there are many columns: a step's codes are unpacked once for all of
 // them.  (Its waves share the positions there too, not the columns: blocks then last a
 // fourth as long, and the last ones of a full card leave less of it idle.)
+// What bounds it: few columns, the cache's bytes while enough waves have a step of 4 KB under
+// way each (64 sequences of 16384, 8 heads of 128 channels: 226 us for 1.09 GB, 4.8 TB/s), behind 6
+// to 8 us for the query, the first loads and the waves' sums (2 sequences of 131072, 4 heads:
+// 44 us for 143 MB); many columns, the vector instructions of weights and codes beside the matrix
+// ones (parts of prompts, 2048 rows over 4096 to 8192 positions, 16 heads over 2 of 128: 350 us,
+// 590 TFLOP/s of 1200 that a large float16 product reaches).
 template <int NB, int NP, int NQ, bool HALF>
 __global__ void __launch_bounds__(NQ > 1 ? 256 : NB <= 2 ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(NB <= 2 && NQ == 1 ? 4 : 2)))
 attention4_kernel(const AttentionArgs a) {

@@ -46,6 +46,9 @@ __device__ __forceinline__ uint8_t *octet_of(const Cache4 &c, int page, int head
 // most 7.03 (2^-23 + 2^-24) < 2^-19, so k = rne(v r) is rne(fl(v / s)) where v r is within
 // 0.5 - 2^-16 of k; a chunk with a value nearer to the middle of two codes divides.
 // LB: log2 of the transform's block, -1 where it is known at run time only.
+// Bound by the instructions next to the bytes: 32768 rows of 8 heads of 128, bf16, of a fused
+// query-key-value product: 50 us for 170 MB (a copy of as many 33), 613 vector instructions a
+// wave that take 33 us by themselves (224 of them the 7 butterfly stages of 32 values a lane).
 template <int NB, int LB>
 __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs a, int log_heads) {
     const Unit n = this_unit(a, log_heads);
@@ -121,7 +124,8 @@ __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs
     }
 }
 
-// x' = B (s c) / b: what the codes stand for, 0 where there is no page.
+// x' = B (s c) / b: what the codes stand for, 0 where there is no page.  As many rows as above: 34 to 36
+// us for 170 MB, 5 TB/s, with 550 vector instructions a wave that take 29.
 template <int NB, int LB>
 __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const CacheArgs a, int log_heads) {
     const Unit n = this_unit(a, log_heads);
