@@ -100,6 +100,9 @@ int32_t prepare(int32_t cin, int32_t cout, int32_t gated, int32_t hblock, int32_
     return HATQ_OK;
 }
 
+// The codes of a call's tokens, 16 rows at a time.
+size_t code_bytes(const hatq_linear4_weights *W, int32_t rows) { return align256(((size_t)rows + 15) / 16 * 16 * W->k_stride); }
+
 }  // namespace
 
 extern "C" {
@@ -126,7 +129,7 @@ int32_t hatq_pack_linear4(int32_t cin, int32_t cout, int32_t gated, int32_t hblo
 size_t hatq_linear4_ws_bytes(const hatq_linear4_weights *W, int32_t rows) {
     if (check_weights(W) != HATQ_OK || rows <= 0 || rows > hatq::kMaxRows) return 0;
     if (hatq::linear4_takes_tokens(rows, W->cout, W->k_stride)) return 0;
-    return align256((size_t)rows * W->k_stride) + align256((size_t)rows * 4);
+    return code_bytes(W, rows) + align256((size_t)rows * 4);
 }
 
 int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32_t x_type, int32_t rows,
@@ -147,13 +150,14 @@ int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32
     hatq::TokenArgs t{};
     t.x = x;
     t.xq = static_cast<int8_t *>(ws);
-    t.sx = tokens ? nullptr : reinterpret_cast<float *>(t.xq + align256((size_t)rows * W->k_stride));
+    t.sx = tokens ? nullptr : reinterpret_cast<float *>(t.xq + code_bytes(W, rows));
     t.x_stride = x_stride;
     t.x_type = x_type;
     t.rows = rows;
     t.cin = W->cin;
     t.k_stride = W->k_stride;
     t.log_b = log_block(W->hblock);
+    t.by16 = 1;
     hatq::Linear4Args a{};
     a.xq = t.xq;
     a.sx = t.sx;

@@ -25,6 +25,7 @@ struct TokenArgs {
     int32_t x_type;
     int32_t rows, cin, k_stride;
     int32_t log_b;      // transform block 2^log_b
+    int32_t by16;       // codes: 0 by rows, 1 as 16 rows' matrix operands, [rows / 16][k_stride / 16][16][16]
 };
 hipError_t launch_token_quant(const TokenArgs &a, hipStream_t st);
 

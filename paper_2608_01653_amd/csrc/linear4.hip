@@ -262,8 +262,12 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear
 // weights and 16 rows, and of long calls they are what the L2s give.
 // Few rows are bound by the weights' bytes: 6 rows, 8192 -> 2 x 16384, 27.4 us for 143 MB, 5.2
 // TB/s; many by the codes' loads, and by a conversion and a multiply-add for each sum and group:
-// 128 rows of 8192 -> 2 x 16384 94 us, 730 TOP/s, as 2048 rows of 4096 -> 4096, 95 us.  (The next
+// 128 rows of 8192 -> 2 x 16384 66 us, 1040 TOP/s, as 2048 rows of 4096 -> 4096, 68 us.  (The next
 // step's loads over this one's products, in registers of their own: 5 to 12 % behind.)
+// The codes lie as the operands are, 1 KB for 16 rows by 64 input channels: by rows, adjacent
+// lanes are in 16 lines, a load is 64 accesses of the CU's cache instead of 16, and those bound
+// the same two calls at 94 and 97 us.  Adjacent blocks go to one die each, so the tiles of rows
+// that share weights meet in its L2 (17 rows of 16384 -> 16384 32.7 -> 30.4 us).
 template <int G, int S, int MT, bool GATED>
 __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linear4Args a, int wk) {
     constexpr int U = MT * G >= 16 ? 1 : MT == 1 ? 4 : 2;   // tiles loaded at once
@@ -272,7 +276,9 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linea
     v4f(*part)[G][MT][64] = reinterpret_cast<v4f(*)[G][MT][64]>(lds);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_k = wave & (wk - 1);
     const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16, sets = (groups + N - 1) / N;
-    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t per = ((int64_t)gridDim.y * gridDim.x) >> 3;
+    if (block < 8 * per) block = (block & 7) * per + (block >> 3);
     const int row0 = (int)(block % row_tiles) * (16 * MT);
     const int64_t c16_ = block / row_tiles * (kWaves / wk) + wave / wk;
     const int c16 = (int)(c16_ < sets ? c16_ : sets - 1);
@@ -282,7 +288,7 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linea
     const int8_t *from[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
-        from[m] = a.xq + (int64_t)min(row0 + 16 * m + (lane & 15), a.rows - 1) * a.k_stride + (lane >> 4) * 16;
+        from[m] = a.xq + (int64_t)min((row0 >> 4) + m, (a.rows - 1) >> 4) * 16 * a.k_stride + lane * 16;
     v4f acc[G][MT];
 #pragma unroll
     for (int g = 0; g < G; ++g)
@@ -300,9 +306,9 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linea
                              t[u][g]);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const v4i *c = reinterpret_cast<const v4i *>(from[m] + k * 128);
+                const v4i *c = reinterpret_cast<const v4i *>(from[m] + k * 2048);
                 fx[u][m][0] = c[0];
-                fx[u][m][1] = c[4];
+                fx[u][m][1] = c[64];
             }
         }
 #pragma unroll

@@ -44,12 +44,14 @@ __device__ __forceinline__ void token_quant_row(const TokenArgs &a, int64_t row,
     if (t == 0) a.sx[row] = s;
     const float r = sigma * (1.0f / s);
     const bool plain = token_plain(s);
-    int8_t *q = a.xq + row * a.k_stride;
+    // (by 16 rows: 16 codes of a row, then those of the next)
+    int8_t *q = a.xq + (a.by16 ? (row >> 4) * 16 * a.k_stride + (row & 15) * 16 : row * a.k_stride);
+    const int pair = a.by16 ? 256 : 16;
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
         const int c = i * RT + t;
         const uint2 codes = token_codes8(&v[8 * i], sigma, s, r, plain);
-        if (c < chunks) *reinterpret_cast<uint2 *>(q + c * 8) = codes;
+        if (c < chunks) *reinterpret_cast<uint2 *>(q + (c >> 1) * pair + (c & 1) * 8) = codes;
     }
 }
 

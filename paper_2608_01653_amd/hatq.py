@@ -1110,7 +1110,8 @@ def hatq_linear4_forward(lin: PreparedLinear4, x: torch.Tensor, out_dtype: Optio
     y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
     _here(lin.device, x, y, ws)
     if ws is None and lin.k_stride > 2048 and n * lin.k_stride > HATQ_TOKEN_CODES >> (lin.cout > 8192):
-        ws = _linear_ws(lin, n, ws, x)
+        # hatq_linear4_ws_bytes, without the call
+        ws = x.new_empty((n + 15 & -16) * lin.k_stride + (4 * n + 255 & -256), dtype=torch.int8)
     _need(ws, "ws", torch.int8, 0, optional=True)
     wp, wn = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
     _check(load().hatq_linear4_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, wp, wn, _stream()),

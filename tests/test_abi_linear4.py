@@ -45,11 +45,11 @@ def test_bytes(L):
         assert L.hatq_linear4_weights_bytes(*bad) == 0, bad
     w = weights()
     assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 4) == 0
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 5) == 5 * 4096 + 256
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 5) == 16 * 4096 + 256
     assert L.hatq_linear4_ws_bytes(ctypes.byref(w), 2 ** 24) == (4096 << 24) + (4 << 24)
     wide = weights(cout=8208, cout_pad=8208)
     assert L.hatq_linear4_ws_bytes(ctypes.byref(wide), 2) == 0
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(wide), 3) == 3 * 4096 + 256
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(wide), 3) == 16 * 4096 + 256
     short = weights(cin=2000, k_stride=2048)
     assert L.hatq_linear4_ws_bytes(ctypes.byref(short), 2 ** 24) == 0
     for rows in (0, -1, 2 ** 24 + 1):
