@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_token_kernel(const Linear
     float *scale = reinterpret_cast<float *>(lds + kWaves * G * 1024);      // [16]
     float *most = scale + 16;                                              // [kWaves]
     int8_t *codes = lds + kWaves * G * 1024 + 128;                          // [rows][k_stride + 16]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c16 = blockIdx.x, rows = a.rows;
     const int pitch = a.k_stride + 16;   // 16 rows' pieces then lie in different banks
     TokenRow<T> token = token_row<T>(x, 0);
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear
     constexpr int U = 4, ROWS = 16, TURNS = ROWS / kWaves;
     __shared__ __attribute__((aligned(16))) int8_t codes[ROWS * (512 * CH + 16)];
     __shared__ float scale[ROWS];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = blockIdx.x * ROWS, rows = min(a.rows - row0, ROWS);
     const int tiles = a.k_stride >> 7, pitch = a.k_stride + 16;
     const int end = min(((int)blockIdx.y + 1) * per, (a.cout + 15) / 16);
@@ -270,11 +270,11 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear
 // that share weights meet in its L2 (17 rows of 16384 -> 16384 32.7 -> 30.4 us).
 template <int G, int S, int MT, bool GATED>
 __global__ void __launch_bounds__(64 * kWaves) linear4_stream_kernel(const Linear4Args a, int wk) {
-    constexpr int U = MT * G >= 16 ? 1 : MT == 1 ? 4 : 2;   // tiles loaded at once
+    constexpr int U = MT == 1 ? 4 : MT == 4 ? 1 : 2;              // tiles loaded at once
     constexpr int R = GATED ? 2 : 1, N = G / R;             // products an output, output groups a wave
     extern __shared__ __attribute__((aligned(16))) int8_t lds[];
     v4f(*part)[G][MT][64] = reinterpret_cast<v4f(*)[G][MT][64]>(lds);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part_k = wave & (wk - 1);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part_k = wave & (wk - 1);
     const int row_tiles = (a.rows + 16 * MT - 1) / (16 * MT), groups = (a.cout + 15) / 16, sets = (groups + N - 1) / N;
     int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int64_t per = ((int64_t)gridDim.y * gridDim.x) >> 3;
@@ -498,24 +498,17 @@ void stream(const Linear4Args &a, hipStream_t st) {
     const size_t bytes = wk > 1 ? (size_t)kWaves * G * MT * 1024 : 0;
     linear4_stream_kernel<G, S, MT, GATED><<<grid_of((sets + cols - 1) / cols * row_tiles), 512, bytes, st>>>(a, wk);
 }
-// Groups a wave (a gated layer's count twice): as many as leave the card 256 sets, of up to 16 rows
-// at most 2.  In us at 1, 2 and 4 groups: 64 rows of 4096 -> 4096 (64 sets of 4) 14.9, 17.3, 21.0;
-// 128 rows (256 of 2) 22.6, 17.7, 22.4; 256 rows (256 of 4) 26.6 at 2, 23.1 at 4; 2048 rows 251,
-// 143, 94.7; 16 rows of 8192 -> 16384 (256 of 4) 19.0 and 20.6.  Gated, at 2 and 4: 64 rows of 4096
-// -> 4096 (128 of 4) 17.8 and 21.7; 128 rows 26.0 and 22.5; 128 of 8192 -> 16384 139 and 94.
+// Two groups a wave of more than 16 rows, where they leave the card 256 sets; a gated layer's pair
+// always.  In us at 1, 2 and 4 groups: 16 rows of 8192 -> 16384 16.3, 17.1, 18.0; 64 rows of 4096
+// -> 4096 (128 sets of 2) 10.5, 12.5, 16.2; 128 of 16384 -> 4096 (256 of 2) 33.5, 29.1, 34.6; 128 of
+// 4096 -> 16384 28.4, 24.8, 31.8; 512 of 4096 -> 4096 30.5, 26.6, 33.4.
 template <int S, int MT>
 void stream(const Linear4Args &a, hipStream_t st) {
-    const int64_t groups = (int64_t)((a.cout + 15) / 16) * (a.gated ? 2 : 1), row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
-    if constexpr (MT > 1) {
-        if ((groups + 3) / 4 * row_tiles >= 256) {
-            if (a.gated) stream<4, S, MT, true>(a, st);
-            else stream<4, S, MT, false>(a, st);
-            return;
-        }
-    }
-    if (a.gated) stream<2, S, MT, true>(a, st);
-    else if ((groups + 1) / 2 * row_tiles >= 256) stream<2, S, MT, false>(a, st);
-    else stream<1, S, MT, false>(a, st);
+    const int64_t sets = ((a.cout + 15) / 16 + 1) / 2, row_tiles = (a.rows + 16 * MT - 1) / (16 * MT);
+    if (a.gated) return stream<2, S, MT, true>(a, st);
+    if constexpr (MT > 1)
+        if (sets * row_tiles >= 256) return stream<2, S, MT, false>(a, st);
+    stream<1, S, MT, false>(a, st);
 }
 template <int S>
 void stream(const Linear4Args &a, hipStream_t st) {
