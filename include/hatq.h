@@ -644,9 +644,8 @@ int32_t hatq_pack_linear4(int32_t cin, int32_t cout, int32_t gated, int32_t hblo
  *   x: device [rows][cin] of x_type, row stride x_stride >= cin elements;
  *   y: device [rows][cout] of y_type, row stride y_stride >= cout elements.
  *   ws: device memory, 256-byte aligned, of at least hatq_linear4_ws_bytes(W, rows) bytes;
- *       may be NULL where that is 0 (k_stride <= 2048, or a few tokens: rows k_stride <=
- *       HATQ_TOKEN_CODES, of cout > 8192 half that).  Calls that may overlap need workspaces
- *       of their own. */
+ *       may be NULL where that is 0 (a few tokens, small layers of a short contraction).  Calls
+ *       that may overlap need workspaces of their own. */
 size_t hatq_linear4_ws_bytes(const hatq_linear4_weights *W, int32_t rows);
 int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32_t x_type, int32_t rows,
                              int64_t x_stride, void *y, int32_t y_type, int64_t y_stride, void *ws, size_t ws_bytes,

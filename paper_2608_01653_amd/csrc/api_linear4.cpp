@@ -128,7 +128,7 @@ int32_t hatq_pack_linear4(int32_t cin, int32_t cout, int32_t gated, int32_t hblo
 
 size_t hatq_linear4_ws_bytes(const hatq_linear4_weights *W, int32_t rows) {
     if (check_weights(W) != HATQ_OK || rows <= 0 || rows > hatq::kMaxRows) return 0;
-    if (hatq::linear4_takes_tokens(rows, W->cout, W->k_stride)) return 0;
+    if (hatq::linear4_takes_tokens(rows, W->cout, W->gated, W->k_stride)) return 0;
     return code_bytes(W, rows) + align256((size_t)rows * 4);
 }
 
@@ -142,7 +142,7 @@ int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32
     if (rows == 0) return HATQ_OK;
     if ((s = check_rows(y, y_type, rows, W->cout, y_stride)) != HATQ_OK) return s;
     if ((s = check_rows(x, x_type, rows, W->cin, x_stride)) != HATQ_OK) return s;
-    const bool tokens = hatq::linear4_takes_tokens(rows, W->cout, W->k_stride);
+    const bool tokens = hatq::linear4_takes_tokens(rows, W->cout, W->gated, W->k_stride);
     if (!tokens) {
         if (!ws || !aligned(ws, 256)) return HATQ_EINVAL;
         if (ws_bytes < hatq_linear4_ws_bytes(W, rows)) return HATQ_EWORKSPACE;

@@ -33,7 +33,7 @@ struct Linear4Args {
     float inv_b;
 };
 // Tokens that the product's blocks quantize themselves, with no workspace (xq and sx unused).
-bool linear4_takes_tokens(int32_t rows, int32_t cout, int32_t k_stride);
+bool linear4_takes_tokens(int32_t rows, int32_t cout, int32_t gated, int32_t k_stride);
 hipError_t launch_linear4_tokens(const Linear4Args &a, const TokenArgs &x, hipStream_t st);
 // Codes and scales from memory.
 hipError_t launch_linear4(const Linear4Args &a, hipStream_t st);

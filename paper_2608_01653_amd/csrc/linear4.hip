@@ -519,16 +519,24 @@ void stream(const Linear4Args &a, hipStream_t st) {
 
 }  // namespace
 
-// (us in a graph, two kernels and one, bf16, 128 input channels a scale: 17 rows, 512 -> 512 6.3
-// and 4.7; 77, 1000 -> 1001 9.0 and 6.7; 128, 1024 -> 16384 22.3 and 15.0; 128, 2048 -> 8192 22.6
-// and 22.0; 4096, 2048 -> 4096 254 and 108; behind only for few groups of a long contraction,
-// 16, 2048 -> 4096 7.2 and 8.6.)
+// Which tokens the product's blocks quantize themselves.  (us in a graph, so and through memory,
+// bf16, 128 input channels a scale.)
+// Contractions up to 1024: a pass of the small kernel over all tiles of 16 rows by 16 outputs is
+// shorter than two launches up to 2^22 tiles' input channels, 2^23 of at most 256 groups: 16 rows,
+// 512 -> 4096 4.8 and 5.7; 128, 1024 -> 4096 6.8 and 9.9; 77, 1024 -> 16384 12.7 and 12.2; 512, 1024
+// -> 4096 11.3 and 12.8; 512, 256 -> 16384 18.4 and 15.6; 4096, 512 -> 512 7.9 and 14.3, 512 -> 4096
+// 33.8 and 32.2.  Up to 2048: few rows (4 rows, 2048 -> 16384 7.6 and 7.9, 16 rows 9.7 and 8.1, gated
+// 4 rows 9.3 and 7.0), and of more than 64 rows with few outputs (77, 2048 -> 4096 9.1 and 10.6; 512,
+// 2048 -> 512 8.7 and 10.5; 32, 2048 -> 4096 8.8 and 7.5; gated 77, 2048 -> 2048 11.6 and 10.3).
 // Longer ones: where every block quantizes all rows, up to 16 K codes, but 8 K of more than 512
-// blocks (so and from memory: 4 rows, 4096 -> 4096 6.9 and 7.7; 1 row, 16384 -> 4096 11.2 and
-// 13.4; 1 row, 8192 -> 16384 16.1 and 16.1; 4 rows, 4096 -> 16384 13.8 and 10.9; 1 row, 16384 ->
-// 16384 38.9 and 26.3).
-bool linear4_takes_tokens(int32_t rows, int32_t cout, int32_t k_stride) {
-    return k_stride <= 2048 || (int64_t)rows * k_stride <= (cout <= 8192 ? HATQ_TOKEN_CODES : HATQ_TOKEN_CODES / 2);
+// blocks: 4 rows, 4096 -> 4096 6.9 and 7.7; 1 row, 16384 -> 4096 11.2 and 13.4; 1 row, 8192 -> 16384
+// 16.1 and 16.1; 4 rows, 4096 -> 16384 13.8 and 10.9; 1 row, 16384 -> 16384 38.9 and 26.3.
+bool linear4_takes_tokens(int32_t rows, int32_t cout, int32_t gated, int32_t k_stride) {
+    if (k_stride > 2048) return (int64_t)rows * k_stride <= (cout <= 8192 ? HATQ_TOKEN_CODES : HATQ_TOKEN_CODES / 2);
+    if (rows < 4) return true;
+    const int64_t groups = (int64_t)((cout + 15) / 16) * (gated ? 2 : 1), work = ((int64_t)rows + 15) / 16 * groups * k_stride;
+    if (k_stride > 1024) return rows > 64 && !gated && groups <= 256 && work <= 1 << 23;
+    return work <= (groups <= 256 ? 1 << 23 : 1 << 22);
 }
 
 hipError_t launch_linear4_prepare(const Linear4PrepArgs &a, hipStream_t st) {

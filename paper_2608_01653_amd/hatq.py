@@ -1029,6 +1029,9 @@ class PreparedLinear4:
     def __post_init__(self):
         self.ref = ctypes.byref(self.w)
         self.device = self.buf.get_device()
+        # rows up to which a short contraction's call needs no workspace (hatq_linear4_ws_bytes
+        # knows the rest)
+        self.rows = (1 << 22) // (self.k_stride * self.w.cout_pad // 16) * 16 if self.k_stride <= 1024 else 0
 
 
 def _linear4(call: str, w: torch.Tensor, gated: bool, hblock: int, group: int, run) -> PreparedLinear4:
@@ -1109,9 +1112,10 @@ def hatq_linear4_forward(lin: PreparedLinear4, x: torch.Tensor, out_dtype: Optio
     n, _, xs, xt = _rows(x, "x", lin.cin)
     y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
     _here(lin.device, x, y, ws)
-    if ws is None and lin.k_stride > 2048 and n * lin.k_stride > HATQ_TOKEN_CODES >> (lin.cout > 8192):
-        # hatq_linear4_ws_bytes, without the call
-        ws = x.new_empty((n + 15 & -16) * lin.k_stride + (4 * n + 255 & -256), dtype=torch.int8)
+    if ws is None and n > lin.rows and n * lin.k_stride > HATQ_TOKEN_CODES // 4:    # (else it needs none)
+        nbytes = load().hatq_linear4_ws_bytes(lin.ref, n)
+        if nbytes:
+            ws = x.new_empty(nbytes, dtype=torch.int8)
     _need(ws, "ws", torch.int8, 0, optional=True)
     wp, wn = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
     _check(load().hatq_linear4_forward(lin.ref, x.data_ptr(), xt, n, xs, y.data_ptr(), yt, ys, wp, wn, _stream()),

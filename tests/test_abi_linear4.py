@@ -50,8 +50,11 @@ def test_bytes(L):
     wide = weights(cout=8208, cout_pad=8208)
     assert L.hatq_linear4_ws_bytes(ctypes.byref(wide), 2) == 0
     assert L.hatq_linear4_ws_bytes(ctypes.byref(wide), 3) == 16 * 4096 + 256
-    short = weights(cin=2000, k_stride=2048)
-    assert L.hatq_linear4_ws_bytes(ctypes.byref(short), 2 ** 24) == 0
+    short = weights(cin=1000, k_stride=1024)
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(short), 1000) == 0
+    assert L.hatq_linear4_ws_bytes(ctypes.byref(short), 2 ** 24) == (1024 << 24) + (4 << 24)
+    middle = weights(cin=2000, k_stride=2048)
+    assert [L.hatq_linear4_ws_bytes(ctypes.byref(middle), n) for n in (3, 4, 65)] == [0, 16 * 2048 + 256, 0]
     for rows in (0, -1, 2 ** 24 + 1):
         assert L.hatq_linear4_ws_bytes(ctypes.byref(w), rows) == 0
     assert L.hatq_linear4_ws_bytes(None, 17) == 0

@@ -236,9 +236,10 @@ def test_refusals():
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("gated", [False, True])
-@pytest.mark.parametrize("rows,cin,cout", [(1, 600, 20), (3, 2048, 33), (4, 2048, 33), (1, 1000, 8200), (2, 4096, 8200), (3, 4096, 8200), (4, 4000, 8192)])
+@pytest.mark.parametrize("rows,cin,cout", [(1, 600, 20), (3, 2048, 33), (4, 2048, 33), (1, 1000, 8200), (2, 4096, 8200), (3, 4096, 8200), (4, 4000, 8192),
+                                           (3, 2048, 8200), (70, 1504, 40), (90, 2048, 33)])
 def test_few_rows(rows, cin, cout, gated, dtype):
-    """The sizes at which a few rows change kernels."""
+    """The sizes at which rows change kernels."""
     rng = np.random.default_rng(rows + cin + cout)
     codes, scale, bias = layer(rng, cout * (2 if gated else 1), cin, 64, True)
     x = tokens(rng, rows, cin, dtype)
