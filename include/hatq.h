@@ -729,10 +729,11 @@ int32_t hatq_cache4_read(const hatq_cache4 *C, const hatq_heads *k, const hatq_h
  *   ws: device memory, 256-byte aligned, of at least hatq_attention4_ws_bytes bytes for
  *       the same sizes (ragged: ends is given); may be NULL where that is 0.  Calls that may
  *       overlap need workspaces of their own.
- * Scores, weights and sums are fp32.  Products: the transformed query in two fp16 halves,
- * 22 bits (many rows of bf16: one, 11 bits), against the codes; the weights times the
- * values' scales in fp16, off by 2^-11 of each or 2^-24 of the largest (if q or y is not
- * bf16, in two halves, 2^-21 of each).  No result depends on the order in which blocks run. */
+ * y may be q, with the same strides and type.  Scores, weights and sums are fp32.  Products:
+ * the transformed query in two fp16 halves, 22 bits (many rows of bf16: one, 11 bits),
+ * against the codes; the weights times the values' scales in fp16, off by 2^-11 of each or
+ * 2^-24 of the largest (if q or y is not bf16, in two halves, 2^-21 of each).  No result
+ * depends on the order in which blocks run. */
 size_t hatq_attention4_ws_bytes(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch,
                                 int32_t ragged, int32_t window, int32_t max_len);
 int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_heads *y, int32_t rows, int32_t q_heads,

@@ -260,9 +260,9 @@ __global__ void __launch_bounds__(64 * kWaves) linear4_small_kernel(const Linear
 // contraction in turn (they add up in LDS), the others channels further on.  Adjacent groups (and
 // a gated layer's gates and values) share the rows' codes: of those a wave reads 2 KB for 1 KB of
 // weights and 16 rows, and of long calls they are what the L2s give.
-// Few rows are bound by the weights' bytes: 6 rows, 8192 -> 2 x 16384, 27.4 us for 143 MB, 5.2
+// Few rows are bound by the weights' bytes: 6 rows, 8192 -> 2 x 16384, 25.4 us for 143 MB, 5.6
 // TB/s; many by the codes' loads, and by a conversion and a multiply-add for each sum and group:
-// 128 rows of 8192 -> 2 x 16384 66 us, 1040 TOP/s, as 2048 rows of 4096 -> 4096, 68 us.  (The next
+// 128 rows of 8192 -> 2 x 16384 63 us, 1090 TOP/s, as 2048 rows of 4096 -> 4096, 68 us.  (The next
 // step's loads over this one's products, in registers of their own: 5 to 12 % behind.)
 // The codes lie as the operands are, 1 KB for 16 rows by 64 input channels: by rows, adjacent
 // lanes are in 16 lines, a load is 64 accesses of the CU's cache instead of 16, and those bound

@@ -371,6 +371,49 @@ def test_another_stream():
     assert torch.equal(here, there)
 
 
+def test_pages_that_sequences_share():
+    """Sequences with the same first pages read them as if each had its own."""
+    s = Sequences([96, 80], 2, 64, 64, 16, torch.bfloat16, seed=101)
+    s.k[96:160], s.v[96:160] = s.k[:64].clone(), s.v[:64].clone()
+    s.write()
+    q = queries(s, [5, 5], 4, torch.bfloat16)
+    own = hatq.hatq_attention4(s.cache, q.to(DEV), s.table, s.lens)
+    table = s.table_np.copy()
+    table[1, :4] = table[0, :4]
+    assert torch.equal(own, hatq.hatq_attention4(s.cache, q.to(DEV), dev(table), s.lens))
+    table[0, 4] = table[0, 5]       # the same page twice in one sequence: its positions twice
+    y = hatq.hatq_attention4(s.cache, q.to(DEV), dev(table), s.lens, causal=False)
+    at = 5 * 16
+    s.k[64:80], s.v[64:80] = s.k[at:at + 16].clone(), s.v[at:at + 16].clone()
+    compare(s, q, [5, 5], y, causal=False)
+
+
+@pytest.mark.parametrize("lens,new", [([3000, 2900], 1), ([300, 200], 40), ([5000], 3)])
+def test_into_the_queries(lens, new):
+    """Results may take the queries' place."""
+    s = Sequences(lens, 2, 128, 64, 64, torch.bfloat16, seed=102)
+    s.write()
+    q = queries(s, [new] * len(lens), 8, torch.bfloat16).to(DEV)
+    y = hatq.hatq_attention4(s.cache, q, s.table, s.lens)
+    assert hatq.hatq_attention4(s.cache, q, s.table, s.lens, y=q) is q
+    assert torch.equal(q, y)
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own workspace (which a call makes itself)."""
+    s = Sequences([20000, 9000], 2, 128, 64, 64, torch.float16, seed=103)
+    s.write()
+    q = [queries(s, [1, 1], 16, torch.float16).to(DEV) for _ in range(2)]
+    alone = [hatq.hatq_attention4(s.cache, x, s.table, s.lens) for x in q]
+    assert hatq.hatq_attention4_ws_bytes(s.cache, 2, 16, s.table.shape[1], 2) > 0
+    side = [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        both = [hatq.hatq_attention4(s.cache, x, s.table, s.lens, stream=st) for x, st in zip(q, side)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(alone, both))
+
+
 def test_refusals():
     s = Sequences([30, 30], 2, 64, 64, 16, torch.float32, seed=97)
     s.write()
