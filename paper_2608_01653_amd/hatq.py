@@ -1232,9 +1232,11 @@ def hatq_cache4_read(cache: Cache4, rows: int, table: torch.Tensor, lens: torch.
             return hatq_cache4_read(cache, rows, table, lens, ends, out_dtype, k, v)
     _sizes("rows", rows)
     new = torch.empty if ends is None else torch.zeros
-    if k is None:
+    if k is None and v is None:     # (one allocation, and one launch that clears it)
+        k, v = new((2, rows, cache.heads, cache.dim), dtype=out_dtype, device=cache.buf.device).unbind(0)
+    elif k is None:
         k = new((rows, cache.heads, cache.dim), dtype=out_dtype, device=cache.buf.device)
-    if v is None:
+    elif v is None:
         v = new((rows, cache.heads, cache.dim), dtype=out_dtype, device=cache.buf.device)
     _, _, hk = _heads(k, "k", cache.dim, cache.heads, rows)
     _, _, hv = _heads(v, "v", cache.dim, cache.heads, rows)
@@ -1267,7 +1269,9 @@ def hatq_attention4(cache: Cache4, q: torch.Tensor, table: torch.Tensor, lens: t
     n, h, hq = _heads(q, "q", cache.dim)
     if y is None:
         y = (q.new_empty if ends is None else q.new_zeros)((n, h, cache.dim), dtype=out_dtype or q.dtype)
-    _, _, hy = _heads(y, "y", cache.dim, h, n)
+        hy = Heads(_dtype(y.dtype, "y"), max(h, 1) * cache.dim, cache.dim, y.data_ptr())
+    else:
+        _, _, hy = _heads(y, "y", cache.dim, h, n)
     batch, width = _places(cache, n, table, lens, ends)
     _sizes("window, max_len", window, max_len)
     _here(cache.device, q, y, table, lens, ends, ws)
