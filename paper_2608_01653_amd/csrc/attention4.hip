@@ -631,6 +631,10 @@ __global__ void __launch_bounds__(1024) attention4_join_kernel(const AttentionAr
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int j = 0; j < 4; ++j) s.o[b][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    // (two parts under way at once: 2 sequences of 131072 48.9 -> 48.1 us; heads of more than 128
+    // channels have no registers for it)
+    constexpr int kParts = NB <= 2 ? 2 : 1;
+#pragma unroll kParts
     for (int k = wave; k < a.splits; k += waves) {
         const char *part = parts + k * (int64_t)(NB * 4096 + 128);
         const float *ml = reinterpret_cast<const float *>(part + NB * 4096);
