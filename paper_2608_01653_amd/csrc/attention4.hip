@@ -52,12 +52,10 @@ __device__ __forceinline__ float chunks_sum(float v) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// a b and c d, exact products rounded once, as two float16.  (Written out: the compiler rounds
-// each to float32, or packs the halves in an instruction of its own.)
+// a b and c d as two float16: the sum with 0 lets the compiler join a product and its rounding in
+// one instruction, and it keeps the waits that a matrix instruction needs behind it.
 __device__ __forceinline__ uint32_t product_pair(float a, float b, float c, float d) {
-    uint32_t r;
-    asm("v_fma_mixlo_f16 %0, %1, %2, 0\n\tv_fma_mixhi_f16 %0, %3, %4, 0" : "=&v"(r) : "v"(a), "v"(b), "v"(c), "v"(d));
-    return r;
+    return __builtin_bit_cast(uint32_t, v2h{(_Float16)__builtin_fmaf(a, b, 0.0f), (_Float16)__builtin_fmaf(c, d, 0.0f)});
 }
 
 // ---- which rows a tile has --------------------------------------------------------
