@@ -11,9 +11,12 @@
 // First product: the codes in float16, exact, against the query in two float16 halves, 22
 // bits (many rows of bf16: one half, 11 bits), after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
-// kept relative to the largest of w s_v (not of w) or to one up to 2^8 smaller, so the
-// float16 range holds whatever the scales are (2^-100 to 2^100): off by 2^-11 of each weight
-// or 2^-25 of the largest.  For float16 and float32 results NP = 2 halves carry 22 bits of it.
+// kept in a unit that the largest w s_v (not w) so far passes by 2^12 to 2^15, so that the
+// largest fits float16 whatever the scales are (2^-100 to 2^100) and small ones have all of its
+// range below: off by 2^-11 of each (for float16 and float32 results in NP = 2 halves, 2^-21), or
+// by half of float16's least step, 2^-37 of the largest.  One unit serves a head's groups of 64
+// channels, so the largest is that of all of them: a group whose scales are that far below
+// another's is lost.
 #include "cache4_device.h"
 
 #ifndef HATQ_ATTENTION_PART
@@ -189,8 +192,14 @@ __device__ __forceinline__ void see(const AttentionArgs &a, const ColTile &t, in
 template <int NB>
 struct Sums {
     v4f o[NB][4];       // [block][channel of the run]: runs are rows, columns lanes
-    float m, l;         // the largest log2 of a weight so far; this lane's sum of weights
+    float m, l;         // log2 of the unit of a weight; this lane's sum of weights, times kSumDown
 };
+// log2 of where the unit is put, below the largest weight, and of where that may grow to before the
+// unit follows.  (2^7 and 2^15 took as long, and kept 5 bits less of small weights.)
+constexpr float kUnitBelow = 12.0f, kUnitFollows = 15.0f;
+// A weight without its scale is up to 2^115: sums of 2^24 of them stay finite.
+constexpr int kSumDownLog = 12;
+constexpr float kSumDown = 0x1p-12f;
 
 // One step's operands as they lie in memory.  Each part is loaded again, for the step after,
 // as soon as it has been used, so a step's loads are under way over the rest of the step
@@ -352,10 +361,11 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
         }
         most = chunks_max(most);
         if (kBits) most = __builtin_fmaf(most, 0x1p-7f, -127.0f);
-        // (A weight may be up to 2^8 of the unit before the unit follows: float16 has room for
+        // (A weight may be up to 2^15 of the unit before the unit follows: float16 has room for
         // that, and most columns' largest grows by less after its first step.)
-        if (__any(most > o.m + 8.0f)) {
-            const float m = most > o.m ? most : o.m, down = __builtin_amdgcn_exp2f(o.m - m);
+        if (__any(most > o.m + kUnitFollows)) {
+            const float to = most - kUnitBelow;
+            const float m = to > o.m ? to : o.m, down = __builtin_amdgcn_exp2f(o.m - m);
             o.m = m;
             o.l *= down;
 #pragma unroll
@@ -363,12 +373,15 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o.o[b][j] *= down;
         }
+        // (a step's weights among themselves first: alone, small ones are lost beside a large sum)
+        float all = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t[n][j], q[n].step, -o.m));
             t[n][j] = !EDGE || (seen[n] >> j & 1) ? p : 0.0f;
-            o.l += t[n][j];
+            all = j ? all + t[n][j] : t[n][j];
         }
+        o.l = __builtin_fmaf(all, kSumDown, o.l);
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -470,7 +483,7 @@ __device__ __forceinline__ void store_columns(const AttentionArgs &a, const ColT
     const int lane = threadIdx.x & 63, chunk = lane >> 4, c = t.col0 + col + (lane & 15);
     float v[NB][16];
     // (l = 0: no position is seen, and the sums are 0)
-    const float by = l == 0.0f ? 0.0f : __uint_as_float((uint32_t)(127 - a.c.log_b) << 23) / l;
+    const float by = l == 0.0f ? 0.0f : __uint_as_float((uint32_t)(127 - kSumDownLog - a.c.log_b) << 23) / l;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
