@@ -44,7 +44,8 @@ __device__ __forceinline__ uint8_t *octet_of(const Cache4 &c, int page, int head
 // but the clamp of a maximum up to 7.03 steps away.
 // Codes without a division for each: with r within 2^-23 of 1 / s, v r and v / s differ by at
 // most 7.03 (2^-23 + 2^-24) < 2^-19, so k = rne(v r) is rne(fl(v / s)) where v r is within
-// 0.5 - 2^-16 of k; a chunk with a value nearer to the middle of two codes divides.
+// 0.5 - 2^-16 of k; a chunk with a value nearer to the middle of two codes divides, or clears
+// its codes if the head is not fine.
 // LB: log2 of the transform's block, -1 where it is known at run time only.
 // Bound by the instructions next to the bytes: 32768 rows of 8 heads of 128, bf16, of a fused
 // query-key-value product: 50 us for 170 MB (a copy of as many 33), 613 vector instructions a
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs
             }
             off = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(d[0]), fabsf(d[1])), off);
         }
-        if (!(off <= 0.5f - 0x1p-16f)) {
+        if (!(fine && off <= 0.5f - 0x1p-16f)) {
             asm volatile("");   // a branch: else the compiler divides for every chunk and selects
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
