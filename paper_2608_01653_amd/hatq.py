@@ -1016,6 +1016,9 @@ def hatq_expert_mlp(w_in: PreparedLinear, w_out: PreparedLinear, x: torch.Tensor
     return y
 
 
+_LINEAR4_ROWS = 1 << 24     # the most rows of a call
+
+
 @dataclass
 class PreparedLinear4:
     """Prepared 4-bit linear weights: the device buffer and the C view into it."""
@@ -1029,9 +1032,15 @@ class PreparedLinear4:
     def __post_init__(self):
         self.ref = ctypes.byref(self.w)
         self.device = self.buf.get_device()
-        # rows up to which a short contraction's call needs no workspace (hatq_linear4_ws_bytes
-        # knows the rest)
-        self.rows = (1 << 22) // (self.k_stride * self.w.cout_pad // 16) * 16 if self.k_stride <= 1024 else 0
+        # the rows up to which a call needs no workspace, as the library has it (of more rows, a call asks
+        # hatq_linear4_ws_bytes)
+        none, some = 0, 1
+        while some <= _LINEAR4_ROWS and not load().hatq_linear4_ws_bytes(self.ref, some):
+            none, some = some, 2 * some
+        while some - none > 1 and none < _LINEAR4_ROWS:
+            half = (none + some) // 2
+            none, some = (none, half) if load().hatq_linear4_ws_bytes(self.ref, half) else (half, some)
+        self.rows = none
 
 
 def _linear4(call: str, w: torch.Tensor, gated: bool, hblock: int, group: int, run) -> PreparedLinear4:
@@ -1112,7 +1121,7 @@ def hatq_linear4_forward(lin: PreparedLinear4, x: torch.Tensor, out_dtype: Optio
     n, _, xs, xt = _rows(x, "x", lin.cin)
     y, ys, yt = _out_rows(y, n, lin.cout, out_dtype or x.dtype, x)
     _here(lin.device, x, y, ws)
-    if ws is None and n > lin.rows and n * lin.k_stride > HATQ_TOKEN_CODES // 4:    # (else it needs none)
+    if ws is None and n > lin.rows:
         nbytes = load().hatq_linear4_ws_bytes(lin.ref, n)
         if nbytes:
             ws = x.new_empty(nbytes, dtype=torch.int8)
