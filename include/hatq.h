@@ -605,7 +605,8 @@ int32_t hatq_expert_mlp(const hatq_linear_weights *W_in, const hatq_linear_weigh
  * with exact sums in each group and fp32 sums over the groups; y from z as there, gated or
  * not.  A NaN among a channel's scales makes its outputs NaN, a token that is not finite
  * its own.
- * Any number of rows is taken; the kernels are made for up to about 128. */
+ * Any number of rows is taken; the kernels are made for up to about 128.  Outputs and the
+ * workspace do not overlap the inputs. */
 typedef struct {
     int32_t cin, cout;
     int32_t gated;          /* 1: holds 2 cout channels, gives cout */
@@ -680,15 +681,16 @@ int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32
  * last end stay as they are.
  *
  * Tensors [rows][heads][dim] have a stride in elements between rows and between heads,
- * and adjacent channels; outputs' rows and heads do not overlap.  Any alignment of the
- * type.  rows <= 2^24; no rows: HATQ_OK, nothing launched.  A sequence has at most 2^30
+ * and adjacent channels; outputs' rows and heads do not overlap, nor do outputs each other, the
+ * cache, the workspace or inputs, but where it says so.  Any alignment of the type.  rows <= 2^24; no rows: HATQ_OK, nothing launched.  A sequence has at most 2^30
  * positions (width page_size, else HATQ_EUNSUPPORTED). */
 typedef struct {
     int32_t pages;
     int32_t page_size;      /* positions, a power of two in [16, 65536] */
     int32_t heads, dim;     /* of the keys and values */
     int32_t hblock;         /* transform block on dim, a power of two in [1, 128] */
-    void *buf;              /* library-internal layout, 68 bytes for 64 codes of both */
+    void *buf;              /* library-internal layout: a position's key and value 68 bytes for each 64
+                               channels of a head, the last ones whole */
 } hatq_cache4;
 
 typedef struct {

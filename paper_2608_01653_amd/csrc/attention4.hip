@@ -13,10 +13,11 @@
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
 // kept in a unit that the largest w s_v (not w) so far passes by 2^12 to 2^15, so that the
 // largest fits float16 whatever the scales are (2^-100 to 2^100) and small ones have all of its
-// range below: off by 2^-11 of each (for float16 and float32 results in NP = 2 halves, 2^-21), or
-// by half of float16's least step, 2^-37 of the largest.  One unit serves a head's groups of 64
-// channels, so the largest is that of all of them: a group whose scales are that far below
-// another's is lost.
+// range below: off by 2^-11 of each (for float16 and float32 results in NP = 2 halves, 2^-21; bf16
+// outputs round by 2^-8 themselves, and two halves, of the queries too, take 13 % more for 64 tokens
+// of 16384 positions and 43 % for prompts), or by half of float16's least step, 2^-37 of the
+// largest.  One unit serves a head's groups of 64 channels, so the largest is that of all of them: a
+// group whose scales are that far below another's is lost.
 #include "cache4_device.h"
 
 #ifndef HATQ_ATTENTION_PART
@@ -554,8 +555,8 @@ __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, cha
 // way each (64 sequences of 16384, 8 heads of 128 channels: 226 us for 1.09 GB, 4.8 TB/s), behind 6
 // to 8 us for the query, the first loads and the waves' sums (2 sequences of 131072, 4 heads:
 // 44 us for 143 MB); many columns, the vector instructions of weights and codes beside the matrix
-// ones (parts of prompts, 2048 rows over 4096 to 8192 positions, 16 heads over 2 of 128: 350 us,
-// 590 TFLOP/s of 1200 that a large float16 product reaches).
+// ones, and blocks of unlike length (the last 1365 rows of prompts of 5461 to 8192 positions, three of
+// them, 16 heads over 2 of 128: 350 us, 590 TFLOP/s of 1200 that a large float16 product reaches).
 template <int NB, int NP, int NQ, bool HALF>
 __global__ void __launch_bounds__(NQ > 1 ? 256 : NB <= 2 ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(NB <= 2 && NQ == 1 ? 4 : 2)))
 attention4_kernel(const AttentionArgs a) {

@@ -28,7 +28,7 @@ AttentionPlan plan_attention(int32_t batch, int32_t rows, int32_t heads, int32_t
     // block would share its CU (at 16 to 64 steps 16 are behind: 1 token of 4 sequences of 1024 15.6
     // us for 14.4), fewer where a sequence is shorter.  (us a call in a graph, 8
     // heads of 128 channels, bf16: 1 sequence of 8192 in 8 parts 18.2, in 16 16.2, in 32 16.6;
-    // 8 of 4096 in 1 part 26, in 4 20.8, in 8 22.1; 32 of 820 to 4096 whole, 8 waves 35.6, 16
+    // 8 of 4096 in 1 part 26, in 4 20.8, in 8 22.1; 32 of 921 to 4096 whole, 8 waves 35.6, 16
     // 33.6, in 2 parts 34.7; 2 of 131072, 4 heads, fp16, 32 parts, 8 waves 48.3, 16 46.8; 1 of
     // 300, 64 channels, 4 waves 8.3, 8 7.9, 16 8.9.)
     int64_t most = max_len;

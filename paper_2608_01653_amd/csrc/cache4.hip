@@ -40,7 +40,7 @@ __device__ __forceinline__ uint8_t *octet_of(const Cache4 &c, int page, int head
 // S = B x of a head, A = max |S| of each 64 channels, s = bf16(fl32(A / 7)), codes
 // clamp(rne(fl32(S / s)), -7, 7); a head with a value that is not below 2^102 gets scales
 // NaN and codes 0.  bf16 scales: the range of the floats that come in, at 2 bytes for 32 of
-// codes; the codes are made with the rounded scale, so the rounding (2^-9) costs nothing
+// codes; the codes are made with the rounded scale, so the rounding (2^-8) costs nothing
 // but the clamp of a maximum up to 7.03 steps away.
 // Codes without a division for each: with r within 2^-23 of 1 / s, v r and v / s differ by at
 // most 7.03 (2^-23 + 2^-24) < 2^-19, so k = rne(v r) is rne(fl(v / s)) where v r is within
@@ -48,7 +48,7 @@ __device__ __forceinline__ uint8_t *octet_of(const Cache4 &c, int page, int head
 // its codes if the head is not fine.
 // LB: log2 of the transform's block, -1 where it is known at run time only.
 // Bound by the instructions next to the bytes: 32768 rows of 8 heads of 128, bf16, of a fused
-// query-key-value product: 50 us for 170 MB (a copy of as many 33), 613 vector instructions a
+// query-key-value product: 49 us for 170 MB (a copy of as many 33), 616 vector instructions a
 // wave that take 33 us by themselves (224 of them the 7 butterfly stages of 32 values a lane).
 template <int NB, int LB>
 __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs a, int log_heads) {
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) cache4_append_kernel(const CacheArgs
     }
 }
 
-// x' = B (s c) / b: what the codes stand for, 0 where there is no page.  As many rows as above: 34 to 36
+// x' = B (s c) / b: what the codes stand for, 0 where there is no page.  As many rows as above: 33 to 36
 // us for 170 MB, 5 TB/s, with 550 vector instructions a wave that take 29.
 template <int NB, int LB>
 __global__ void __launch_bounds__(kThreads) cache4_read_kernel(const CacheArgs a, int log_heads) {
