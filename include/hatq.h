@@ -681,9 +681,10 @@ int32_t hatq_linear4_forward(const hatq_linear4_weights *W, const void *x, int32
  * last end stay as they are.
  *
  * Tensors [rows][heads][dim] have a stride in elements between rows and between heads,
- * and adjacent channels; outputs' rows and heads do not overlap, nor do outputs each other, the
- * cache, the workspace or inputs, but where it says so.  Any alignment of the type.  rows <= 2^24; no rows: HATQ_OK, nothing launched.  A sequence has at most 2^30
- * positions (width page_size, else HATQ_EUNSUPPORTED). */
+ * and adjacent channels; outputs' rows and heads do not overlap, nor do outputs and the workspace
+ * overlap each other, the cache or inputs, unless said below.  Any alignment of the type.
+ * rows <= 2^24; no rows: HATQ_OK, nothing launched.  A sequence has at most 2^30 positions
+ * (width page_size, else HATQ_EUNSUPPORTED). */
 typedef struct {
     int32_t pages;
     int32_t page_size;      /* positions, a power of two in [16, 65536] */
