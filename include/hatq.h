@@ -738,8 +738,10 @@ int32_t hatq_cache4_read(const hatq_cache4 *C, const hatq_heads *k, const hatq_h
  * scales in fp16, off by 2^-11 of each (if q or y is not bf16, in two halves, 2^-21 of each) or
  * by 2^-37 of the head's largest, that of all its groups of 64 channels.  So a group whose
  * scales are 2^-r of another's in the same positions has an error of up to 2^(r-37) of its own
- * largest, and from 2^-38 on it can be lost.  No result depends on the order in which blocks
- * run. */
+ * largest, and from 2^-38 on it can be lost.  The values of a query's transform are off by up to
+ * 2^-38 of its head's largest alike.  Scores up to 2^120 in magnitude give numbers: where float32
+ * no longer resolves their softmax, a mean of the values at the top.  No result depends on the
+ * order in which blocks run. */
 size_t hatq_attention4_ws_bytes(const hatq_cache4 *C, int32_t rows, int32_t q_heads, int32_t width, int32_t batch,
                                 int32_t ragged, int32_t window, int32_t max_len);
 int32_t hatq_attention4(const hatq_cache4 *C, const hatq_heads *q, const hatq_heads *y, int32_t rows, int32_t q_heads,

@@ -9,7 +9,8 @@
 // rows so that a lane's scores are the second product's operand as they are.
 //
 // First product: the codes in float16, exact, against the query in two float16 halves, 22
-// bits (many rows of bf16: one half, 11 bits), after a power of two that puts its largest value at 2^13 to 2^14; fp32 sums.
+// bits (many rows of bf16: one half, 11 bits) or 2^-38 of its largest value, after a power of two that
+// puts that at 2^13 to 2^14; fp32 sums.
 // Second product: weights w s_v in float16 against the codes in float16, exact.  A weight is
 // kept in a unit that the largest w s_v (not w) so far passes by 2^12 to 2^15, so that the
 // largest fits float16 whatever the scales are (2^-100 to 2^100) and small ones have all of its
@@ -198,6 +199,9 @@ struct Sums {
 // log2 of where the unit is put, below the largest weight, and of where that may grow to before the
 // unit follows.  (2^7 and 2^15 took as long, and kept 5 bits less of small weights.)
 constexpr float kUnitBelow = 12.0f, kUnitFollows = 15.0f;
+// From here on (a score's magnitude, times log2 e) float32 no longer holds a unit to a small part of a
+// power of two.
+constexpr float kLargeScore = 0x1p20f;
 // A weight without its scale is up to 2^115: sums of 2^24 of them stay finite.
 constexpr int kSumDownLog = 12;
 constexpr float kSumDown = 0x1p-12f;
@@ -281,10 +285,11 @@ __device__ __forceinline__ float scale_of(const v4u &w, int j) {
 }
 
 // One step of 32 positions from p0 on by NQ times sixteen columns, and the next one's loads.
-// EDGE: some positions may be hidden from some columns.
+// EDGE: some positions may be hidden from some columns.  large: 1 once a column's largest score
+// was kLargeScore or more.
 template <int NB, int NP, int NQ, bool EDGE, bool HALF>
 __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const StepAt &next, const LaneAt &mine, const Query (&q)[NQ],
-                                     const char *query, int p0, Sums<NB> (&sum)[NQ]) {
+                                     const char *query, int p0, Sums<NB> (&sum)[NQ], uint32_t &large) {
     const int lane = threadIdx.x & 63;
     const int first = p0 + 8 * (lane >> 4);
     float t[NQ][8];
@@ -364,21 +369,33 @@ __device__ __forceinline__ void step(Step<NB> &s, const StepAt &here, const Step
         if (kBits) most = __builtin_fmaf(most, 0x1p-7f, -127.0f);
         // (A weight may be up to 2^15 of the unit before the unit follows: float16 has room for
         // that, and most columns' largest grows by less after its first step.)
-        if (__any(most > o.m + kUnitFollows)) {
-            const float to = most - kUnitBelow;
-            const float m = to > o.m ? to : o.m, down = __builtin_amdgcn_exp2f(o.m - m);
+        if (__builtin_expect(__any(most > o.m + kUnitFollows) || large, 0)) {
+            // (NaN stays; two float32 steps less, so that rounding does not leave the largest below)
+            const float to = __builtin_fmaf(fabsf(most), -0x1p-22f, most - kUnitBelow);
+            const float m = to <= o.m ? o.m : to, down = __builtin_amdgcn_exp2f(o.m - m);
             o.m = m;
             o.l *= down;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o.o[b][j] *= down;
+            if (__any(fabsf(most) >= kLargeScore && most > -__builtin_inff())) large = 1;
         }
         // (a step's weights among themselves first: alone, small ones are lost beside a large sum)
         float all = 0.0f;
 #pragma unroll
+        for (int j = 0; j < 8; ++j) t[n][j] = __builtin_fmaf(t[n][j], q[n].step, -o.m);
+        if (__builtin_expect(large != 0, 0)) {
+            // The unit may be off by several powers of two, as the scores themselves are: a weight
+            // above 2^15 of it is taken as that much, for float16 would not hold it.
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                t[n][j] = __builtin_elementwise_minimum(
+                    t[n][j], kBits ? __builtin_fmaf(lv[j], -0x1p-7f, kUnitFollows + 127.0f) : kUnitFollows - lv[j]);
+        }
+#pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(t[n][j], q[n].step, -o.m));
+            const float p = __builtin_amdgcn_exp2f(t[n][j]);
             t[n][j] = !EDGE || (seen[n] >> j & 1) ? p : 0.0f;
             all = j ? all + t[n][j] : t[n][j];
         }
@@ -439,6 +456,7 @@ struct Walk {
     Step<NB> s;
     StepAt here;
     Pages pages;
+    uint32_t large = 0;
 
     // (the step after a wave's last one: the same again, not used)
     __device__ __forceinline__ int after(int p) const { return p + stride < to ? p + stride : p; }
@@ -462,7 +480,7 @@ struct Walk {
     __device__ __forceinline__ void one(int p, const Query (&q)[NQ], const char *query, Sums<NB> (&sum)[NQ]) {
         const StepAt next = step_at<NB, HALF>(a.c, head0, mine, pages, after(p));
         pages = pages_of<HALF>(a.c, a.at, table, after(after(p)));
-        step<NB, NP, NQ, EDGE, HALF>(s, here, next, mine, q, query, p, sum);
+        step<NB, NP, NQ, EDGE, HALF>(s, here, next, mine, q, query, p, sum, large);
         here = next;
     }
     template <int NP, int NQ>
