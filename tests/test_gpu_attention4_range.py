@@ -93,6 +93,38 @@ def test_groups_of_a_head_far_apart(dim, hblock, dtype, apart):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("apart", [6, 12, 20, 26])
+@pytest.mark.parametrize("dim,hblock", [(128, 64), (128, 1), (192, 32), (80, 16)])
+def test_queries_and_keys_far_apart(dim, hblock, apart, dtype):
+    """A group of 64 channels with small queries and keys as much larger: it counts as the others.  A
+    query's value is also off by half of float16's least step where its largest is at least 2^13,
+    2^-38 of it, which moves a score by that of the sum of |k|: row64's error of a score, 2 of it a
+    weight, is made larger by as much."""
+    s = Sequences([300], 8, dim, hblock, 16, torch.float32, seed=dim + apart)
+    s.k[..., 64:] *= 2.0 ** apart
+    q = torch.from_numpy(s.rng.normal(size=(1, 16, dim)).astype(np.float32))
+    q[..., 64:] *= 2.0 ** -apart
+    q = q.to(dtype)
+    s.write()
+    fine = dtype != torch.bfloat16
+    many = q.unflatten(1, (8, 2)).repeat_interleave(4, dim=2).flatten(1, 2).expand(ROWS, -1, -1)
+    k, v = s.of(0)
+    for rows in (q, many):
+        y = hatq.hatq_attention4(s.cache, rows.to(DEV), s.table, s.lens, causal=False, out_dtype=dtype)
+        per = rows.shape[1] // 8
+        for h in range(0, rows.shape[1], 3):
+            one = rows[0, h].float().numpy()
+            y64, off = row64(one, k[:, h // per], v[:, h // per], hblock, dim ** -0.5, fine)
+            (ck, sk), (cv, sv) = ([x.astype(np.float64) for x in quantize(x[:, h // per], hblock)] for x in (k, v))
+            t = (ck * sk) @ butterfly(one.astype(np.float64), hblock) * (dim ** -0.5 / hblock)
+            w = np.exp(t - t.max()) / np.exp(t - t.max()).sum()
+            qt = np.abs(butterfly(one.astype(np.float64), hblock)).max()
+            more = np.expm1(2 * 2.0 ** -38 * qt * np.abs(ck * sk).sum(1).max() * (dim ** -0.5 / hblock))
+            off = off + more * butterfly_abs((w @ np.abs(cv * sv))[None], hblock)[0]
+            check(y[0, h].cpu(), y64, off, f"head {h} of {rows.shape[1]}")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_weights_that_grow(dtype):
     """Every step's largest weight a little or a lot above the one before."""
     for nats in (0.5, 2.0, 5.0, 9.0):
