@@ -574,7 +574,7 @@ __device__ __forceinline__ void join_waves(Sums<NB> &s, int wave, int waves, cha
 // to 8 us for the query, the first loads and the waves' sums (2 sequences of 131072, 4 heads:
 // 44 us for 143 MB); many columns, the vector instructions of weights and codes beside the matrix
 // ones, and blocks of unlike length (the last 1365 rows of prompts of 5461 to 8192 positions, three of
-// them, 16 heads over 2 of 128: 350 us, 590 TFLOP/s of 1200 that a large float16 product reaches).
+// them, 16 heads over 2 of 128: 355 us, 580 TFLOP/s of 1200 that a large float16 product reaches).
 template <int NB, int NP, int NQ, bool HALF>
 __global__ void __launch_bounds__(NQ > 1 ? 256 : NB <= 2 ? 1024 : 512) __attribute__((amdgpu_waves_per_eu(NB <= 2 && NQ == 1 ? 4 : 2)))
 attention4_kernel(const AttentionArgs a) {
